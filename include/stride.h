@@ -85,7 +85,7 @@ extern "C" {
 typedef enum stride_status {
   STRIDE_OK = 0,
   STRIDE_ERR_INVALID_ARG = 1,        /* a pointer, size, mode or layout is invalid */
-  STRIDE_ERR_UNSUPPORTED_DTYPE = 2,  /* dtype is not BF16 or F32 */
+  STRIDE_ERR_UNSUPPORTED_DTYPE = 2,  /* dtype is not one that the call takes (here BF16 or F32) */
   STRIDE_ERR_WORKSPACE = 3,          /* workspace missing, too small or misaligned */
   STRIDE_ERR_CUDA = 4,               /* a CUDA runtime call or launch failed */
   STRIDE_ERR_UNSUPPORTED_DEVICE = 5, /* current device is not compute capability 10.3 */

@@ -15,6 +15,10 @@ Per-trajectory state and per-turn statistics are opaque byte tensors
 (``[n, 80]`` and ``[n, 40]`` uint8) laid out as ``stride_scan_state`` and
 ``stride_turn_stats``; :func:`state_to_numpy` / :func:`turn_stats_to_numpy`
 view copies of them as numpy structured arrays.
+
+The calls around the scoring in a rollout's decode step (norm and rotation,
+paged cache, attention of drafted tokens, sampling; include/stride_decode.h)
+are in :mod:`.decode` and part of this namespace.
 """
 from __future__ import annotations
 
@@ -117,6 +121,7 @@ def lib() -> ctypes.CDLL:
                    "stride_score_batch_noalloc", "stride_score_step_compact", "stride_force_batch_kernel",
                    "stride_force_step_shape"):
             getattr(L, fn).restype = ctypes.c_int
+        decode.declare(L)
         _LIB = L
     return _LIB
 
@@ -157,7 +162,7 @@ def _native():
 
 _NATIVE_ENTRIES = ("state_init", "score_batch", "score_batch_noalloc", "score_batch_multi_teacher", "score_step",
                    "score_step_compact", "select_restart", "buffer_record", "partial_lse", "combine_partials",
-                   "scan_logprobs")
+                   "scan_logprobs", "qk_norm_rope", "qk_norm_rope_backward", "kv_append", "tree_attention", "sample")
 
 
 def stride_status_string(code: int) -> str:
@@ -610,3 +615,9 @@ def stride_score_batch_noalloc(S, T, tokens, traj_row_off, turn_row_off, traj_tu
         _dev(profile, "profile", torch.float64, 3 * PROFILE_BINS, optional=True),
         _dev(dev_status, "dev_status", torch.int32, 1, optional=True), _stream(stream))
     _check("stride_score_batch_noalloc", rc)
+
+
+from . import decode  # noqa: E402  (the decode step's calls, written with the helpers above)
+from .decode import *  # noqa: E402,F401,F403
+
+__all__ += decode.__all__

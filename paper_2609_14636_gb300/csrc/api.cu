@@ -15,6 +15,10 @@ namespace {
 constexpr int kMaxDevices = 64;
 std::atomic<int> g_device_ok[kMaxDevices];  // 0 unknown, 1 sm_103, 2 other
 
+}  // namespace
+
+namespace stride {
+
 int check_device() {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return STRIDE_ERR_CUDA;
@@ -30,6 +34,12 @@ int check_device() {
   }
   return s == 1 ? STRIDE_OK : STRIDE_ERR_UNSUPPORTED_DEVICE;
 }
+
+}  // namespace stride
+
+namespace {
+
+using stride::check_device;
 
 size_t dtype_bytes(int32_t dtype) {
   return dtype == STRIDE_DTYPE_BF16 ? 2 : (dtype == STRIDE_DTYPE_F32 ? 4 : 0);
@@ -63,7 +73,7 @@ const char* stride_status_string(int code) {
   switch (code) {
     case STRIDE_OK: return "STRIDE_OK";
     case STRIDE_ERR_INVALID_ARG: return "STRIDE_ERR_INVALID_ARG: invalid pointer, size, mode or layout";
-    case STRIDE_ERR_UNSUPPORTED_DTYPE: return "STRIDE_ERR_UNSUPPORTED_DTYPE: dtype must be BF16 or F32";
+    case STRIDE_ERR_UNSUPPORTED_DTYPE: return "STRIDE_ERR_UNSUPPORTED_DTYPE: dtype is not one that the call takes";
     case STRIDE_ERR_WORKSPACE: return "STRIDE_ERR_WORKSPACE: workspace missing, too small or not 256-byte aligned";
     case STRIDE_ERR_CUDA: return "STRIDE_ERR_CUDA: a CUDA runtime call or kernel launch failed";
     case STRIDE_ERR_UNSUPPORTED_DEVICE: return "STRIDE_ERR_UNSUPPORTED_DEVICE: the current device is not sm_103 (GB300)";

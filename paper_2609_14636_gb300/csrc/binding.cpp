@@ -24,7 +24,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "stride.h"
+#include "stride_decode.h"
 
 namespace {
 
@@ -40,6 +40,11 @@ struct Entry {
   decltype(&stride_partial_lse) partial_lse;
   decltype(&stride_combine_partials) combine_partials;
   decltype(&stride_scan_logprobs) scan_logprobs;
+  decltype(&stride_qk_norm_rope) qk_norm_rope;
+  decltype(&stride_qk_norm_rope_backward) qk_norm_rope_backward;
+  decltype(&stride_kv_append) kv_append;
+  decltype(&stride_tree_attention) tree_attention;
+  decltype(&stride_sample) sample;
 } g_entry;
 
 const char* const kRowOutputs[] = {"logp_s", "logp_t", "opd", "lse_s", "lse_t", "x_s", "x_t"};
@@ -446,6 +451,168 @@ int scan_logprobs(PyObject* const* a) {
   });
 }
 
+// ---- the decode step (stride_decode.h) ----
+int32_t row_dtype(at::ScalarType t) {
+  if (t == at::kBFloat16) return STRIDE_DTYPE_BF16;
+  if (t == at::kHalf) return STRIDE_DTYPE_F16;
+  need(t == at::kFloat);
+  return STRIDE_DTYPE_F32;
+}
+
+bool truth(PyObject* o) {
+  need(o == Py_True || o == Py_False);
+  return o == Py_True;
+}
+
+// Head rows [N, heads, D]; those after the first share its type, N and D.
+struct HeadRows {
+  stride_head_rows r;
+  at::ScalarType type;
+  int64_t N, D;
+  explicit HeadRows(PyObject* o) {
+    const at::Tensor& t = tensor(o);
+    need(t.dim() == 3 && (t.size(2) <= 1 || t.stride(2) == 1) && t.size(1) <= INT32_MAX && t.size(2) <= INT32_MAX);
+    type = t.scalar_type();
+    N = t.size(0);
+    D = t.size(2);
+    r = {t.data_ptr(), t.stride(0), t.stride(1), (int32_t)t.size(1)};
+  }
+  HeadRows(PyObject* o, const HeadRows& like) : HeadRows(o) { need(type == like.type && N == like.N && D == like.D); }
+};
+
+// pos, cos, sin at a[0..2]
+stride_norm_rope norm_rope(PyObject* const* a, PyObject* q_weight, PyObject* k_weight, PyObject* eps, PyObject* interleaved,
+                           const HeadRows& like) {
+  stride_norm_rope h = {};
+  h.q_weight = dev_or_null(q_weight, like.type, like.D);
+  h.k_weight = dev_or_null(k_weight, like.type, like.D);
+  h.eps = real(eps);
+  h.interleaved = truth(interleaved);
+  if (a[1] == Py_None && a[2] == Py_None) return h;
+  const at::Tensor &c = tensor(a[1]), &s = tensor(a[2]);
+  need(c.dim() == 2 && s.dim() == 2 && c.size(0) == s.size(0) && c.size(1) == s.size(1) && c.size(1) <= INT32_MAX / 2);
+  h.rot_dim = (int32_t)(2 * c.size(1));
+  h.pos = dev_as<const int32_t>(a[0], at::kInt, like.N);
+  h.cos_table = dev_as<const float>(a[1], at::kFloat);
+  h.sin_table = dev_as<const float>(a[2], at::kFloat);
+  h.table_rows = c.size(0);
+  return h;
+}
+
+// k_cache, v_cache, block_table, ctx_len, tok_off
+stride_paged_cache paged_cache(PyObject* const* a, const HeadRows& like) {
+  const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &t = tensor(a[2]);
+  need(k.dim() == 4 && v.dim() == 4 && (k.size(3) <= 1 || k.stride(3) == 1) && k.scalar_type() == like.type &&
+       v.scalar_type() == like.type && k.size(3) == like.D && t.dim() == 2 && t.size(0) < INT32_MAX);
+  for (int i = 0; i < 4; ++i) need(k.size(i) == v.size(i) && k.stride(i) == v.stride(i) && k.size(i) <= INT32_MAX);
+  const int64_t n = t.size(0);
+  return {k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(0), (int32_t)k.size(1),
+          (int32_t)k.size(2), (int32_t)n, dev_as<const int32_t>(a[2], at::kInt), t.size(1),
+          dev_as<const int32_t>(a[3], at::kInt, n), dev_as<const int32_t>(a[4], at::kInt, n + 1)};
+}
+
+// q, k, q_out, k_out, pos, cos, sin, q_weight, k_weight, eps, interleaved, dev_status, stream
+int qk_norm_rope(PyObject* const* a) {
+  const HeadRows q(a[0]), k(a[1], q), qo(a[2], q), ko(a[3], q);
+  const stride_norm_rope how = norm_rope(a + 4, a[7], a[8], a[9], a[10], q);
+  const int32_t dt = row_dtype(q.type);
+  auto* status = dev_or_null_as<int32_t>(a[11], at::kInt, 1);
+  void* st = stream(a[12]);
+  return unlocked(
+      [&] { return g_entry.qk_norm_rope(&q.r, &k.r, &qo.r, &ko.r, dt, q.N, (int32_t)q.D, &how, status, st); });
+}
+
+// dq_out, dk_out, q, k, dq, dk, pos, cos, sin, q_weight, k_weight, eps, interleaved, dq_weight, dk_weight, workspace,
+// dev_status, stream
+int qk_norm_rope_backward(PyObject* const* a) {
+  const HeadRows q(a[2]), go(a[0], q), ho(a[1], q), k(a[3], q), g(a[4], q), h(a[5], q);
+  const stride_norm_rope how = norm_rope(a + 6, a[9], a[10], a[11], a[12], q);
+  const int32_t dt = row_dtype(q.type);
+  auto* dqw = dev_or_null_as<float>(a[13], at::kFloat, q.D);
+  auto* dkw = dev_or_null_as<float>(a[14], at::kFloat, q.D);
+  const Workspace ws(a[15]);
+  auto* status = dev_or_null_as<int32_t>(a[16], at::kInt, 1);
+  void* st = stream(a[17]);
+  return unlocked([&] {
+    return g_entry.qk_norm_rope_backward(&go.r, &ho.r, &q.r, &k.r, &g.r, &h.r, dt, q.N, (int32_t)q.D, &how, dqw, dkw, status,
+                                         ws.p, ws.bytes, st);
+  });
+}
+
+// k, v, k_cache, v_cache, block_table, ctx_len, tok_off, pos, cos, sin, k_weight, q, q_out, q_weight, eps, interleaved,
+// dev_status, stream
+int kv_append(PyObject* const* a) {
+  const HeadRows k(a[0]), v(a[1], k);
+  const stride_paged_cache cache = paged_cache(a + 2, k);
+  const stride_norm_rope how = norm_rope(a + 7, a[13], a[10], a[14], a[15], k);
+  const bool with_q = a[11] != Py_None;
+  need(with_q == (a[12] != Py_None));
+  stride_head_rows q = {}, qo = {};
+  if (with_q) {
+    q = HeadRows(a[11], k).r;
+    qo = HeadRows(a[12], k).r;
+  }
+  const int32_t dt = row_dtype(k.type);
+  auto* status = dev_or_null_as<int32_t>(a[16], at::kInt, 1);
+  void* st = stream(a[17]);
+  return unlocked(
+      [&] { return g_entry.kv_append(&k.r, &v.r, &q, &qo, dt, k.N, (int32_t)k.D, &how, &cache, status, st); });
+}
+
+// q, k_cache, v_cache, block_table, ctx_len, tok_off, tree_mask, scale, out, lse, workspace, dev_status, stream
+int tree_attention(PyObject* const* a) {
+  const HeadRows q(a[0]), out(a[8], q);
+  const stride_paged_cache cache = paged_cache(a + 1, q);
+  const int32_t dt = row_dtype(q.type);
+  const auto* mask = static_cast<const uint64_t*>(dev_or_null(a[6], at::kLong, q.N));
+  const float scale = real(a[7]);
+  auto* lse = dev_or_null_as<float>(a[9], at::kFloat, q.N * q.r.n_heads);
+  const Workspace ws(a[10]);
+  auto* status = dev_or_null_as<int32_t>(a[11], at::kInt, 1);
+  void* st = stream(a[12]);
+  return unlocked([&] {
+    return g_entry.tree_attention(&q.r, &out.r, lse, dt, q.N, (int32_t)q.D, scale, mask, &cache, status, ws.p, ws.bytes, st);
+  });
+}
+
+// logits, noise, tokens, temperature, top_k, top_p, min_p, logp, dev_status, V, stream
+int sample(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0]);
+  need(x.dim() == 2 && (x.size(1) <= 1 || x.stride(1) == 1) && x.size(0) <= INT32_MAX);
+  const int64_t rows = x.size(0), V = a[9] == Py_None ? x.size(1) : integer(a[9]);
+  const int64_t ld = rows <= 1 && x.stride(0) < x.size(1) ? x.size(1) : x.stride(0);
+  const int32_t dt = row_dtype(x.scalar_type());
+  const float* noise = nullptr;
+  int64_t ld_noise = 0;
+  if (a[1] != Py_None) {
+    const at::Tensor& e = tensor(a[1]);
+    need(e.scalar_type() == at::kFloat && e.dim() == 2 && e.size(0) >= rows && e.size(1) >= V && (e.size(1) <= 1 || e.stride(1) == 1));
+    noise = static_cast<const float*>(e.data_ptr());
+    ld_noise = rows <= 1 && e.stride(0) < e.size(1) ? e.size(1) : e.stride(0);
+  }
+  stride_sample_params p = {};
+  const auto each = [&](PyObject* o, const float*& array, float& all) {
+    if (THPVariable_CheckExact(o))
+      array = dev_as<const float>(o, at::kFloat, rows);
+    else
+      all = real(o);
+  };
+  each(a[3], p.temperature, p.temperature_all);
+  if (THPVariable_CheckExact(a[4]))
+    p.top_k = dev_as<const int32_t>(a[4], at::kInt, rows);
+  else
+    p.top_k_all = integer32(a[4]);
+  each(a[5], p.top_p, p.top_p_all);
+  each(a[6], p.min_p, p.min_p_all);
+  auto* tokens = dev_as<int32_t>(a[2], at::kInt, rows);
+  auto* logp = dev_or_null_as<float>(a[7], at::kFloat, rows);
+  auto* status = dev_or_null_as<int32_t>(a[8], at::kInt, 1);
+  void* st = stream(a[10]);
+  const void* const xp = x.data_ptr();
+  return unlocked(
+      [&] { return g_entry.sample(xp, dt, ld, V, (int32_t)rows, noise, ld_noise, &p, tokens, logp, status, st); });
+}
+
 // The addresses of the library's functions, from the handle that the Python
 // module opened (in the order of Entry's members).
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -482,6 +649,11 @@ PyMethodDef g_methods[] = {
     STRIDE_METHOD(partial_lse, 8),
     STRIDE_METHOD(combine_partials, 7),
     STRIDE_METHOD(scan_logprobs, 16),
+    STRIDE_METHOD(qk_norm_rope, 13),
+    STRIDE_METHOD(qk_norm_rope_backward, 18),
+    STRIDE_METHOD(kv_append, 18),
+    STRIDE_METHOD(tree_attention, 13),
+    STRIDE_METHOD(sample, 11),
     {nullptr, nullptr, 0, nullptr},
 };
 

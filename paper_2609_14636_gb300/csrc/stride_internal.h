@@ -120,6 +120,9 @@ struct TeacherTable {
 cudaError_t launch_teacher_rows(const BatchParams& p, const TeacherTable& tt, const uint8_t* traj_domain,
                                 const int64_t* traj_T_row0, const void** rows_out, cudaStream_t stream);
 
+// STRIDE_OK if the current device is sm_103, else the status that a call returns.
+int check_device();
+
 // Multiprocessor count of the current device, looked up once per device
 // (thread-safe); 0 with the CUDA error in *err if it cannot be queried.
 int current_device_sms(int* dev_out, cudaError_t* err);
