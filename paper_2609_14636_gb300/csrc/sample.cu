@@ -5,27 +5,33 @@
 //   index first) up to top_k, then up to top_p of their mass, then w >= min_p;
 //   token = argmax over the kept of w_i / noise_i (an exponential race).
 //
-// A row is read from memory once, by a thread-block cluster whose CTAs keep
-// their shares of it in shared memory.  Three ways from there:
+// A row belongs to a thread-block cluster of 1 to 8 CTAs, each of which takes a
+// share of it: as many CTAs as run at once.  The row comes from memory once;
+// what is read again comes from L2.  Three ways:
 // - nothing is cut off: the race is run while the row streams in, each thread's
 //   ratios relative to the largest logit it has met;
 // - what is kept lies among the few largest tokens (a top_k of up to some
-//   hundreds; a top_p whose mass they hold): of groups of lanes each one's
-//   largest logit is known from the load, and the R-th largest of those is a
-//   bound that at least R tokens reach and few more do.  The tokens that reach it
-//   go to the cluster's first CTA, which ranks them by (logit, index) and does the
-//   rest on that list, while the other CTAs make room for the next rows;
-// - else the threshold is found without sorting: a histogram over the ordered
-//   bit patterns of the logits in the range that can hold it (counts for top-k,
-//   masses for top-p), summed over the cluster, gives the bin where the running
-//   count or mass crosses its target; that bin is the next range.  Masses are
-//   fixed-point integers (2^-40 of the largest weight), so the atomics' order
-//   changes nothing.  What is kept is all above the threshold and, at it, the
-//   first few by index; one pass over the share races them.
+//   hundreds; a top_p whose mass they hold): the first pass leaves each thread's
+//   largest logit (and the sum of weights, for a top_p of the whole row); of
+//   groups of threads, the R-th largest of their maxima is a bound that at least R
+//   tokens reach and few more do.  The threads that reach it look their tokens
+//   up again, and send those to the cluster's first CTA, which sorts them by
+//   (logit, index) and does the rest on that list, while the other CTAs make room
+//   for the next rows;
+// - else the last kept token is bracketed, for a count by a histogram of the
+//   logits by their distance from the largest, for a mass by the masses above a
+//   few pivots, three times (sums in registers: an atomic sum per token of the tail
+//   took 25 us a row where this takes 5); the tokens of the bracket are sorted as
+//   above, and the last kept one is found among them.  Where they are too many for
+//   that (ties), the threshold is found by histograms over the ordered bit
+//   patterns, each level the next one's range, and the ties kept at it by
+//   counting.  One more pass races what is kept.
+//   All sums that atomics make are integers: their order changes nothing.
 // Noise is read for kept tokens alone.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <float.h>
 #include <math.h>
 
 #include "decode_internal.h"
@@ -39,9 +45,12 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 1024;
-constexpr int kLoads = 5;      // vectors that a thread has in flight while it loads its share
-constexpr int kGroups = 1024;  // groups of lanes at most
-constexpr int kList = 1024;    // tokens that the first CTA ranks at most
+constexpr int kLoads = 6;      // vectors that a thread has in flight
+constexpr int kDepth = 6;
+constexpr int kGroups = 1024;  // groups of threads at most
+constexpr int kList = 1024;    // tokens that the first CTA sorts at most
+constexpr float kOne = 1099511627776.f;  // 2^40, the fixed-point 1 of masses
+constexpr int kPivots = 7;
 constexpr int kUsual = 96;     // groups that a top_p without top_k asks to reach the bound
 constexpr int kMaxCluster = 8;
 
@@ -100,49 +109,64 @@ __device__ __forceinline__ void take(Best& a, float v, int32_t i) {
   if (v > a.v || (v == a.v && i < a.i)) a = {v, i};
 }
 
+struct Pick {  // the last kept token, by falling key and rising index
+  uint32_t key;
+  int32_t i;
+};
+
+struct Found {  // where a search's target falls: a bin, its count, the count and the mass above it
+  uint32_t bin, cnt, above, pad;
+  uint64_t mass_above;
+};
+
 struct Shared {
   union {
     struct {
       uint32_t cnt[kBins], lo[kBins], hi[kBins];
     };
-    struct {
-      float group[kGroups];  // the largest logits of the cluster's groups
-      uint64_t list[kList];  // (key, ~index) of the tokens that reach the bound; the first CTA's, ranked
-    };
+    uint64_t list[kList];  // (key, ~index) of the tokens that reach the bound; the first CTA's, sorted
   };
   // exchanged with the cluster
   float own_group[kThreads];
   uint64_t pushed[kList];  // the first CTA's: the tokens, in one segment per CTA
-  Best top[kWarps];        // of the warps
-  int32_t bad;
+  float top;
   uint32_t listed[kMaxCluster];
   float sum_all[kMaxCluster], sum_listed[kMaxCluster];
-  float sum;
-  uint32_t total_cnt;
-  uint64_t total_mass;
-  uint32_t found_bin, found_cnt, found_at;  // the crossing bin, its count, the count above it
-  uint64_t found_mass;                      // the mass above it
+  int32_t lowest[kMaxCluster];
+  uint32_t total_cnt[kMaxCluster];  // of the CTAs' slices of a histogram
+  uint64_t total_mass[kMaxCluster];
+  Found found;
   Best race[kMaxCluster];                   // the first CTA's
-  float kept[kMaxCluster], largest[kMaxCluster];
+  float kept[kMaxCluster];
   // of the CTA
   Best wb[kWarps];
   float wf[kWarps];
   uint32_t wc[kWarps];
   uint64_t wm[kWarps];
   int32_t cutoff;
-  uint32_t count;
-  float bound;
+  uint32_t count, bound;
+  Pick pick;
+  float pivot[kMaxCluster][kPivots], part[kWarps][kPivots];
 };
 
-// A CTA's share of a row: whole 16-byte vectors (of the row's frame, which
-// starts at the vector that holds its first logit), the first `cap` of them in
-// shared memory.
+// The CTA's.  (A function called out of line that had it as an argument would
+// make its atomics generic ones, an order of magnitude slower.)
+__device__ __forceinline__ Shared& shared() {
+  __shared__ Shared s;
+  return s;
+}
+
+// Whether a token of a row comes no later than the last kept one.
+__device__ __forceinline__ bool kept_by(const Pick& last, uint32_t key, int32_t i) { return key > last.key || (key == last.key && i <= last.i); }
+
+
+// A CTA's share of a row: whole 16-byte vectors of the row's frame, which starts
+// at the vector that holds its first logit.
 template <typename T>
 struct Share {
   const T* row;
-  Vec<T>* held;
   int32_t shift;  // elements of the frame's first vector before the row
-  int32_t V, first, end, cap;
+  int32_t V, first, end;
 
   __device__ __forceinline__ int32_t index(int32_t v) const { return v * Vec<T>::N - shift; }
   __device__ __forceinline__ Vec<T> load(int32_t v) const {
@@ -156,8 +180,124 @@ struct Share {
     }
     return x;
   }
-  __device__ __forceinline__ Vec<T> get(int32_t v) const { return v - first < cap ? held[v - first] : load(v); }
+  // f(v, x) for this thread's vectors, U of them in flight.
+  template <int U, typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    for (int32_t v0 = first + threadIdx.x; v0 < end; v0 += U * kThreads) {
+      Vec<T> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * kThreads < end) x[u] = load(v0 + u * kThreads);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * kThreads < end) f(v0 + u * kThreads, x[u]);
+    }
+  }
+  // The same with kDepth of them on their way through shared memory: one copy of
+  // f's code, for passes that do more than a few operations a token.
+  template <typename F>
+  __device__ __forceinline__ void stream(F&& f) const {
+    extern __shared__ uint4 ring[];  // [kDepth][kThreads], each thread its own
+    uint4* slot = ring + threadIdx.x;
+    int32_t ahead = first + threadIdx.x;
+    const auto ask = [&](int k) {
+      if (ahead < end) {
+        const int32_t i = index(ahead);
+        if (i >= 0 && i + Vec<T>::N <= V) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slot + k * kThreads)), "l"(row + i)
+                       : "memory");
+        } else {
+          const Vec<T> x = load(ahead);
+          slot[k * kThreads] = *reinterpret_cast<const uint4*>(&x);
+        }
+        ahead += kThreads;
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 1
+    for (int k = 0; k < kDepth; ++k) ask(k);
+    int k = 0;
+#pragma unroll 1
+    for (int32_t v = first + threadIdx.x; v < end; v += kThreads) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+      const uint4 u = slot[k * kThreads];
+      f(v, *reinterpret_cast<const Vec<T>*>(&u));
+      ask(k);
+      k = k + 1 == kDepth ? 0 : k + 1;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  }
+  // f(v, x) for the vectors of the warp's threads that want them: the warp takes
+  // a few such threads' vectors together, one per lane, so that it waits for
+  // memory once.
+  template <typename F>
+  __device__ __forceinline__ void each_of(bool wanted, F&& f) const {
+    unsigned who = __ballot_sync(0xffffffffu, wanted);
+    if (__popc(who) > 8) {
+      if (wanted) stream(f);
+      return;
+    }
+    const int lane = threadIdx.x & 31;
+    const int32_t base = first + (int32_t)(threadIdx.x - lane), stride = 32 * kThreads;
+    // the next vector is on its way while one is looked at
+    int32_t v = 0, next = 0;
+    Vec<T> x, xn;
+    bool have = false;
+    for (; who; who &= who - 1)
+      for (int32_t v0 = base + __ffs(who) - 1; v0 < end; v0 += stride) {
+        next = v0 + lane * kThreads;
+        if (next < end) xn = load(next);
+        if (have && v < end) f(v, x);
+        v = next;
+        x = xn;
+        have = true;
+      }
+    if (have && v < end) f(v, x);
+  }
 };
+
+// The larger, or NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float c;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+  return c;
+}
+__device__ __forceinline__ float vec_max(const Vec<float>& x) { return max_nan(max_nan(x.e[0], x.e[1]), max_nan(x.e[2], x.e[3])); }
+template <typename P>
+__device__ __forceinline__ float pair_max(const uint4& u, P) {
+  const P* h = reinterpret_cast<const P*>(&u);
+  const P m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  return max_nan(widen(m.x), widen(m.y));
+}
+__device__ __forceinline__ float vec_max(const Vec<__nv_bfloat16>& x) { return pair_max(*reinterpret_cast<const uint4*>(&x), __nv_bfloat162()); }
+__device__ __forceinline__ float vec_max(const Vec<__half>& x) { return pair_max(*reinterpret_cast<const uint4*>(&x), __half2()); }
+
+// Element e of a vector (e not known when compiled).
+__device__ __forceinline__ float pick(const Vec<float>& x, int e) {
+  const float a = e & 1 ? x.e[1] : x.e[0], b = e & 1 ? x.e[3] : x.e[2];
+  return e & 2 ? b : a;
+}
+template <typename T>
+__device__ __forceinline__ T pick(const Vec<T>& x, int e) {
+  const uint4 u = *reinterpret_cast<const uint4*>(&x);
+  const uint32_t a = e & 2 ? u.y : u.x, b = e & 2 ? u.w : u.z, w = e & 4 ? b : a;
+  const uint16_t h = (uint16_t)(e & 1 ? w >> 16 : w & 0xffffu);
+  return *reinterpret_cast<const T*>(&h);
+}
+
+// does(x, e) for a vector's elements that are(x, e): what few elements need is
+// written, and stands in the instruction cache, once.
+template <typename T, typename P, typename F>
+__device__ __forceinline__ void visit(const Vec<T>& x, P&& are, F&& does) {
+  unsigned in = 0;
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e)
+    if (are(x.e[e], e)) in |= 1u << e;
+  for (; in; in &= in - 1) {
+    const int e = __ffs(in) - 1;
+    does(pick(x, e), e);
+  }
+}
 
 struct Weight {
   float m, T;
@@ -165,7 +305,8 @@ struct Weight {
   __device__ __forceinline__ float operator()(float x) const { return expf(log(x)); }
 };
 
-__device__ __forceinline__ float block_sum(float x, Shared& s) {
+__device__ __forceinline__ float block_sum(float x) {
+  Shared& s = shared();
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   if ((threadIdx.x & 31) == 0) s.wf[threadIdx.x >> 5] = x;
@@ -176,7 +317,8 @@ __device__ __forceinline__ float block_sum(float x, Shared& s) {
   return t;
 }
 
-__device__ __forceinline__ Best block_best(Best b, Shared& s) {
+__device__ __forceinline__ Best block_best(Best b) {
+  Shared& s = shared();
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const float v = __shfl_xor_sync(0xffffffffu, b.v, o);
@@ -192,7 +334,8 @@ __device__ __forceinline__ Best block_best(Best b, Shared& s) {
 }
 
 // Exclusive prefix over the block of (c, m) in thread order; the totals in *tc, *tm.
-__device__ __forceinline__ void block_scan(uint32_t& c, uint64_t& m, uint32_t* tc, uint64_t* tm, Shared& s) {
+__device__ __forceinline__ void block_scan(uint32_t& c, uint64_t& m, uint32_t* tc, uint64_t* tm) {
+  Shared& s = shared();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t c0 = c;
   const uint64_t m0 = m;
@@ -227,6 +370,88 @@ __device__ __forceinline__ void block_scan(uint32_t& c, uint64_t& m, uint32_t* t
   __syncthreads();
 }
 
+// A remote CTA's copy of a member of Shared.
+template <typename M>
+__device__ __forceinline__ M* at_rank(M* p, int rank, cg::cluster_group& cluster) {
+  return cluster.map_shared_rank(p, rank);
+}
+
+// The bin of the cluster's summed histograms at which the running count or mass,
+// from `above` and `mass_above` on, first reaches the target (lowered to the
+// total where that is less).  mass_of(bin, count, sum of lo and hi): a bin's mass.
+template <typename F>
+__device__ __forceinline__ Found crossing(uint32_t above, uint64_t mass_above, bool by_mass, bool masses, uint64_t& target, cg::cluster_group& cluster, F&& mass_of) {
+  Shared& s = shared();
+  constexpr int kPer = (kBins + kThreads - 1) / kThreads;
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  cluster.sync();
+  // this CTA's slice of the bins, a run of them per thread
+  const int slice = kBins / C, per = (slice + kThreads - 1) / kThreads, b0 = rank * slice + threadIdx.x * per;
+  const bool mine = (int)threadIdx.x * per < slice;
+  uint32_t c[kPer], tc = 0;
+  uint64_t m[kPer], tm = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    c[j] = 0;
+    m[j] = 0;
+    if (mine && j < per) {  // (the CTAs' parts asked for together)
+      uint32_t pc[kMaxCluster], pl[kMaxCluster], ph[kMaxCluster];
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        const Shared* o = cluster.map_shared_rank(&s, r < C ? r : 0);
+        pc[r] = r < C ? o->cnt[b0 + j] : 0u;
+        pl[r] = masses && r < C ? o->lo[b0 + j] : 0u;
+        ph[r] = masses && r < C ? o->hi[b0 + j] : 0u;
+      }
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        c[j] += pc[r];
+        m[j] += ((uint64_t)ph[r] << 32) + pl[r];
+      }
+      m[j] = masses && c[j] ? mass_of((uint32_t)(b0 + j), c[j], m[j]) : 0;
+    }
+    tc += c[j];
+    tm += m[j];
+  }
+  uint32_t ec = tc, all_c;
+  uint64_t em = tm, all_m;
+  block_scan(ec, em, &all_c, &all_m);
+  if (threadIdx.x < C) {
+    *at_rank(&s.total_cnt[rank], threadIdx.x, cluster) = all_c;
+    *at_rank(&s.total_mass[rank], threadIdx.x, cluster) = all_m;
+  }
+  cluster.sync();
+  uint64_t sum = by_mass ? mass_above : above, range = sum;
+  for (int r = 0; r < C; ++r) range += by_mass ? s.total_mass[r] : s.total_cnt[r];
+  if (target > range) target = range;
+  int owner = 0;
+  uint32_t base_c = above;
+  uint64_t base_m = mass_above;
+  for (; owner < C - 1; ++owner) {
+    const uint64_t next = sum + (by_mass ? s.total_mass[owner] : s.total_cnt[owner]);
+    if (next >= target) break;
+    sum = next;
+    base_c += s.total_cnt[owner];
+    base_m += s.total_mass[owner];
+  }
+  if (rank == owner) {
+    ec += base_c;
+    em += base_m;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const uint64_t before = by_mass ? em : ec, after = before + (by_mass ? m[j] : c[j]);
+      if (before < target && after >= target) {
+        const Found f = {(uint32_t)(b0 + j), c[j], ec, 0, em};
+        for (int r = 0; r < C; ++r) *at_rank(&s.found, r, cluster) = f;
+      }
+      ec += c[j];
+      em += m[j];
+    }
+  }
+  cluster.sync();
+  return s.found;
+}
+
 // Where a search ended: a key, the range's tokens that have it, and the count
 // and mass of those above it.
 struct Cut {
@@ -236,11 +461,12 @@ struct Cut {
 
 // The key in [lo, hi] at which the count (by_mass false) or the mass of the
 // tokens from the largest down first reaches the target (at most the range's
-// total: a larger target is lowered to it).
+// total: a larger target is lowered to it), of tokens up to `last` alone.  own:
+// the key of this thread's largest logit.
 template <typename T>
-__device__ Cut search(const Share<T>& sh, const Weight& weight, uint32_t lo, uint32_t hi, bool by_mass, uint64_t target, bool masses,
-                      Shared& s, cg::cluster_group& cluster) {
-  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+__device__ Cut search(const Share<T>& sh, const Weight& weight, const Pick& last, uint32_t own, uint32_t lo, uint32_t hi, bool by_mass, uint64_t target, bool masses,
+                      cg::cluster_group& cluster) {
+  Shared& s = shared();
   uint32_t above = 0;
   uint64_t mass_above = 0;
   while (true) {
@@ -248,90 +474,28 @@ __device__ Cut search(const Share<T>& sh, const Weight& weight, uint32_t lo, uin
     while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
     for (int b = threadIdx.x; b < kBins; b += kThreads) s.cnt[b] = s.lo[b] = s.hi[b] = 0;
     __syncthreads();
-    for (int32_t v = sh.first + threadIdx.x; v < sh.end; v += kThreads) {
-      const Vec<T> x = sh.get(v);
-#pragma unroll
-      for (int e = 0; e < Vec<T>::N; ++e) {
-        const uint32_t k = Key<T>::of(x.e[e]);
-        if (k < lo || k > hi) continue;
-        const uint32_t b = (hi - k) >> shift;
-        atomicAdd(&s.cnt[b], 1u);
-        if (masses) {
-          const float w = weight(widen(x.e[e])) * 256.f, whole = floorf(w);
-          const uint32_t q = __float2uint_rz((w - whole) * 4294967296.f);
-          const uint32_t old = atomicAdd(&s.lo[b], q);
-          const uint32_t up = (uint32_t)whole + (old + q < old ? 1u : 0u);
-          if (up) atomicAdd(&s.hi[b], up);
-        }
-      }
-    }
-    cluster.sync();
-    // the cluster's sums of this CTA's slice of the bins, a run of them per thread
-    const int slice = kBins / C, per = (slice + kThreads - 1) / kThreads, b0 = rank * slice + threadIdx.x * per;
-    const bool mine = (int)threadIdx.x * per < slice;
-    uint32_t c[(kBins + kThreads - 1) / kThreads];
-    uint64_t m[(kBins + kThreads - 1) / kThreads];
-    uint32_t tc = 0;
-    uint64_t tm = 0;
-    for (int j = 0; j < per; ++j) {
-      c[j] = 0;
-      m[j] = 0;
-      if (mine)
-        for (int r = 0; r < C; ++r) {
-          const Shared* o = cluster.map_shared_rank(&s, r);
-          c[j] += o->cnt[b0 + j];
-          if (masses) m[j] += ((uint64_t)o->hi[b0 + j] << 32) + o->lo[b0 + j];
-        }
-      tc += c[j];
-      tm += m[j];
-    }
-    uint32_t ec = tc, all_c;
-    uint64_t em = tm, all_m;
-    block_scan(ec, em, &all_c, &all_m, s);
-    if (threadIdx.x == 0) {
-      s.total_cnt = all_c;
-      s.total_mass = all_m;
-    }
-    cluster.sync();
-    uint64_t sum = by_mass ? mass_above : above, range = sum;
-    for (int r = 0; r < C; ++r) {
-      const Shared* o = cluster.map_shared_rank(&s, r);
-      range += by_mass ? o->total_mass : o->total_cnt;
-    }
-    if (target > range) target = range;
-    int owner = 0;
-    uint32_t base_c = above;
-    uint64_t base_m = mass_above;
-    for (; owner < C - 1; ++owner) {
-      const Shared* o = cluster.map_shared_rank(&s, owner);
-      const uint64_t next = sum + (by_mass ? o->total_mass : o->total_cnt);
-      if (next >= target) break;
-      sum = next;
-      base_c += o->total_cnt;
-      base_m += o->total_mass;
-    }
-    if (rank == owner) {
-      ec += base_c;
-      em += base_m;
-      for (int j = 0; j < per && mine; ++j) {
-        const uint64_t before = by_mass ? em : ec, after = before + (by_mass ? m[j] : c[j]);
-        if (before < target && after >= target) {
-          s.found_bin = b0 + j;
-          s.found_cnt = c[j];
-          s.found_at = ec;
-          s.found_mass = em;
-        }
-        ec += c[j];
-        em += m[j];
-      }
-    }
-    cluster.sync();
-    const Shared* o = cluster.map_shared_rank(&s, owner);
-    const uint32_t bin = o->found_bin;
-    above = o->found_at;
-    mass_above = o->found_mass;
-    hi -= bin << shift;
-    if (shift == 0) return {hi, o->found_cnt, above, mass_above};
+    sh.each_of(own >= lo, [&](int32_t v, const Vec<T>& x) {
+      visit(
+          x, [&](T y, int e) { const uint32_t k = Key<T>::of(y); return k >= lo && k <= hi && kept_by(last, k, sh.index(v) + e); },
+          [&](T y, int) {
+            const uint32_t b = (hi - Key<T>::of(y)) >> shift;
+            atomicAdd(&s.cnt[b], 1u);
+            if (masses && shift > 0) {  // (in a bin of one key all weigh the same)
+              const float w = weight(widen(y)) * 256.f, whole = floorf(w);
+              const uint32_t q = __float2uint_rz((w - whole) * 4294967296.f);
+              const uint32_t old = atomicAdd(&s.lo[b], q);
+              const uint32_t up = (uint32_t)whole + (old + q < old ? 1u : 0u);
+              if (up) atomicAdd(&s.hi[b], up);
+            }
+          });
+    });
+    const Found f = crossing(above, mass_above, by_mass, masses, target, cluster, [&](uint32_t b, uint32_t c, uint64_t q) {
+      return shift > 0 ? q : c * (uint64_t)(weight(Key<T>::value(hi - b)) * kOne);
+    });
+    above = f.above;
+    mass_above = f.mass_above;
+    hi -= f.bin << shift;
+    if (shift == 0) return {hi, f.cnt, above, mass_above};
     const uint32_t width = (1u << shift) - 1;
     if (hi - lo > width) lo = hi - width;
   }
@@ -340,7 +504,8 @@ __device__ Cut search(const Share<T>& sh, const Weight& weight, uint32_t lo, uin
 // The index below which this share's tokens with the given key are kept, if the
 // row's first `keep` of them (in order of index) are.
 template <typename T>
-__device__ int32_t tie_cutoff(const Share<T>& sh, uint32_t key, uint32_t keep, Shared& s, cg::cluster_group& cluster) {
+__device__ int32_t tie_cutoff(const Share<T>& sh, uint32_t own_key, uint32_t key, uint32_t keep, cg::cluster_group& cluster) {
+  Shared& s = shared();
   const auto tied = [&](const Vec<T>& x) {
     uint32_t n = 0;
 #pragma unroll
@@ -349,43 +514,43 @@ __device__ int32_t tie_cutoff(const Share<T>& sh, uint32_t key, uint32_t keep, S
   };
   uint32_t n = 0, own;
   uint64_t z = 0, zt;
-  for (int32_t v = sh.first + threadIdx.x; v < sh.end; v += kThreads) n += tied(sh.get(v));
-  block_scan(n, z, &own, &zt, s);
-  if (threadIdx.x == 0) s.total_cnt = own;
+  sh.each_of(own_key >= key, [&](int32_t, const Vec<T>& x) { n += tied(x); });
+  block_scan(n, z, &own, &zt);
+  const int rank = (int)cluster.block_rank();
+  if (threadIdx.x < cluster.num_blocks()) *at_rank(&s.total_cnt[rank], threadIdx.x, cluster) = own;
   cluster.sync();
   uint32_t before = 0;
-  for (int o = 0; o < (int)cluster.block_rank(); ++o) before += cluster.map_shared_rank(&s, o)->total_cnt;
+  for (int o = 0; o < rank; ++o) before += s.total_cnt[o];
   if (before >= keep) return -1;
   const uint32_t want = keep - before;
   if (own <= want) return INT32_MAX;
   uint32_t seen = 0;  // the want-th of this share is the last kept: a round covers consecutive vectors
-  for (int32_t v0 = sh.first; seen < want; v0 += kThreads) {
-    const int32_t v = v0 + threadIdx.x;
-    Vec<T> x;
-    uint32_t c = 0, all;
-    if (v < sh.end) {
-      x = sh.get(v);
-      c = tied(x);
-    }
-    uint32_t at = c;
-    z = 0;
-    block_scan(at, z, &all, &zt, s);
-    if (c && seen + at < want && seen + at + c >= want) {
-      uint32_t left = want - seen - at;
+  for (int32_t v0 = sh.first; seen < want; v0 += kLoads * kThreads) {
+    uint32_t c[kLoads];
 #pragma unroll
-      for (int e = 0; e < Vec<T>::N; ++e)
-        if (Key<T>::of(x.e[e]) == key && --left == 0) s.cutoff = sh.index(v) + e + 1;
+    for (int u = 0; u < kLoads; ++u) {
+      const int32_t v = v0 + u * kThreads + threadIdx.x;
+      c[u] = v < sh.end && own_key >= key ? tied(sh.load(v)) : 0u;
     }
-    seen += all;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      if (seen >= want) continue;
+      uint32_t at = c[u], all;
+      z = 0;
+      block_scan(at, z, &all, &zt);
+      if (c[u] && seen + at < want && seen + at + c[u] >= want) {
+        const int32_t v = v0 + u * kThreads + threadIdx.x;
+        const Vec<T> x = sh.load(v);
+        uint32_t left = want - seen - at;
+#pragma unroll
+        for (int e = 0; e < Vec<T>::N; ++e)
+          if (Key<T>::of(x.e[e]) == key && --left == 0) s.cutoff = sh.index(v) + e + 1;
+      }
+      seen += all;
+    }
   }
   __syncthreads();
   return s.cutoff;
-}
-
-// A remote CTA's copy of a member of Shared.
-template <typename M>
-__device__ __forceinline__ M* at_rank(M* p, int rank, cg::cluster_group& cluster) {
-  return cluster.map_shared_rank(p, rank);
 }
 
 // The noise of a vector's tokens (1 where there is no token).
@@ -406,112 +571,448 @@ __device__ __forceinline__ void load_noise(float (&e)[N], const float* noise, in
   }
 }
 
+// A thread's largest logit, and the sum of exp((x - m) / T) over its tokens.
+struct Running {
+  float m = -INFINITY, z = 0.f, off = 0.f;  // off = m * scale
+};
+
+// Takes a vector into it: w[] = exp((x - m) / T) of its tokens relative to the
+// new m; the factor by which what was relative to the old one shrinks.
+template <typename T>
+__device__ __forceinline__ float run_on(Running& a, const Vec<T>& x, float (&w)[Vec<T>::N], float scale) {
+  const float mx = max_nan(a.m, vec_max(x));
+  float by = 1.f;
+  if (!(mx == a.m)) {  // (also once, and from then on, where there is a NaN)
+    by = a.m == -INFINITY ? 0.f : ex2((a.m - mx) * scale);
+    a.m = mx;
+    a.z *= by;
+    a.off = mx * scale;
+  }
+  if (fabsf(a.off) < 64.f) {  // (one rounding of at most 2^-19 of the exponent's unit, the same for all the thread's tokens)
+#pragma unroll
+    for (int k = 0; k < Vec<T>::N; ++k) w[k] = ex2(fmaf(widen(x.e[k]), scale, -a.off));
+  } else {  // (no token yet, or logits of a size that would lose more)
+#pragma unroll
+    for (int k = 0; k < Vec<T>::N; ++k) w[k] = a.m == -INFINITY ? 0.f : ex2((widen(x.e[k]) - a.m) * scale);
+  }
+#pragma unroll
+  for (int k = 0; k < Vec<T>::N; ++k) a.z += w[k];
+  return by;
+}
+
+// The largest of the cluster's threads' values, NaN if one is.
+__device__ __forceinline__ float cluster_top(float top, cg::cluster_group& cluster) {
+  Shared& s = shared();
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) s.wf[threadIdx.x >> 5] = top;
+  __syncthreads();
+  top = s.wf[lane % kWarps];
+#pragma unroll
+  for (int o = kWarps / 2; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (threadIdx.x == 0) s.top = top;
+  cluster.sync();
+  top = *at_rank(&s.top, lane % (int)cluster.num_blocks(), cluster);
+#pragma unroll
+  for (int o = kMaxCluster / 2; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  return top;
+}
+
+__device__ __forceinline__ void answer(const SampleParams& p, int32_t r, int32_t token, float logp) {
+  p.tokens[r] = token;
+  if (p.logp) p.logp[r] = logp;
+  if (token < 0) set_status(p.dev_status, STRIDE_DEV_NO_TOKEN);
+}
+
+// The CTAs' winners race each other; the first CTA answers.
+template <typename T>
+__device__ __forceinline__ void finish(const SampleParams& p, const Share<T>& sh, int32_t r, const Weight& weight, bool sound, Best best,
+                                       float kept, cg::cluster_group& cluster) {
+  Shared& s = shared();
+  const int rank = (int)cluster.block_rank();
+  if (threadIdx.x == 0) {
+    *at_rank(&s.race[rank], 0, cluster) = best;
+    *at_rank(&s.kept[rank], 0, cluster) = kept;
+  }
+  cluster.sync();
+  if (rank != 0 || threadIdx.x != 0) return;
+  kept = 0.f;
+  for (int o = 0; o < (int)cluster.num_blocks(); ++o) {
+    take(best, s.race[o].v, s.race[o].i);
+    kept += s.kept[o];
+  }
+  if (sound && best.v > 0.f)
+    answer(p, r, best.i, weight.log(widen(sh.row[best.i])) - logf(kept));
+  else
+    answer(p, r, -1, NAN);
+}
+
+// The threads' best ratios (no token: INT32_MAX), of approximate exponentials and
+// quotients (2^-22, and the rounding of an exponent of up to 64), race again with
+// exact ones where they come within 1e-5 of the CTA's largest; kept: the threads'
+// sums of weights.
+template <typename T>
+__device__ __forceinline__ void exact_race(const SampleParams& p, const Share<T>& sh, const float* noise, int32_t r, const Weight& weight,
+                                           bool sound, Best best, float kept, cg::cluster_group& cluster) {
+  if (best.i == INT32_MAX) best.v = -1.f;
+  const Best lead = block_best(best);
+  kept = block_sum(kept);
+  Best exact = {-1.f, INT32_MAX};
+  if (sound && best.i != INT32_MAX && best.v >= lead.v * 0.99999f)
+    exact = {best.v < INFINITY ? weight(widen(sh.row[best.i])) / __ldg(noise + best.i) : INFINITY, best.i};
+  exact = block_best(exact);
+  finish(p, sh, r, weight, sound, exact, kept, cluster);
+}
+
 // Nothing is cut off: one pass over logits and noise together.  A thread keeps
 // its largest logit m, sum exp((x - m) / T) and its best ratio exp((x - m) / T) /
-// noise, rescaled where m grows.  Exponentials and quotients on the way are the
-// approximate ones (2^-22); the threads' best that come within 1e-5 of the largest
-// then race again with exact ones.
+// noise, rescaled where m grows.
 template <typename T>
-__device__ void race_all(const SampleParams& p, const Share<T>& sh, const float* noise, float temp, int32_t r, Shared& s,
-                         cg::cluster_group& cluster) {
+__device__ __noinline__ void race_all(const SampleParams& p, const Share<T>& sh, const float* noise, float temp, int32_t r, cg::cluster_group& cluster) {
+  Shared& s = shared();
   constexpr int N = Vec<T>::N, U = N == 8 ? 2 : 4;
-  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const float scale = kLog2e / temp;
   const bool whole = (reinterpret_cast<uintptr_t>(noise + sh.index(0)) & 15) == 0;
-  Best best = {-1.f, INT32_MAX};
-  float m = -INFINITY, z = 0.f;
-  bool bad = false;
-  for (int32_t v0 = sh.first; v0 < sh.end; v0 += U * kThreads) {
+  Best best = {0.f, INT32_MAX};
+  Running a;
+  for (int32_t v0 = sh.first + tid; v0 < sh.end; v0 += U * kThreads) {
     Vec<T> x[U];
     float e[U][N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int32_t v = v0 + u * kThreads + tid;
-      if (v < sh.end) {
-        x[u] = sh.load(v);
-        load_noise<N>(e[u], noise, sh.index(v), sh.V, whole);
+    for (int u = 0; u < U; ++u)
+      if (v0 + u * kThreads < sh.end) {
+        x[u] = sh.load(v0 + u * kThreads);
+        load_noise<N>(e[u], noise, sh.index(v0 + u * kThreads), sh.V, whole);
       }
-    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int32_t v = v0 + u * kThreads + tid;
-      if (v >= sh.end) continue;
-      float f[N], mx = m;
+      if (v0 + u * kThreads >= sh.end) continue;
+      float w[N], mx = 0.f;
+      const float by = run_on(a, x[u], w, scale);
+      if (best.v < INFINITY) best.v *= by;
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        f[k] = widen(x[u].e[k]);
-        bad |= !(f[k] < INFINITY);
-        mx = fmaxf(mx, f[k]);
+        w[k] = __fdividef(w[k], e[u][k]);  // (NaN, from a NaN noise or 0 / 0, wins nothing)
+        mx = fmaxf(mx, w[k]);
       }
-      if (mx > m) {
-        const float by = ex2((m - mx) * scale);
-        z *= by;
-        if (best.v < INFINITY) best.v *= by;  // (a thread without a token has -1 or -0: still no ratio)
-        m = mx;
-      }
-      if (m == -INFINITY) continue;
+      if (mx > best.v) {
+        best.v = mx;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const float w = ex2((f[k] - m) * scale);
-        z += w;
-        const float q = __fdividef(w, e[u][k]);
-        if (q > best.v && w > 0.f) best = {q, sh.index(v) + k};
+        for (int k = N - 1; k >= 0; --k)
+          if (w[k] == mx) best.i = sh.index(v0 + u * kThreads) + k;
       }
     }
   }
-  // the row's largest logit, then everything relative to it
-  float top = m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((tid & 31) == 0) s.wf[tid >> 5] = top;
-  bad = __syncthreads_or(bad);
-  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s.wf[w]);
-  if (tid == 0) {
-    s.sum = top;
-    s.bad = bad;
+  const float top = cluster_top(a.m, cluster);
+  const bool sound = top > -INFINITY && top < INFINITY;
+  const float by = a.m == -INFINITY ? 0.f : ex2((a.m - top) * scale);
+  if (best.v < INFINITY) best.v *= by;
+  exact_race(p, sh, noise, r, Weight{top, temp}, sound, best, a.m == -INFINITY ? 0.f : a.z * by, cluster);
+}
+
+// The first CTA's list from the segments that the cluster's CTAs pushed, sorted.
+__device__ __forceinline__ void sort_list(uint32_t n);
+__device__ __forceinline__ void gather_list(uint32_t n, uint32_t segment) {
+  Shared& s = shared();
+  for (uint32_t j = threadIdx.x; j < n; j += kThreads) {
+    uint32_t o = 0, k = j;
+    while (k >= s.listed[o]) k -= s.listed[o++];
+    s.list[j] = s.pushed[o * segment + k];
   }
+  sort_list(n);
+}
+
+// Sorts s.list[0, n) (distinct values) from the largest down; n <= kList.  Up to
+// 256 values each one's rank is counted, by several threads a value; the passes of
+// a bitonic sort cost less above.
+__device__ __forceinline__ void sort_list(uint32_t n) {
+  Shared& s = shared();
+  __syncthreads();
+  if (n <= 256) {
+    uint32_t P = 32;
+    while (P < n) P *= 2;
+    const uint32_t team = kThreads / P, j = threadIdx.x / team, part = threadIdx.x % team;
+    const uint64_t mine = j < n ? s.list[j] : 0;
+    uint32_t place = 0;
+    for (uint32_t k = part; k < n; k += team) place += s.list[k] > mine;
+    for (uint32_t o = 1; o < team; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+    __syncthreads();
+    if (j < n && part == 0) s.list[place] = mine;
+    __syncthreads();
+    return;
+  }
+  uint32_t P = 512;
+  while (P < n) P *= 2;
+  for (uint32_t j = n + threadIdx.x; j < P; j += kThreads) s.list[j] = 0;
+  __syncthreads();
+  for (uint32_t run = 2; run <= P; run *= 2)
+    for (uint32_t d = run / 2; d > 0; d /= 2) {
+      for (uint32_t q = threadIdx.x; q < P / 2; q += kThreads) {
+        const uint32_t i = 2 * q - (q & (d - 1)), j = i + d;
+        const uint64_t a = s.list[i], b = s.list[j];
+        if ((a < b) == ((i & run) == 0)) {
+          s.list[i] = b;
+          s.list[j] = a;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+// The last kept token, among those up to `last` that in(x) holds for (none of a
+// thread that `any` is false for): the first of them, in order, where base plus the
+// count or mass up to it reaches the target.  False where they are too many to be
+// sorted.
+template <typename T, typename In>
+__device__ __forceinline__ bool pick_among(const Share<T>& sh, const Weight& weight, bool any, In&& in, bool by_mass, uint64_t base,
+                                           uint64_t target, Pick& last, cg::cluster_group& cluster) {
+  Shared& s = shared();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const Pick limit = last;
+  const bool all = limit.i < 0;  // (no limit yet)
+  __syncthreads();
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  sh.each_of(any, [&](int32_t v, const Vec<T>& x) {
+    visit(
+        x, [&](T y, int e) { return in(widen(y)) && (all || kept_by(limit, Key<T>::of(y), sh.index(v) + e)); },
+        [&](T y, int e) {
+          const uint32_t j = atomicAdd(&s.count, 1u);
+          if (j < kList) s.list[j] = (uint64_t)Key<T>::of(y) << 32 | (uint32_t)~(sh.index(v) + e);
+        });
+  });
+  __syncthreads();
+  const uint32_t own_n = s.count, segment = kList / C;
+  for (uint32_t j = threadIdx.x; j < min(own_n, segment); j += kThreads) *at_rank(&s.pushed[rank * segment + j], 0, cluster) = s.list[j];
+  if (threadIdx.x < C) *at_rank(&s.listed[rank], threadIdx.x, cluster) = own_n;
   cluster.sync();
+  uint32_t n = 0;
+  bool fits = true;
   for (int o = 0; o < C; ++o) {
-    top = fmaxf(top, *at_rank(&s.sum, o, cluster));
-    bad |= *at_rank(&s.bad, o, cluster) != 0;
+    fits = fits && s.listed[o] <= segment;
+    n += s.listed[o];
   }
-  const float by = m == -INFINITY ? 0.f : ex2((m - top) * scale);
-  z = block_sum(z * by, s);
-  if (best.i == INT32_MAX)
-    best.v = -1.f;
-  else if (best.v < INFINITY)
-    best.v *= by;
-  const Best lead = block_best(best, s);
-  // (the CTA's near-best race exactly; those of a CTA that is not near the row's best lose either way)
-  const Weight weight = {top, temp};
-  Best exact = {-1.f, INT32_MAX};
-  if (best.i != INT32_MAX && best.v >= lead.v * 0.99999f)
-    exact = {best.v < INFINITY ? weight(widen(sh.row[best.i])) / __ldg(noise + best.i) : INFINITY, best.i};
-  exact = block_best(exact, s);
-  if (tid == 0) {
-    *at_rank(&s.race[rank], 0, cluster) = exact;
-    *at_rank(&s.kept[rank], 0, cluster) = z;
+  if (!fits || n == 0) return false;
+  if (rank == 0) {
+    gather_list(n, segment);
+    constexpr int kPer = kList / kThreads;
+    uint32_t c = 0, tc;
+    uint64_t m = 0, tm, w[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const uint32_t j = threadIdx.x * kPer + u;
+      w[u] = j < n ? (by_mass ? (uint64_t)(weight(Key<T>::value((uint32_t)(s.list[j] >> 32))) * kOne) : 1) : 0;
+      m += w[u];
+    }
+    block_scan(c, m, &tc, &tm);
+    const auto tell = [&](uint32_t j) {
+      const Pick q = {(uint32_t)(s.list[j] >> 32), (int32_t)~(uint32_t)s.list[j]};
+      for (int o = 0; o < C; ++o) *at_rank(&s.pick, o, cluster) = q;
+    };
+    m += base;
+    const bool reached = tm + base >= target;
+    if (!reached && threadIdx.x == 0) tell(n - 1);  // (by the sums' rounding: all of them are kept)
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      if (reached && w[u] && m < target && m + w[u] >= target) tell(threadIdx.x * kPer + u);
+      if (reached && threadIdx.x == 0 && u == 0 && m >= target) tell(0);
+      m += w[u];
+    }
   }
   cluster.sync();
-  if (rank == 0 && tid == 0) {
-    z = 0.f;
-    for (int o = 0; o < C; ++o) {
-      take(exact, s.race[o].v, s.race[o].i);
-      z += s.kept[o];
-    }
-    const bool found = !bad && exact.v > 0.f && exact.i != INT32_MAX;
-    p.tokens[r] = found ? exact.i : -1;
-    if (p.logp) p.logp[r] = found ? weight.log(widen(sh.row[exact.i])) - logf(z) : NAN;
-    if (!found) set_status(p.dev_status, STRIDE_DEV_NO_TOKEN);
+  last = s.pick;
+  return true;
+}
+
+// The `target`-th token: a histogram of 1,024 bins of the 32 units below the
+// largest logit (the last one takes all below), then the tokens of one bin.
+template <typename T>
+__device__ __forceinline__ bool last_by_count(const Share<T>& sh, const Weight& weight, float own, uint64_t target, Pick& last,
+                                              cg::cluster_group& cluster) {
+  Shared& s = shared();
+  // (the order of bins is that of the logits: each operation is monotone)
+  const auto bin_of = [&](float x) { return (uint32_t)fminf((weight.m - x) * (kBins / 32.f), (float)(kBins - 1)); };
+  for (int b = threadIdx.x; b < kBins; b += kThreads) s.cnt[b] = 0;
+  __syncthreads();
+  sh.each_of(own > -INFINITY, [&](int32_t, const Vec<T>& x) {
+    visit(
+        x, [&](T y, int) { return widen(y) > -INFINITY; }, [&](T y, int) { atomicAdd(&s.cnt[bin_of(widen(y))], 1u); });
+  });
+  const Found f = crossing(0, 0, false, false, target, cluster, [](uint32_t, uint32_t, uint64_t) { return uint64_t(0); });
+  if (f.cnt > kList) return false;
+  return pick_among(
+      sh, weight, own > -INFINITY && bin_of(own) <= f.bin, [&](float x) { return x > -INFINITY && bin_of(x) == f.bin; }, false, f.above,
+      target, last, cluster);
+}
+
+// A thread's sums become the cluster's (in a fixed order) in every CTA.
+__device__ __forceinline__ void cluster_sums(float (&sum)[kPivots], cg::cluster_group& cluster) {
+  Shared& s = shared();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int j = 0; j < kPivots; ++j) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+    if (lane == j) s.part[warp][j] = sum[j];
   }
+  __syncthreads();
+  if (threadIdx.x < kPivots * C) {
+    const int j = threadIdx.x % kPivots;
+    float q = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) q += s.part[w][j];
+    *at_rank(&s.pivot[rank][j], threadIdx.x / kPivots, cluster) = q;
+  }
+  cluster.sync();
+#pragma unroll
+  for (int j = 0; j < kPivots; ++j) {
+    sum[j] = 0.f;
+    for (int o = 0; o < C; ++o) sum[j] += s.pivot[o][j];
+  }
+  cluster.sync();  // (they make room for the next)
+}
+
+// The token where the mass of those up to `last` reaches the goal (in 2^-40).
+// Tokens below `low` are not needed for it.  The masses above 7 pivots leave an
+// eighth of the range, and twice those of the tokens in it above 7 more an eighth
+// of that.
+template <typename T>
+__device__ __forceinline__ bool last_by_mass(const Share<T>& sh, const Weight& weight, float own, float low, uint64_t goal, Pick& last,
+                                             cg::cluster_group& cluster) {
+  const float scale = kLog2e / weight.T, want = (float)goal * (1.f / kOne);
+  const Pick limit = last;
+  const bool all = limit.i < 0;  // (no limit yet)
+  float lo = low, hi = INFINITY, above = 0.f;  // mass(x >= hi) = above < goal <= mass(x >= lo)
+  for (int pass = 0; pass < 3; ++pass) {
+    const float step = ((hi < INFINITY ? hi : weight.m) - lo) * (1.f / (kPivots + 1));
+    float t[kPivots], sum[kPivots];
+#pragma unroll
+    for (int j = 0; j < kPivots; ++j) {
+      t[j] = lo + step * (j + 1);
+      sum[j] = 0.f;
+    }
+    const auto add = [&](float f, float w) {
+#pragma unroll
+      for (int j = 0; j < kPivots; ++j) sum[j] += f >= t[j] ? w : 0.f;
+    };
+    if (pass == 0) {
+      sh.each_of(own >= lo, [&](int32_t v, const Vec<T>& x) {
+#pragma unroll
+        for (int e = 0; e < Vec<T>::N; ++e) {
+          const float f = widen(x.e[e]);
+          add(f, all || kept_by(limit, Key<T>::of(x.e[e]), sh.index(v) + e) ? ex2((f - weight.m) * scale) : 0.f);
+        }
+      });
+    } else {
+      sh.each_of(own >= lo, [&](int32_t v, const Vec<T>& x) {
+        visit(
+            x, [&](T y, int e) { return widen(y) >= lo && widen(y) < hi && (all || kept_by(limit, Key<T>::of(y), sh.index(v) + e)); },
+            [&](T y, int) { add(widen(y), ex2((widen(y) - weight.m) * scale)); });
+      });
+    }
+    cluster_sums(sum, cluster);
+    float next_lo = lo, next_hi = hi, next_above = above;
+    bool below = false;
+#pragma unroll
+    for (int j = kPivots - 1; j >= 0; --j) {
+      if (below) continue;
+      if (above + sum[j] >= want) {
+        next_lo = t[j];
+        below = true;
+      } else {
+        next_hi = t[j];
+        next_above = above + sum[j];
+      }
+    }
+    lo = next_lo;
+    hi = next_hi;
+    above = next_above;
+  }
+  return pick_among(
+      sh, weight, own >= lo, [&](float x) { return x >= lo && x < hi; }, true, (uint64_t)(above * kOne), goal, last, cluster);
+}
+
+// What the first passes leave of a row.
+struct Row {
+  float temp, top_p, least, own, z;  // own: the thread's largest logit; z: the row's mass (of a top_p without top_k)
+  int32_t top_k, r;
+  bool cut_k, cut_p;
+};
+
+// The general way: the threshold by histograms, then the race.
+template <typename T>
+__device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& sh, const float* noise, const Weight& weight, const Row& q,
+                                        cg::cluster_group& cluster) {
+  Shared& s = shared();
+  constexpr int N = Vec<T>::N;
+  const uint32_t none = Key<T>::of(lowest<T>()), first = Key<T>::of(static_cast<T>(weight.m)), own_key = Key<T>::of(static_cast<T>(q.own));
+  Pick last = {none, -1};  // (all that are not ruled out)
+  if (q.cut_k) {
+    const uint64_t target = (uint64_t)q.top_k;
+    if (!last_by_count(sh, weight, q.own, target, last, cluster)) {
+      cluster.sync();
+      const Cut cut = search(sh, weight, last, own_key, none + 1, first, false, target, false, cluster);
+      const uint32_t ties = min((uint32_t)target - cut.above, cut.ties);
+      last = {cut.key, ties < cut.ties ? tie_cutoff(sh, own_key, cut.key, ties, cluster) - 1 : INT32_MAX};
+    }
+  }
+  if (q.cut_p) {
+    float z = q.z;
+    if (q.cut_k) {  // the mass of what top_k leaves
+      float t = 0.f;
+      sh.each_of(own_key >= last.key && own_key > none, [&](int32_t v, const Vec<T>& x) {
+        visit(
+            x, [&](T y, int e) { return kept_by(last, Key<T>::of(y), sh.index(v) + e); }, [&](T y, int) { t += weight(widen(y)); });
+      });
+      t = block_sum(t);
+      cluster.sync();
+      if (threadIdx.x < cluster.num_blocks()) *at_rank(&s.sum_all[cluster.block_rank()], threadIdx.x, cluster) = t;
+      cluster.sync();
+      z = 0.f;
+      for (int o = 0; o < (int)cluster.num_blocks(); ++o) z += s.sum_all[o];
+    }
+    const uint64_t goal = (uint64_t)fmax(ceil((double)q.top_p * z * kOne), 1.0);
+    // The tokens of w < (1 - top_p) z / (2 V) hold less than half of what may be left out: none of them is needed.
+    const float low = weight.m + q.temp * logf(fmaxf((1.f - fmaxf(q.top_p, 0.f)) * z / (2.f * (float)p.V), 1e-30f));
+    if (!last_by_mass(sh, weight, q.own, low, goal, last, cluster)) {
+      cluster.sync();
+      const Cut cut = search(sh, weight, last, own_key, none + 1, first, true, goal, true, cluster);
+      const uint64_t one = max((uint64_t)(weight(Key<T>::value(cut.key)) * kOne), uint64_t(1));
+      const uint64_t need = goal > cut.mass_above ? (goal - cut.mass_above + one - 1) / one : 1;
+      const uint32_t ties = (uint32_t)min(need, (uint64_t)cut.ties);
+      const int32_t at = ties < cut.ties ? tie_cutoff(sh, own_key, cut.key, ties, cluster) - 1 : INT32_MAX;
+      if (cut.key > last.key || at < last.i) last = {cut.key, at};
+    }
+  }
+  Best best = {0.f, INT32_MAX};
+  float kept = 0.f;
+  const float scale = kLog2e / q.temp;
+  sh.each_of(own_key >= last.key && q.own > -INFINITY && ex2((q.own - weight.m) * scale) >= q.least, [&](int32_t v, const Vec<T>& x) {
+    const int32_t i0 = sh.index(v);
+    float w[N], e[N];  // (the noise of the kept ones, asked for together)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      w[i] = ex2((widen(x.e[i]) - weight.m) * scale);
+      if (!kept_by(last, Key<T>::of(x.e[i]), i0 + i) || w[i] < q.least) w[i] = 0.f;
+      e[i] = w[i] > 0.f ? __ldg(noise + i0 + i) : 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      kept += w[i];
+      w[i] = __fdividef(w[i], e[i]);
+      if (w[i] > best.v) best = {w[i], i0 + i};
+    }
+  });
+  exact_race(p, sh, noise, q.r, weight, true, best, kept, cluster);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, const int cap) {
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  extern __shared__ __align__(16) unsigned char dyn[];
-  Shared& s = *reinterpret_cast<Shared*>(dyn);
+  Shared& s = shared();
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -520,13 +1021,15 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, 
 
   Share<T> sh;
   sh.row = static_cast<const T*>(p.x) + (int64_t)r * p.ld;
-  sh.held = reinterpret_cast<Vec<T>*>(dyn + ((sizeof(Shared) + 15) & ~(size_t)15));
   sh.shift = (int32_t)((reinterpret_cast<uintptr_t>(sh.row) & 15) / sizeof(T));
   sh.V = p.V;
   const int64_t vecs = ((int64_t)p.V + sh.shift + N - 1) / N;
   sh.first = (int32_t)(vecs * rank / C);
   sh.end = (int32_t)(vecs * (rank + 1) / C);
-  sh.cap = cap;
+  if (tid == 0 && sh.end > sh.first) {  // on its way while the row's parameters are
+    const int32_t i0 = max(sh.index(sh.first), 0), i1 = min(sh.index(sh.end), p.V);
+    prefetch_l2(sh.row + i0, (int64_t)(i1 - i0) * sizeof(T));
+  }
   const float* noise = p.noise + (int64_t)r * p.ld_noise;
   const float temp = p.how.temperature ? __ldg(p.how.temperature + r) : p.how.temperature_all;
   const int32_t top_k = p.how.top_k ? __ldg(p.how.top_k + r) : p.how.top_k_all;
@@ -536,123 +1039,125 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, 
   const bool params = temp >= 0.f && temp < INFINITY && !isnan(top_p) && !isnan(min_p);
 
   if (params && temp > 0.f && !cut_k && !cut_p && min_p <= 0.f) {
-    race_all(p, sh, noise, temp, r, s, cluster);
+    race_all(p, sh, noise, temp, r, cluster);
     return;
   }
 
-  // the share into shared memory, and its largest logits
-  Best top = {-INFINITY, INT32_MAX};
-  bool bad = false;
-  for (int32_t v0 = sh.first; v0 < sh.end; v0 += kLoads * kThreads) {
-    Vec<T> x[kLoads];
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int32_t v = v0 + u * kThreads + tid;
-      if (v < sh.end) x[u] = sh.load(v);
-    }
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int32_t v = v0 + u * kThreads + tid;
-      if (v >= sh.end) continue;
-      if (v - sh.first < cap) sh.held[v - sh.first] = x[u];
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float f = widen(x[u].e[e]);
-        bad |= !(f < INFINITY);
-        if (f > top.v) top = {f, sh.index(v) + e};
-      }
-    }
-  }
-  const float own_top = top.v;
-  // groups of `per` lanes: at least 128 of them, and a third more than the bound asks for
+  // each thread's largest logit (NaN if it has one) and, for a top_p of the whole row, its sum of weights
+  const bool need_all = params && temp > 0.f && cut_p && !cut_k;
+  Running a;
+  if (need_all)
+    sh.template each<kLoads>([&](int32_t, const Vec<T>& x) {
+      float w[N];
+      run_on(a, x, w, kLog2e / temp);
+    });
+  else
+    sh.template each<kLoads>([&](int32_t, const Vec<T>& x) { a.m = max_nan(a.m, vec_max(x)); });
+  const float own = a.m;
+  // groups of `per` threads: at least 128 of them, and a third more than the bound asks for
   const uint32_t reach = cut_k ? (uint32_t)top_k : (uint32_t)kUsual;
   int per = 32;
   while (per > 1 && (uint32_t)(C * kThreads / per) < max(reach + reach / 3, 128u)) per /= 2;
   const int groups = C * kThreads / per, own_groups = kThreads / per;
   const bool by_list = (cut_k || cut_p) && groups <= kGroups && (uint32_t)groups >= reach;
-  Best b = top;
-  for (int o = 1; o < 32; o <<= 1) {
-    if (by_list && o == per && lane % per == 0) s.own_group[tid / per] = b.v;
-    const float v = __shfl_xor_sync(0xffffffffu, b.v, o);
-    const int32_t i = __shfl_xor_sync(0xffffffffu, b.i, o);
-    take(b, v, i);
+  if (by_list) {
+    float g = own;
+    for (int o = 1; o < per; o <<= 1) g = max_nan(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if (lane % per == 0) s.own_group[tid / per] = g;
   }
-  if (by_list && per == 32 && lane == 0) s.own_group[warp] = b.v;
-  if (lane == 0) s.top[warp] = b;
-  if (tid == 0) s.count = 0;
-  bad = __syncthreads_or(bad);
-  if (tid == 0) s.bad = bad;
-  cluster.sync();
-  // every warp reads all warps' best
-  bool any_bad = false;
-  top = {-INFINITY, INT32_MAX};
-  for (int j = lane; j < C * kWarps; j += 32) {
-    const Best o = *at_rank(&s.top[j % kWarps], j / kWarps, cluster);
-    take(top, o.v, o.i);
+  if (tid == 0) {
+    s.count = 0;
+    s.cutoff = INT32_MAX;
   }
-  if (lane < C) any_bad = *at_rank(&s.bad, lane, cluster) != 0;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float v = __shfl_xor_sync(0xffffffffu, top.v, o);
-    const int32_t i = __shfl_xor_sync(0xffffffffu, top.i, o);
-    take(top, v, i);
-  }
-  any_bad = __any_sync(0xffffffffu, any_bad);
-  const Weight weight = {top.v, temp};
+  const float top = cluster_top(own, cluster);
+  const Weight weight = {top, temp};
 
-  const auto answer = [&](int32_t token, float logp) {
-    p.tokens[r] = token;
-    if (p.logp) p.logp[r] = logp;
-    if (token < 0) set_status(p.dev_status, STRIDE_DEV_NO_TOKEN);
-  };
-  const bool sound = !any_bad && top.v > -INFINITY && params;
+  const bool sound = params && top > -INFINITY && top < INFINITY;
   if (!sound || temp == 0.f) {
-    if (rank == 0 && tid == 0) answer(sound ? top.i : -1, sound ? 0.f : NAN);
-    cluster.sync();  // no CTA leaves while another may read its shared memory
+    if (sound) {  // the first of the largest
+      sh.each_of(own == top, [&](int32_t v, const Vec<T>& x) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (widen(x.e[e]) == top) atomicMin(&s.cutoff, sh.index(v) + e);
+      });
+      __syncthreads();
+      if (tid == 0) *at_rank(&s.lowest[rank], 0, cluster) = s.cutoff;
+    }
+    cluster.sync();  // (no CTA leaves while another may read its shared memory)
+    if (rank == 0 && tid == 0) {
+      int32_t token = INT32_MAX;
+      for (int o = 0; sound && o < C; ++o) token = min(token, s.lowest[o]);
+      answer(p, r, sound ? token : -1, sound ? 0.f : NAN);
+    }
     return;
   }
   const float least = fminf(min_p, 1.f);
-  const uint32_t none = Key<T>::of(lowest<T>()), first = Key<T>::of(static_cast<T>(top.v));
+  const uint32_t none = Key<T>::of(lowest<T>()), first = Key<T>::of(static_cast<T>(top)), own_key = Key<T>::of(static_cast<T>(own));
+  float all = 0.f, z = 0.f;  // the mass of the share's tokens, of the row's
+  if (need_all) all = block_sum(own == -INFINITY ? 0.f : a.z * ex2((own - top) * (kLog2e / temp)));
 
   if (by_list) {
-    for (int j = tid; j < groups; j += kThreads) s.group[j] = *at_rank(&s.own_group[j % own_groups], j / own_groups, cluster);
-    __syncthreads();
-    // the bound: the smallest of them that fewer than `reach` exceed
-    for (int j = tid; j < groups; j += kThreads) {
-      const float f = s.group[j];
-      uint32_t greater = 0, equal_before = 0;
-      for (int k = 0; k < groups; ++k) {
-        greater += s.group[k] > f;
-        equal_before += s.group[k] == f && k < j;
-      }
-      if (greater + equal_before == reach - 1) s.bound = f;
-    }
-    __syncthreads();
-    const float bound = s.bound;
-    float all = 0.f, listed = 0.f;
-    const bool need_all = !cut_k;
-    if (need_all || own_top >= bound) {
-      for (int32_t v = sh.first + tid; v < sh.end; v += kThreads) {
-        const Vec<T> x = sh.get(v);
+    // The bound: the largest key that at least `reach` of the groups reach (to within an eighth of them), by bisection;
+    // one warp's work where it holds all groups (four a lane).
+    constexpr int kMine = kGroups / kThreads;
+    uint32_t lo = none, hi = first + 1;  // (all groups reach lo; fewer than `reach` reach hi, or hi is past the largest)
+    const auto group = [&](int j) {
+      return j < groups ? Key<T>::of(static_cast<T>(*at_rank(&s.own_group[j % own_groups], j / own_groups, cluster))) : 0u;
+    };
+    if (groups <= 128) {
+      if (warp == 0) {
+        uint32_t g[4];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float f = widen(x.e[e]);
-          const float w = need_all ? weight(f) : 0.f;
-          all += w;
-          if (f >= bound && f > -INFINITY) {
-            listed += w;
-            const uint32_t at = atomicAdd(&s.count, 1u);
-            if (at < kList) s.list[at] = (uint64_t)Key<T>::of(x.e[e]) << 32 | (uint32_t)~(sh.index(v) + e);
+        for (int u = 0; u < 4; ++u) g[u] = group(lane + u * 32);
+        while (hi - lo > 1) {
+          const uint32_t mid = lo + (hi - lo) / 2;
+          uint32_t n = 0;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) n += __popc(__ballot_sync(0xffffffffu, g[u] >= mid));
+          if (n >= reach) {
+            lo = mid;
+            if (n <= reach + reach / 8) break;
+          } else {
+            hi = mid;
           }
+        }
+        if (lane == 0) s.bound = lo;
+      }
+      __syncthreads();
+      lo = s.bound;
+    } else {
+      uint32_t g[kMine];
+#pragma unroll
+      for (int u = 0; u < kMine; ++u) g[u] = group(tid + u * kThreads);
+      while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        uint32_t n = 0;
+#pragma unroll
+        for (int u = 0; u < kMine; ++u)
+          if (u * kThreads < groups) n += __syncthreads_count(g[u] >= mid);
+        if (n >= reach) {
+          lo = mid;
+          if (n <= reach + reach / 8) break;
+        } else {
+          hi = mid;
         }
       }
     }
-    if (need_all) {
-      all = block_sum(all, s);
-      listed = block_sum(listed, s);
-    } else {
+    const uint32_t bound = max(lo, none + 1);  // (tokens of -inf are none)
+    float listed = 0.f;
+    sh.each_of(own_key >= bound, [&](int32_t v, const Vec<T>& x) {
+      visit(
+          x, [&](T y, int) { return Key<T>::of(y) >= bound; },
+          [&](T y, int e) {
+            if (need_all) listed += weight(widen(y));
+            const uint32_t at = atomicAdd(&s.count, 1u);
+            if (at < kList) s.list[at] = (uint64_t)Key<T>::of(y) << 32 | (uint32_t)~(sh.index(v) + e);
+          });
+    });
+    if (need_all)
+      listed = block_sum(listed);
+    else
       __syncthreads();
-    }
     const uint32_t n_own = s.count, segment = kList / C;
     for (uint32_t j = tid; j < min(n_own, segment); j += kThreads) *at_rank(&s.pushed[rank * segment + j], 0, cluster) = s.list[j];
     if (tid < C) {
@@ -663,7 +1168,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, 
     cluster.sync();
     bool held = true;
     uint32_t n = 0;
-    float z = 0.f, zl = 0.f;
+    float zl = 0.f;
     for (int o = 0; o < C; ++o) {
       held = held && s.listed[o] <= segment;
       n += s.listed[o];
@@ -671,34 +1176,12 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, 
       zl += s.sum_listed[o];
     }
     // the list holds what is kept: top_k of the largest; or more than top_p of the mass, or all of w >= min_p
-    if (held && (cut_k || zl > top_p * z * 1.00001f || weight(bound) < least)) {
+    if (held && (cut_k || zl > top_p * z * 1.00001f || weight(Key<T>::value(bound)) < least)) {
       if (rank == 0) {
-        for (uint32_t j = tid; j < n; j += kThreads) {
-          uint32_t o = 0, k = j;
-          while (k >= s.listed[o]) k -= s.listed[o++];
-          s.list[j] = s.pushed[o * segment + k];
-        }
-        __syncthreads();
-        // ranks by (logit, index): at most kList / kThreads tokens a thread
-        uint64_t mine[kList / kThreads];
-        uint32_t place[kList / kThreads];
-#pragma unroll
-        for (int u = 0; u < kList / kThreads; ++u) {
-          const uint32_t j = tid + u * kThreads;
-          place[u] = 0;
-          if (j < n) {
-            mine[u] = s.list[j];
-            for (uint32_t k = 0; k < n; ++k) place[u] += s.list[k] > mine[u];
-          }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kList / kThreads; ++u)
-          if (tid + u * kThreads < n) s.list[place[u]] = mine[u];
-        __syncthreads();
+        gather_list(n, segment);
         constexpr int kPer = kList / kThreads;  // consecutive ranks of a thread
         const uint32_t kept_k = cut_k ? min((uint32_t)top_k, n) : n;
-        float w[kPer], e[kPer], mass = 0.f;
+        float w[kPer], e[kPer], d[kPer], mass = 0.f;
         int32_t idx[kPer];
 #pragma unroll
         for (int u = 0; u < kPer; ++u) {
@@ -709,7 +1192,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, 
             const uint64_t q = s.list[j];
             idx[u] = (int32_t)~(uint32_t)q;
             e[u] = __ldg(noise + idx[u]);
-            w[u] = weight(Key<T>::value((uint32_t)(q >> 32)));
+            d[u] = weight.log(Key<T>::value((uint32_t)(q >> 32)));
+            w[u] = expf(d[u]);
           }
           mass += w[u];
         }
@@ -741,116 +1225,38 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p, 
           }
           before += w[u];
         }
-        best = block_best(best, s);
-        kept = block_sum(kept, s);
-        if (tid == 0) {
-          if (best.v > 0.f)
-            answer(best.i, weight.log(widen(sh.row[best.i])) - logf(kept));
-          else
-            answer(-1, NAN);
+        const Best mine = best;
+        best = block_best(best);
+        kept = block_sum(kept);
+        if (best.v > 0.f) {
+#pragma unroll
+          for (int u = 0; u < kPer; ++u)
+            if (mine.i == best.i && idx[u] == best.i && tid * kPer + u < kept_k) answer(p, r, best.i, d[u] - logf(kept));
+        } else if (tid == 0) {
+          answer(p, r, -1, NAN);
         }
       }
       return;  // (nothing of another CTA is read after the last cluster.sync)
     }
-    cluster.sync();  // s.list and s.group make room for the histogram
+    cluster.sync();  // s.list makes room for the histogram
   }
 
-  // what is kept: keys above `key`, and of those at it the ones of index below `cutoff`
-  uint32_t key = none;
-  int32_t cutoff = 0;
-  if (cut_k || cut_p) {
-    constexpr double kOne = 1099511627776.0;  // 2^40, the fixed-point 1
-    Cut cut = {none, 0, 0, 0};
-    uint32_t ties = 0;  // of the tokens at the cut, the first so many are kept
-    uint32_t from = none + 1;
-    double mass = 0.0;
-    if (cut_k) {  // (all tokens that are not ruled out, where those are fewer)
-      cut = search(sh, weight, from, first, false, (uint64_t)top_k, cut_p, s, cluster);
-      ties = min((uint32_t)top_k - cut.above, cut.ties);
-      mass = (double)cut.mass_above + kOne * ties * weight(Key<T>::value(cut.key));
-      from = cut.key;
-    } else {
-      float t = 0.f;
-      for (int32_t v = sh.first + tid; v < sh.end; v += kThreads) {
-        const Vec<T> x = sh.get(v);
-#pragma unroll
-        for (int e = 0; e < N; ++e) t += weight(widen(x.e[e]));
-      }
-      t = block_sum(t, s);
-      if (tid == 0) s.sum = t;
-      cluster.sync();
-      double z = 0.0;
-      for (int o = 0; o < C; ++o) z += *at_rank(&s.sum, o, cluster);
-      mass = kOne * z;
-      // The tokens of w < (1 - top_p) z / (2 V) hold less than half of what may be left out: none of them is needed.
-      const float low = top.v + temp * logf(fmaxf((1.f - fmaxf(top_p, 0.f)) * (float)z / (2.f * (float)p.V), 1e-30f));
-      const uint32_t k = Key<T>::of(static_cast<T>(fmaxf(low, -1e30f)));
-      if (k > from + 1 && k <= first) from = k - 1;  // (a step below: the conversion may have rounded up)
-    }
-    if (cut_p) {
-      const double goal = fmax(ceil((double)top_p * mass), 1.0);
-      const Cut by_mass = search(sh, weight, from, first, true, (uint64_t)goal, true, s, cluster);
-      const uint32_t most = cut_k && by_mass.key == cut.key ? ties : by_mass.ties;
-      const double one = fmax((double)weight(Key<T>::value(by_mass.key)) * kOne, 1.0);
-      const double need = ceil((goal - (double)by_mass.mass_above) / one);
-      ties = need < 1.0 ? 1u : need < (double)most ? (uint32_t)need : most;
-      cut = by_mass;
-    }
-    key = cut.key;
-    cutoff = INT32_MAX;
-    if (ties < cut.ties) cutoff = tie_cutoff(sh, key, ties, s, cluster);
-  }
-  // the race
-  Best best = {-1.f, INT32_MAX};
-  float kept = 0.f;
-  for (int32_t v = sh.first + tid; v < sh.end; v += kThreads) {
-    const Vec<T> x = sh.get(v);
-    const int32_t i0 = sh.index(v);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const uint32_t k = Key<T>::of(x.e[e]);
-      if (k < key || (k == key && i0 + e >= cutoff)) continue;
-      const float w = weight(widen(x.e[e]));
-      if (w < least) continue;
-      kept += w;
-      take(best, w / __ldg(noise + i0 + e), i0 + e);
-    }
-  }
-  best = block_best(best, s);
-  kept = block_sum(kept, s);
-  if (tid == 0) {
-    *at_rank(&s.race[rank], 0, cluster) = best;
-    *at_rank(&s.kept[rank], 0, cluster) = kept;
-  }
-  cluster.sync();
-  if (rank == 0 && tid == 0) {
-    float z = 0.f;
-    for (int o = 0; o < C; ++o) {
-      take(best, s.race[o].v, s.race[o].i);
-      z += s.kept[o];
-    }
-    if (best.v > 0.f)
-      answer(best.i, weight.log(widen(sh.row[best.i])) - logf(z));
-    else
-      answer(-1, NAN);
-  }
+  const Row row = {temp, top_p, least, own, z, top_k, r, cut_k, cut_p};
+  race_above(p, sh, noise, weight, row, cluster);
 }
 
 template <typename T>
-cudaError_t run(const SampleParams& p, cudaStream_t stream) {
-  int C = kMaxCluster;
-  while (C > 1 && p.V < 4096 * C) C /= 2;
-  const int64_t vecs = ((int64_t)p.V * sizeof(T) + 15) / 16 + 1;
-  const int64_t share = (vecs + C - 1) / C + 1;
-  const int64_t most = (220 * 1024 - (int64_t)sizeof(Shared) - 16) / 16;
-  const int cap = (int)(share < most ? share : most);
-  const size_t smem = ((sizeof(Shared) + 15) & ~(size_t)15) + (size_t)cap * 16;
-  cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-  if (e != cudaSuccess) return e;
+cudaError_t run(const SampleParams& p, int sms, cudaStream_t stream) {
+  // CTAs of a row: 8 where all run at once (two on an SM), 4 up to two rows an SM, else 1; at least a vector per thread.
+  // us a call on rows of 151,936 bf16 logits, with 8 / 4 / 2 / 1: 1 row, top_k 50: 10.0 / 11.3 / 13.3 / 18.4; 64 rows: 24.8 /
+  // 14.6 / 16.8 / 27.0; 256 rows of mixed parameters, a few with a top_p over the tail: 131 / 106 / 139 / 226; 512 uncut rows of
+  // 32,000 fp32: 144 / 80.5 / 60.4 / 47.7.
+  int C = (int64_t)p.rows * kMaxCluster <= 2 * sms ? kMaxCluster : p.rows <= 2 * sms ? 4 : 1;
+  while (C > 1 && p.V < C * kThreads * Vec<T>::N) C /= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)p.rows * C));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kDepth * kThreads * 16;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -860,17 +1266,19 @@ cudaError_t run(const SampleParams& p, cudaStream_t stream) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, p, cap);
+  cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDepth * kThreads * 16);
+  if (e != cudaSuccess) return e;
+  e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, p);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_sample(const SampleParams& p, int dtype, int, cudaStream_t stream) {
+cudaError_t launch_sample(const SampleParams& p, int dtype, int sms, cudaStream_t stream) {
   if (p.rows > INT32_MAX / kMaxCluster) return cudaErrorInvalidConfiguration;
-  if (dtype == STRIDE_DTYPE_BF16) return run<__nv_bfloat16>(p, stream);
-  if (dtype == STRIDE_DTYPE_F16) return run<__half>(p, stream);
-  return run<float>(p, stream);
+  if (dtype == STRIDE_DTYPE_BF16) return run<__nv_bfloat16>(p, sms, stream);
+  if (dtype == STRIDE_DTYPE_F16) return run<__half>(p, sms, stream);
+  return run<float>(p, sms, stream);
 }
 
 }  // namespace stride
