@@ -1,0 +1,230 @@
+// attention_line.cuh -- the line of tiles that attention over a paged cache is
+// cut into, shared by its kernels (sm_103a).
+//
+// A unit is a sequence, a block of its rows (new tokens times the query heads of
+// one key/value head) and a kv head; its tiles are runs of slots.  The units'
+// tiles, one unit after the other, form a line, of which every worker (a warp or
+// a CTA) takes an equal share whatever the sequences' lengths.  Where a unit is
+// cut between workers each leaves its part (largest score, sum, unnormalised
+// output, in 32 bits) in a slot of the workspace, and the worker where it starts
+// leaves a Joined record for the kernel that joins them, in the line's order.
+#pragma once
+
+#include <math.h>
+
+#include "decode_internal.h"
+#include "stride_device.cuh"
+
+namespace stride {
+
+constexpr int kLineSeqs = 1024;  // sequences whose places in the line fit in shared memory
+
+// A sequence of the call.
+struct Seq {
+  int32_t ctx, n, off;  // committed tokens, new tokens, the first new token's row
+  bool bad;             // its rows are NaN
+};
+
+__device__ __forceinline__ Seq sequence(const AttentionParams& p, int b) {
+  Seq s;
+  s.off = __ldg(p.cache.tok_off + b);
+  s.n = __ldg(p.cache.tok_off + b + 1) - s.off;
+  s.ctx = __ldg(p.cache.ctx_len + b);
+  s.bad = false;
+  if (s.off < 0 || s.n < 0 || (int64_t)s.off + s.n > p.n_tokens) {
+    s.n = 0;  // (no rows of the call: nothing to write)
+    s.bad = true;
+  }
+  if (s.ctx < 0 || (int64_t)s.ctx + s.n > (int64_t)p.cache.table_stride * p.cache.page_size || (int64_t)s.ctx + s.n > INT32_MAX - 256 ||
+      (p.tree_mask && s.n > STRIDE_MAX_TREE))
+    s.bad = true;
+  return s;
+}
+
+// How rows and slots are grouped: row = token * group + head within the kv
+// head's query heads.
+struct Grouping {
+  int32_t group, rows, tile;  // query heads per kv head, rows of a block, slots of a tile
+  bool chain;                 // no tree mask: each token sees the new ones up to itself
+  __device__ __forceinline__ int blocks(const Seq& s) const { return (int)(((int64_t)s.n * group + rows - 1) / rows); }
+  // One past the last slot that a block's rows may see.
+  __device__ __forceinline__ int end(const Seq& s, int block) const {
+    if (!chain) return s.ctx + s.n;
+    const int64_t last = min((int64_t)(block + 1) * rows, (int64_t)s.n * group) - 1;
+    return s.ctx + (int)(last / group) + 1;
+  }
+  __device__ __forceinline__ int tiles(const Seq& s, int block) const { return s.bad ? 1 : (end(s, block) + tile - 1) / tile; }
+  // The tiles of one head of all blocks.
+  __device__ __forceinline__ int64_t all_tiles(const Seq& s) const {
+    const int nb = blocks(s);
+    if (nb == 0) return 0;
+    if (!chain || s.bad || nb == 1) return (int64_t)nb * tiles(s, 0);
+    int64_t t = 0;
+    for (int k = 0; k < nb; ++k) t += tiles(s, k);
+    return t;
+  }
+};
+
+// A place in the line.
+struct Cursor {
+  int32_t b, block, head, tile, tiles;
+  Seq s;
+
+  __device__ __forceinline__ void next(const AttentionParams& p, const Grouping& g) {
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++head < p.cache.n_heads) return;
+    head = 0;
+    if (++block >= g.blocks(s)) {
+      block = 0;
+      do {
+        if (++b >= p.cache.n_seqs) return;  // (past the last tile of the line)
+        s = sequence(p, b);
+      } while (s.n == 0);
+    }
+    tiles = g.tiles(s, block);
+  }
+};
+
+// Sequences' places in the line: line[b] is the number of tiles before sequence b
+// + 1 (all heads), for the first kLineSeqs.  Returns the line's length; called by
+// all of a CTA's threads, whose warps' sums pass through part.
+template <int kThreads>
+__device__ __forceinline__ int64_t lay_line(const AttentionParams& p, const Grouping& g, int64_t* line, int64_t* part) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int64_t total = 0;
+  for (int b0 = 0; b0 < p.cache.n_seqs; b0 += kThreads) {
+    const int b = b0 + tid;
+    int64_t t = 0;
+    if (b < p.cache.n_seqs) {
+      const Seq s = sequence(p, b);
+      if (s.bad && blockIdx.x == 0) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
+      t = g.all_tiles(s) * p.cache.n_heads;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += v;
+    }
+    __syncthreads();
+    if (lane == 31) part[warp] = t;
+    __syncthreads();
+    int64_t before = total;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += part[w];
+      total += part[w];
+    }
+    if (b < p.cache.n_seqs && b < kLineSeqs) line[b] = before + t;
+  }
+  __syncthreads();
+  return total;
+}
+
+// The place of tile t (one that the line has), for a whole warp alike.
+__device__ __forceinline__ Cursor place_in_line(const AttentionParams& p, const Grouping& g, const int64_t* line, int64_t t) {
+  const int lane = threadIdx.x & 31, n = p.cache.n_seqs, m = min(n, kLineSeqs);
+  Cursor c;
+  int64_t inside;
+  if (t < line[m - 1]) {
+    int lo = 0, hi = m - 1;  // the first sequence whose end lies past t
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (line[mid] > t)
+        hi = mid;
+      else
+        lo = mid + 1;
+    }
+    c.b = lo;
+    inside = t - (lo ? line[lo - 1] : 0);
+  } else {
+    int64_t before = line[m - 1];
+    c.b = m;
+    inside = 0;
+    for (int b0 = m; b0 < n; b0 += 32) {
+      const int b = b0 + lane;
+      const int64_t own = b < n ? g.all_tiles(sequence(p, b)) * p.cache.n_heads : 0;
+      int64_t incl = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, before + incl > t);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        c.b = b0 + l;
+        inside = t - before - __shfl_sync(0xffffffffu, incl - own, l);
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+  }
+  c.s = sequence(p, c.b);
+  c.block = 0;
+  while (true) {
+    c.tiles = g.tiles(c.s, c.block);
+    const int64_t of_block = (int64_t)c.tiles * p.cache.n_heads;
+    if (inside < of_block) break;
+    inside -= of_block;
+    ++c.block;
+  }
+  c.head = (int)(inside / c.tiles);
+  c.tile = (int)(inside - (int64_t)c.head * c.tiles);
+  return c;
+}
+
+// A worker's share of the line: each of the first min(workers, total) has one.
+struct Span {
+  int64_t begin, end, total;
+  int32_t workers;  // that have a share
+};
+__device__ __forceinline__ Span span_of(int64_t total, int worker, int workers) {
+  Span s;
+  s.total = total;
+  s.workers = (int)(total < workers ? total : workers);
+  s.begin = worker < s.workers ? total * worker / s.workers : 0;
+  s.end = worker < s.workers ? total * (worker + 1) / s.workers : 0;
+  return s;
+}
+
+// What a worker leaves: the unit that starts in its share and goes on in those
+// of the workers after it, up to `last` (none: last 0).
+struct Joined {
+  int32_t last, seq, block, head;
+};
+// The last worker that has tiles of a unit that ends at tile unit_end.
+__device__ __forceinline__ int last_worker(const Span& s, int worker, int64_t unit_end) {
+  int64_t last = unit_end * s.workers / s.total;
+  while (last > worker && s.total * last / s.workers >= unit_end) --last;
+  while (s.total * (last + 1) / s.workers < unit_end) ++last;
+  return (int)last;
+}
+
+// Workspace: a Joined per worker, then two slots a worker (of the unit that it
+// starts with and the one that it ends with, if cut): rows x D outputs, the rows'
+// largest scores (in units of ln 2), their sums.
+__host__ __device__ inline size_t slot_floats(int rows, int D) { return (size_t)rows * (D + 2); }
+__host__ __device__ inline size_t slots_offset(int workers) { return ((size_t)workers * sizeof(Joined) + 255) & ~(size_t)255; }
+struct Slots {
+  Joined* joined;
+  float* base;
+  size_t size;
+  __device__ __forceinline__ Slots(void* workspace, int workers, int rows, int D)
+      : joined(static_cast<Joined*>(workspace)),
+        base(reinterpret_cast<float*>(static_cast<char*>(workspace) + slots_offset(workers))),
+        size(slot_floats(rows, D)) {}
+  // starts: the unit starts in this worker's share
+  __device__ __forceinline__ float* of(int worker, bool starts) const { return base + (size_t)(2 * worker + (starts ? 1 : 0)) * size; }
+};
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+cudaError_t launch_attention_few(const AttentionParams& p, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_attention_many(const AttentionParams& p, int dtype, int sms, cudaStream_t stream);
+size_t attention_few_bytes(int D);
+size_t attention_many_bytes(int D);
+// Joins the cut units of a kernel of `workers` workers and blocks of `rows` rows.
+cudaError_t launch_attention_join(const AttentionParams& p, int dtype, int workers, int rows, cudaStream_t stream);
+
+}  // namespace stride
