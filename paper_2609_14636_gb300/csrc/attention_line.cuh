@@ -222,6 +222,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 cudaError_t launch_attention_few(const AttentionParams& p, int dtype, int sms, cudaStream_t stream);
 cudaError_t launch_attention_many(const AttentionParams& p, int dtype, int sms, cudaStream_t stream);
+// Whether the kernel for many rows takes the cache (its copies are boxes of 8 slots at least).
+bool attention_many_takes(const AttentionParams& p);
 size_t attention_few_bytes(int D);
 size_t attention_many_bytes(int D);
 // Joins the cut units of a kernel of `workers` workers and blocks of `rows` rows.

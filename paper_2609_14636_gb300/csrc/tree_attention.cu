@@ -6,8 +6,9 @@
 //   lse = ln sum exp s
 //
 // A sequence's new tokens times the query heads of one key/value head are the
-// rows of one product, which reads the keys and values once
-// (tree_attention_few.cu, 16 rows at a time).
+// rows of one product, which reads the keys and values once.  Up to 16 of them:
+// tree_attention_few.cu, a stream of keys and values through warps; more:
+// tree_attention_many.cu, tcgen05 products of 128 rows.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -112,10 +113,14 @@ cudaError_t launch_attention_join(const AttentionParams& p, int dtype, int worke
 }
 
 size_t attention_workspace_bytes(int64_t, int, int, int D) {
-  return (attention_few_bytes(D) + 255) & ~(size_t)255;
+  const size_t few = attention_few_bytes(D), many = attention_many_bytes(D);
+  return ((few > many ? few : many) + 255) & ~(size_t)255;
 }
 
 cudaError_t launch_tree_attention(const AttentionParams& p, int dtype, int sms, cudaStream_t stream) {
+  // (rows of an ordinary sequence: only the device knows how many each has)
+  const int64_t rows = ((p.n_tokens + p.cache.n_seqs - 1) / p.cache.n_seqs) * (p.Hq / p.cache.n_heads);
+  if (rows > 16 && attention_many_takes(p)) return launch_attention_many(p, dtype, sms, stream);
   return launch_attention_few(p, dtype, sms, stream);
 }
 
