@@ -3,14 +3,16 @@
 //
 // Blocks of 128 rows by tiles of 64 slots on the tensor cores.  One CTA on an SM
 // takes a share of the line of tiles (attention_line.cuh); its warps:
-//   4     looks up a tile's pages and starts their tensor copies (a box of up to
+//   8     looks up a tile's pages and starts their tensor copies (a box of up to
 //         64 slots by 128 bytes, swizzled), up to five tiles ahead;
-//   5     one thread issues the products: scores Q K^T of the next tile, then
+//   9     one thread issues the products: scores Q K^T of the next tile, then
 //         output += P V of this one (tcgen05, accumulators in tensor memory);
-//   0-3   a thread for each row: scores from tensor memory, running maximum and
-//         sum, weights P back into tensor memory, where the second product reads
-//         them.  Scores and weights have two buffers each, so the products of one
-//         tile run while the weights of the next are formed.
+//   0-7   two teams of a thread for each row, which take the even and the odd
+//         tiles: scores from tensor memory, running maximum and sum, weights P
+//         back into tensor memory, where the second product reads them.  Each
+//         team has scores, weights and an output of its own, as if the tiles were
+//         two sequences, joined where the unit or the share ends: nothing of one
+//         tile waits for the other's.
 // The output is rescaled only where a row's maximum has grown by more than 2^8
 // since it was last (weights up to 256 fit both types as well as weights up to 1;
 // maximum and sum stay consistent either way).  Slots past the end, and new tokens
@@ -31,7 +33,8 @@ namespace {
 
 constexpr int kRows = 128;
 constexpr int kSlots = 64;
-constexpr int kThreads = 192;
+constexpr int kRowWarps = 8;
+constexpr int kThreads = (kRowWarps + 2) * 32;
 constexpr int kMaxWorkers = 152;
 constexpr float kGrowth = 8.f;  // log2
 
@@ -107,8 +110,9 @@ struct Plan {
   static constexpr int kStage = 2 * kKeys;                  // keys, then values
   static constexpr int kStages = 5;
   static constexpr size_t kSmem = kQ + (size_t)kStages * kStage + 1024;  // (the base rounded up to 1,024)
-  // columns of tensor memory: scores (two buffers), output, weights (two)
-  static constexpr int kO = 2 * kSlots, kP = kO + D, kColumns = kP + kSlots <= 256 ? 256 : 512;
+  // columns of tensor memory: scores, outputs, weights of the two teams
+  static constexpr int kO = 2 * kSlots, kP = kO + 2 * D, kColumns = 512;
+  static_assert(kP + kSlots <= kColumns, "tensor memory");
 };
 
 struct Barriers {
@@ -134,6 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ int32_t s_lost[8];  // the tile (1-based, of the share) in a stage that has a slot without a page
   __shared__ int32_t s_abort;
   __shared__ uint32_t s_tmem;
+  __shared__ float s_m[2][kRows], s_l[2][kRows];  // the teams' maxima and sums, where they are joined
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const Grouping g = {p.Hq / p.cache.n_heads, kRows, kSlots, p.tree_mask == nullptr};
@@ -151,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars.weights[i], 4);
       mbar_init(&bars.output[i], 1);
     }
-    mbar_init(&bars.queries, 4);
+    mbar_init(&bars.queries, kRowWarps);
     mbar_init(&bars.drained, 1);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -162,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const Slots slots(p.workspace, gridDim.x, kRows, D);
   if (tid == 0) slots.joined[blockIdx.x] = {0, 0, 0, 0};
   if (span.begin >= span.end) return;  // (all threads alike)
-  if (warp == 5) {
+  if (warp == kRowWarps + 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(L::kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     fence_before();
@@ -176,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, kWaitTimeoutNs, &s_abort); };
   bool ok = true;
 
-  if (warp == 4) {
+  if (warp == kRowWarps) {
     // ---- copies ----
     const int boxes = kSlots / box;  // of a tile's slots: at most 8, so that a lane has one copy
     int t = 0;
@@ -219,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int k = t < L::kStages ? 0 : t - L::kStages; k < t; ++k)
         mbar_wait_warp(&bars.full[k % L::kStages], (k / L::kStages) & 1, kWaitTimeoutNs, &go_on);
     }
-  } else if (warp == 5) {
+  } else if (warp == kRowWarps + 1) {
     // ---- products ----
     if (lane == 0) {
       constexpr uint32_t qk = product<T>(kSlots, false), pv = product<T>(D, true);
@@ -238,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         commit(&bars.scores[t & 1]);
       };
       scores(0, true);
-      bool first = true;
+      unsigned begun = 0;  // teams (bits) whose output holds something of the unit
       for (int t = 0; t < n && ok; ++t) {
         const bool last = ahead.tile + 1 == ahead.tiles;  // of its unit
         ahead.next(p, g);
@@ -249,10 +254,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t v = stages + (t % L::kStages) * L::kStage + L::kKeys;
 #pragma unroll
         for (int x = 0; x < kSlots / 16; ++x)
-          mma_ts(tmem + L::kO, tmem + L::kP + (t & 1) * (kSlots / 2) + x * 8, matrix(v + x * 16 * 128, kSlots * 128), pv, !first || x > 0);
+          mma_ts(tmem + L::kO + (t & 1) * D, tmem + L::kP + (t & 1) * (kSlots / 2) + x * 8, matrix(v + x * 16 * 128, kSlots * 128), pv,
+                 x > 0 || (begun >> (t & 1) & 1));
         commit(&bars.empty[t % L::kStages]);
         commit(&bars.output[t & 1]);
-        first = last;
+        begun = last ? 0 : begun | 1u << (t & 1);
         if (t + 1 < n && last) scores(t + 1, true);
       }
       if (!ok) {
@@ -265,24 +271,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ---- rows ----
-    const uint32_t my = tmem + ((uint32_t)(warp * 32) << 16);  // this warp's lanes of tensor memory
+    const int team = warp / 4, row = tid % kRows;
+    const uint32_t my = tmem + ((uint32_t)(warp % 4 * 32) << 16);  // this warp's lanes of tensor memory
+    const uint32_t my_scores = my + team * kSlots, my_out = my + L::kO + team * D, my_weights = my + L::kP + team * (kSlots / 2);
     const float scale2 = p.scale * kLog2e;
     RowView view = {0, 0};
     float m = -INFINITY, l = 0.f;
     bool nan = false;
-    int first_tile = 0;
-    // This thread's row of a unit's queries into shared memory.
+    int first_tile = 0, first_t = 0;  // of the unit in this share
+    const auto all_rows = [&] { asm volatile("bar.sync 1, %0;" ::"n"(kRowWarps * 32) : "memory"); };
+    // This thread's row of a unit's queries into shared memory (a team takes half of the columns).
     const auto take_queries = [&](const Cursor& u) {
-      const int64_t rr = (int64_t)u.block * kRows + tid;
+      const int64_t rr = (int64_t)u.block * kRows + row;
       const int i = (int)(rr / g.group);
       const bool have = i < u.s.n;
       const T* q = static_cast<const T*>(p.q) + (u.s.off + (have ? i : 0)) * p.q_tok + (u.head * g.group + rr % g.group) * p.q_head;
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (have && c * 8 < p.D) x = *reinterpret_cast<const uint4*>(q + c * 8);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + (c / 8) * kRows * 128 + tid * 128 + (((c % 8) ^ (tid & 7)) << 4)),
-                     "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
+      for (int x = 0; x < D / 16; ++x) {
+        const int c = team * (D / 16) + x;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (have && c * 8 < p.D) v = *reinterpret_cast<const uint4*>(q + c * 8);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + (c / 8) * kRows * 128 + row * 128 + (((c % 8) ^ (row & 7)) << 4)),
+                     "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                      : "memory");
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -292,174 +302,207 @@ __global__ void __launch_bounds__(kThreads, 1)
     take_queries(at);
     bool fresh = true;
     for (int t = 0; t < n; ++t) {
-      const int st = t % L::kStages, b = t & 1;
       if (fresh) {
         fresh = false;
         m = -INFINITY;
         l = 0.f;
         nan = at.s.bad;
         first_tile = at.tile;
-        const int i = (int)(((int64_t)at.block * kRows + tid) / g.group);
+        first_t = t;
+        const int i = (int)(((int64_t)at.block * kRows + row) / g.group);
         const bool have = i < at.s.n;
         view.lim = at.s.ctx + (have ? i + 1 : 0);
         view.bits = have && !g.chain ? __ldg(p.tree_mask + at.s.off + i) : 0;
       }
-      ok = wait(&bars.full[st], (t / L::kStages) & 1) && wait(&bars.scores[b], (t >> 1) & 1);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      fence_after();
-      nan |= s_lost[st] == t + 1;
-      float s[kSlots];
-      {
-        uint32_t r0[32], r1[32];
-        tmem_load32(r0, my + b * kSlots);
-        tmem_load32(r1, my + b * kSlots + 32);
-        tmem_wait_load();
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          s[j] = __uint_as_float(r0[j]);
-          s[32 + j] = __uint_as_float(r1[j]);
-        }
-      }
-      if (at.tile * kSlots + kSlots > at.s.ctx) {  // some slots are new tokens', or past the end
-        const int slot0 = at.tile * kSlots;
-#pragma unroll
-        for (int j = 0; j < kSlots; ++j) {
-          const int back = slot0 + j - at.s.ctx;
-          const bool seen = g.chain ? slot0 + j < view.lim : back < 0 || (back < at.s.n && ((view.bits >> (back & 63)) & 1));
-          if (!seen) s[j] = -INFINITY;
-        }
-        // values that no row uses become zeros
-        const int end = at.s.bad ? 0 : g.end(at.s, at.block), slot = slot0 + (tid & 63), back = slot - at.s.ctx;
-        bool out = slot >= end;
-        if (!out && !g.chain && back >= 0) {
-          uint64_t any = 0;
-          const int i0 = (int)((int64_t)at.block * kRows / g.group), i1 = min(at.s.n, (int)(((int64_t)(at.block + 1) * kRows - 1) / g.group) + 1);
-          for (int i = i0; i < i1; ++i) any |= __ldg(p.tree_mask + at.s.off + i);
-          out = !((any >> (back & 63)) & 1);
-        }
-        if (out && tid / 64 < L::kHalves) {
-          const uint32_t v = stages + st * L::kStage + L::kKeys + (tid / 64) * kSlots * 128 + (tid & 63) * 128;
-#pragma unroll
-          for (int c = 0; c < 8; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + c * 16), "r"(0) : "memory");
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      }
-      float mx = s[0];
-#pragma unroll
-      for (int j = 1; j < kSlots; ++j) mx = fmaxf(mx, s[j]);
-      mx *= scale2;
-      if (scale2 <= 0.f) {  // (the largest score is the smallest product)
-        mx = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < kSlots; ++j) mx = fmaxf(mx, s[j] == -INFINITY ? -INFINITY : s[j] * scale2);
-      }
-      // the row's reference grows at its first tile that sees anything, then by 2^8 at least
-      const bool grows = mx > m + kGrowth || (m == -INFINITY && mx > -INFINITY);
-      float by = 1.f;
-      if (grows) {
-        by = ex2(m - mx);
-        m = mx;
-        l *= by;
-      }
-      if (t > 0 && at.tile != first_tile && __any_sync(0xffffffffu, grows)) {
-        ok = __all_sync(0xffffffffu, wait(&bars.output[b ^ 1], ((t - 1) >> 1) & 1));
+      // (a warp whose wait has run out goes on without waiting, to the barriers that the others are at)
+      if (ok && (t & 1) == team) do {
+        const int st = t % L::kStages;
+        ok = wait(&bars.full[st], (t / L::kStages) & 1) && wait(&bars.scores[team], (t >> 1) & 1);
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t r[32];
-          tmem_load32(r, my + L::kO + c * 32);
+        nan |= s_lost[st] == t + 1;
+        float s[kSlots];
+        {
+          uint32_t r0[32], r1[32];
+          tmem_load32(r0, my_scores);
+          tmem_load32(r1, my_scores + 32);
           tmem_wait_load();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * by);
-          tmem_store32(my + L::kO + c * 32, r);
+          for (int j = 0; j < 32; ++j) {
+            s[j] = __uint_as_float(r0[j]);
+            s[32 + j] = __uint_as_float(r1[j]);
+          }
         }
-        tmem_wait_store();
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      uint32_t w[32];
+        if (at.tile * kSlots + kSlots > at.s.ctx) {  // some slots are new tokens', or past the end
+          const int slot0 = at.tile * kSlots;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        float a = ex2(fmaf(s[2 * j], scale2, -ref)), c = ex2(fmaf(s[2 * j + 1], scale2, -ref));
-        if (scale2 <= 0.f) {  // (a masked score times it is not -inf)
-          a = s[2 * j] == -INFINITY ? 0.f : a;
-          c = s[2 * j + 1] == -INFINITY ? 0.f : c;
+          for (int j = 0; j < kSlots; ++j) {
+            const int back = slot0 + j - at.s.ctx;
+            const bool seen = g.chain ? slot0 + j < view.lim : back < 0 || (back < at.s.n && ((view.bits >> (back & 63)) & 1));
+            if (!seen) s[j] = -INFINITY;
+          }
+          // values that no row uses become zeros
+          const int end = at.s.bad ? 0 : g.end(at.s, at.block), slot = slot0 + (row & 63), back = slot - at.s.ctx;
+          bool out = slot >= end;
+          if (!out && !g.chain && back >= 0) {
+            uint64_t any = 0;
+            const int i0 = (int)((int64_t)at.block * kRows / g.group), i1 = min(at.s.n, (int)(((int64_t)(at.block + 1) * kRows - 1) / g.group) + 1);
+            for (int i = i0; i < i1; ++i) any |= __ldg(p.tree_mask + at.s.off + i);
+            out = !((any >> (back & 63)) & 1);
+          }
+          if (out && row / 64 < L::kHalves) {
+            const uint32_t v = stages + st * L::kStage + L::kKeys + (row / 64) * kSlots * 128 + (row & 63) * 128;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + c * 16), "r"(0) : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        l += a + c;
-        w[j] = pack<T>(a, c);
-      }
-      if (t >= 2) {  // the product that read this buffer's last weights is done
-        ok = __all_sync(0xffffffffu, wait(&bars.output[b], ((t - 2) >> 1) & 1));
-        if (!ok) break;
-      }
-      tmem_store32(my + L::kP + b * (kSlots / 2), w);
-      tmem_wait_store();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars.weights[b]);
+        float mx;
+        if (scale2 > 0.f) {
+          float x[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+          for (int j = 4; j < kSlots; ++j) x[j & 3] = fmaxf(x[j & 3], s[j]);
+          mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * scale2;
+        } else {  // (the largest score is the smallest product)
+          mx = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < kSlots; ++j) mx = fmaxf(mx, s[j] == -INFINITY ? -INFINITY : s[j] * scale2);
+        }
+        // the row's reference grows at its first tile that sees anything, then by 2^8 at least
+        const bool grows = mx > m + kGrowth || (m == -INFINITY && mx > -INFINITY);
+        float by = 1.f;
+        if (grows) {
+          by = ex2(m - mx);
+          m = mx;
+          l *= by;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        uint32_t w[32];
+        if (scale2 > 0.f) {
+          const float2 sc = make_float2(scale2, scale2), nr = make_float2(-ref, -ref);
+          float2 sum[4] = {make_float2(l, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float2 x = __ffma2_rn(make_float2(s[2 * j], s[2 * j + 1]), sc, nr);
+            const float2 e = make_float2(ex2(x.x), ex2(x.y));
+            sum[j & 3] = __fadd2_rn(sum[j & 3], e);
+            w[j] = pack<T>(e.x, e.y);
+          }
+          sum[0] = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
+          l = sum[0].x + sum[0].y;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {  // (a masked score times it is not -inf)
+            const float a = s[2 * j] == -INFINITY ? 0.f : ex2(fmaf(s[2 * j], scale2, -ref));
+            const float c = s[2 * j + 1] == -INFINITY ? 0.f : ex2(fmaf(s[2 * j + 1], scale2, -ref));
+            l += a + c;
+            w[j] = pack<T>(a, c);
+          }
+        }
+        if (t >= 2) {  // the product that read this team's last weights, and added to its output, is done
+          ok = __all_sync(0xffffffffu, wait(&bars.output[team], ((t - 2) >> 1) & 1));
+          if (!ok) break;
+          fence_after();
+        }
+        if (t - 2 >= first_t && __any_sync(0xffffffffu, grows)) {
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t r[32];
+            tmem_load32(r, my_out + c * 32);
+            tmem_wait_load();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * by);
+            tmem_store32(my_out + c * 32, r);
+          }
+        }
+        tmem_store32(my_weights, w);
+        tmem_wait_store();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.weights[team]);
+      } while (false);
+      if (!ok && lane == 0) s_abort = 1;
 
       const bool unit_ends = at.tile + 1 == at.tiles;
+      if (!unit_ends && t + 1 < n) {
+        at.next(p, g);
+        continue;
+      }
+      // The teams' parts of the rows become one; out it goes, or into a slot.
       const Cursor was = at;
       at.next(p, g);
-      if (unit_ends || t + 1 == n) {
-        if (t + 1 < n) take_queries(at);  // (the scores of the unit's last tile are done with the old ones)
-        ok = __all_sync(0xffffffffu, wait(&bars.output[b], (t >> 1) & 1));
-        if (!ok) break;
+      s_m[team][row] = m;
+      s_l[team][row] = nan ? NAN : l;
+      all_rows();
+      if (ok && t + 1 < n) take_queries(at);  // (the scores of the unit's last tile are done with the old ones)
+      bool part_of[2];                  // whether a team had a tile of it
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int tb = t - ((t ^ b) & 1);  // its last tile
+        part_of[b] = tb >= first_t;
+        if (ok && tb >= 0) ok = wait(&bars.output[b], (tb >> 1) & 1);
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok && lane == 0) s_abort = 1;
+      if (ok) {
         fence_after();
         const bool starts = first_tile == 0, whole = unit_ends && starts;
-        const int64_t rr = (int64_t)was.block * kRows + tid;
+        const int64_t rr = (int64_t)was.block * kRows + row;
         const int i = (int)(rr / g.group);
         const bool have = i < was.s.n;
         const int64_t token = was.s.off + i;
         const int head = was.head * g.group + (int)(rr % g.group);
         float* slot = slots.of(blockIdx.x, starts);
-        if (nan) l = NAN;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float m0 = s_m[0][row], m1 = s_m[1][row], M = fmaxf(m0, m1);
+        const float f0 = M == -INFINITY ? 1.f : ex2(m0 - M), f1 = M == -INFINITY ? 1.f : ex2(m1 - M);
+        const float sum = s_l[0][row] * f0 + s_l[1][row] * f1, inv = sum == 0.f ? 0.f : 1.f / sum;
         T* out = static_cast<T*>(p.out) + (have ? token * p.out_tok + head * p.out_head : 0);
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t r[32];
-          tmem_load32(r, my + L::kO + c * 32);
+        for (int x = 0; x < D / 64; ++x) {  // (a team writes half of the columns)
+          const int c = team * (D / 64) + x;
+          uint32_t r0[32], r1[32];
+          tmem_load32(r0, my + L::kO + c * 32);
+          tmem_load32(r1, my + L::kO + D + c * 32);
           tmem_wait_load();
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            v[j] = (part_of[0] ? __uint_as_float(r0[j]) * f0 : 0.f) + (part_of[1] ? __uint_as_float(r1[j]) * f1 : 0.f);
           if (have && !whole) {
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<uint4*>(slot + (size_t)tid * D + c * 32 + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+              *reinterpret_cast<float4*>(slot + (size_t)row * D + c * 32 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           } else if (have) {
 #pragma unroll
             for (int j = 0; j < 32; j += 8) {
               uint32_t h[4];
 #pragma unroll
-              for (int x = 0; x < 4; ++x) h[x] = pack<T>(__uint_as_float(r[j + 2 * x]) * inv, __uint_as_float(r[j + 2 * x + 1]) * inv);
+              for (int y = 0; y < 4; ++y) h[y] = pack<T>(v[j + 2 * y] * inv, v[j + 2 * y + 1] * inv);
               if (c * 32 + j < p.D) *reinterpret_cast<uint4*>(out + c * 32 + j) = make_uint4(h[0], h[1], h[2], h[3]);
             }
           }
           __syncwarp();
         }
-        if (have && !whole) {
-          slot[(size_t)kRows * D + tid] = m;
-          slot[(size_t)kRows * D + kRows + tid] = l;
-        } else if (have && p.lse) {
-          p.lse[token * p.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (team == 0 && have && !whole) {
+          slot[(size_t)kRows * D + row] = M;
+          slot[(size_t)kRows * D + kRows + row] = sum;
+        } else if (team == 0 && have && p.lse) {
+          p.lse[token * p.Hq + head] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
         }
         fence_before();
-        if (tid == 0) {
-          if (nan) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
-          if (starts && !unit_ends)
-            slots.joined[blockIdx.x] = {last_worker(span, blockIdx.x, span.begin + t + was.tiles - was.tile), was.b, was.block, was.head};
-        }
-        fresh = true;
+        if (nan && row == 0) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
+        if (tid == 0 && starts && !unit_ends)
+          slots.joined[blockIdx.x] = {last_worker(span, blockIdx.x, span.begin + t + was.tiles - was.tile), was.b, was.block, was.head};
       }
+      all_rows();  // (outputs, maxima and sums make room for the next unit's)
+      fresh = true;
     }
-    if (!ok && lane == 0) {
-      s_abort = 1;
-      set_status(p.dev_status, STRIDE_DEV_TIMEOUT);
-    }
+    if (!ok && lane == 0) set_status(p.dev_status, STRIDE_DEV_TIMEOUT);
   }
   fence_before();
   __syncthreads();
-  if (warp == 5) {
+  if (warp == kRowWarps + 1) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::kColumns) : "memory");
   }
