@@ -84,6 +84,11 @@ struct Cursor {
     }
     tiles = g.tiles(s, block);
   }
+  // The place `n` tiles on, at most one past the last tile of this unit and head.
+  __device__ __forceinline__ void skip(const AttentionParams& p, const Grouping& g, int n) {
+    tile += n - 1;
+    next(p, g);
+  }
 };
 
 // Sequences' places in the line: line[b] is the number of tiles before sequence b

@@ -3,9 +3,10 @@
 //
 // Blocks of 128 rows by tiles of 64 slots on the tensor cores.  One CTA on an SM
 // takes a share of the line of tiles (attention_line.cuh); its warps:
-//   8     looks up a tile's pages and starts their tensor copies (a box of up to
-//         64 slots by 128 bytes, swizzled), up to five tiles ahead;
-//   9     one thread issues the products: scores Q K^T of the next tile, then
+//   8, 9  look up a tile's pages and start the tensor copies of its keys and its
+//         values (boxes of up to 64 slots by 128 bytes, swizzled), up to five tiles
+//         ahead;
+//   10    one thread issues the products: scores Q K^T of the next tile, then
 //         output += P V of this one (tcgen05, accumulators in tensor memory);
 //   0-7   two teams of a thread for each row, which take the even and the odd
 //         tiles: scores from tensor memory, running maximum and sum, weights P
@@ -34,7 +35,7 @@ namespace {
 constexpr int kRows = 128;
 constexpr int kSlots = 64;
 constexpr int kRowWarps = 8;
-constexpr int kThreads = (kRowWarps + 2) * 32;
+constexpr int kThreads = (kRowWarps + 3) * 32;
 constexpr int kMaxWorkers = 152;
 constexpr float kGrowth = 8.f;  // log2
 
@@ -55,24 +56,35 @@ __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::l
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// One thread of a converged warp; the compiler knows that what it does is uniform.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t x;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(x));
+  return x != 0;
+}
 // The barrier's phase ends when all products issued so far by this thread are done.
 __device__ __forceinline__ void commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
-               "r"(idesc), "r"((uint32_t)add)
-               : "memory");
+// A matrix in shared memory of 128-byte rows, swizzled in groups of eight (1,024
+// bytes apart): the low word of its descriptor, where `next` bytes lie between
+// groups of 64 components (if those are the product's rows); the high word is the
+// same for all.  An address moves on by its bytes / 16.
+__device__ __forceinline__ uint32_t matrix(uint32_t addr, uint32_t next) { return (addr & 0x3ffff) >> 4 | (next >> 4) << 16; }
+constexpr uint32_t kMatrix = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 x, y;\n setp.ne.u32 p, %4, 0;\n mov.b64 x, {%1, %5};\n mov.b64 y, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kMatrix)
+      : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b),
-               "r"(idesc), "r"((uint32_t)add)
-               : "memory");
-}
-// A matrix in shared memory of 128-byte rows, swizzled in groups of eight:
-// `next` bytes lie between 64-component groups (where components are the rows).
-__device__ __forceinline__ uint64_t matrix(uint32_t addr, uint32_t next) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(next >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 y;\n setp.ne.u32 p, %4, 0;\n mov.b64 y, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kMatrix)
+      : "memory");
 }
 // Both operands of type T, 32-bit results of M = 128 by N; b_rows: B's rows, not
 // its columns, run along the summed dimension.
@@ -115,6 +127,19 @@ struct Plan {
   static_assert(kP + kSlots <= kColumns, "tensor memory");
 };
 
+// A place in the ring of stages, and the parity of its barriers' phase.
+template <int kStages>
+struct Place {
+  int st = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void on() {
+    if (++st == kStages) {
+      st = 0;
+      parity ^= 1;
+    }
+  }
+};
+
 struct Barriers {
   uint64_t full[8], empty[8], scores[2], weights[2], output[2], queries, drained;
 };
@@ -128,7 +153,7 @@ struct RowView {
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     attention_many_kernel(const AttentionParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
-                          const int box) {
+                          const int box, const int page_shift) {
   using L = Plan<D>;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -147,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (tid == 0) {
     for (int i = 0; i < L::kStages; ++i) {
-      mbar_init(&bars.full[i], 1);
+      mbar_init(&bars.full[i], 2);
       mbar_init(&bars.empty[i], 1);
       s_lost[i] = 0;
     }
@@ -167,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const Slots slots(p.workspace, gridDim.x, kRows, D);
   if (tid == 0) slots.joined[blockIdx.x] = {0, 0, 0, 0};
   if (span.begin >= span.end) return;  // (all threads alike)
-  if (warp == kRowWarps + 1) {
+  if (warp == kRowWarps + 2) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(L::kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     fence_before();
@@ -175,48 +200,51 @@ __global__ void __launch_bounds__(kThreads, 1)
   Cursor at = place_in_line(p, g, line, span.begin);
   __syncthreads();
   fence_after();
-  const uint32_t tmem = s_tmem;
+  constexpr uint32_t tmem = 0;  // (all columns are this CTA's)
   const int n = (int)(span.end - span.begin);
   // Waits end: after two seconds, or once another warp's wait has run out.
   const auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, kWaitTimeoutNs, &s_abort); };
   bool ok = true;
 
-  if (warp == kRowWarps) {
+  if (warp == kRowWarps || warp == kRowWarps + 1) {
     // ---- copies ----
     const int boxes = kSlots / box;  // of a tile's slots: at most 8, so that a lane has one copy
+    const bool values = warp == kRowWarps + 1;
+    const int bx = lane % boxes, half = lane / boxes;
+    const uint32_t dst = stages + (values ? L::kKeys : 0) + half * kSlots * 128 + bx * box * 128;
+    const CUtensorMap* map = values ? &v_map : &k_map;
+    // The page of this lane's box of a tile, where there is something to read, and its first row there.
+    int32_t page = 0;
+    int row = 0;
+    bool some = false;
+    const auto look_up = [&](const Cursor& u) {
+      const int slot = u.tile * kSlots + bx * box;
+      some = half < L::kHalves && !u.s.bad && slot < g.end(u.s, u.block);
+      if (some) {
+        const int e = page_shift >= 0 ? slot >> page_shift : slot / pc.page_size;
+        row = slot - e * pc.page_size;
+        page = __ldg(pc.block_table + (int64_t)u.b * pc.table_stride + e);
+      }
+    };
+    Place<L::kStages> at_stage;
     int t = 0;
+    look_up(at);
     for (; t < n; ++t) {
-      const int st = t % L::kStages;
+      const bool real = some && page >= 0 && page < pc.n_pages, lost = some && !real;
+      const int now = page, now_row = row, head = at.head;
+      at.next(p, g);
+      if (t + 1 < n) look_up(at);  // (the next tile's, on its way while this one waits for its stage)
       if (t >= L::kStages) {
-        ok = __all_sync(0xffffffffu, wait(&bars.empty[st], (t / L::kStages - 1) & 1));
+        ok = __all_sync(0xffffffffu, wait(&bars.empty[at_stage.st], at_stage.parity ^ 1));
         if (!ok) break;
       }
-      const int end = at.s.bad ? 0 : g.end(at.s, at.block);
-      int32_t page = -1;
-      int row = 0;
-      bool real = false, lost = false;
-      if (lane < boxes) {
-        const int slot = at.tile * kSlots + lane * box;
-        if (slot < end) {
-          const int e = slot / pc.page_size;
-          row = slot - e * pc.page_size;
-          page = __ldg(pc.block_table + (int64_t)at.b * pc.table_stride + e);
-          real = page >= 0 && page < pc.n_pages;
-          lost = !real;
-        }
-      }
+      if (__any_sync(0xffffffffu, lost) && lane == 0) s_lost[at_stage.st] = t + 1;
       const unsigned who = __ballot_sync(0xffffffffu, real);
-      if (__any_sync(0xffffffffu, lost) && lane == 0) s_lost[st] = t + 1;
-      if (lane == 0) mbar_arrive_expect_tx(&bars.full[st], (uint32_t)(__popc(who) * 2 * L::kHalves * box * 128));
+      uint64_t* bar = &bars.full[at_stage.st];
+      if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * box * 128));
       __syncwarp();
-      const int bx = lane % boxes, which = lane / boxes, half = which >> 1;
-      page = __shfl_sync(0xffffffffu, page, bx);
-      row = __shfl_sync(0xffffffffu, row, bx);
-      if (which < 2 * L::kHalves && (who >> bx & 1)) {
-        const uint32_t dst = stages + st * L::kStage + (which & 1) * L::kKeys + half * kSlots * 128 + bx * box * 128;
-        copy_box(dst, which & 1 ? &v_map : &k_map, half * 64, row, at.head, page, &bars.full[st]);
-      }
-      at.next(p, g);
+      if (real) copy_box(dst + at_stage.st * L::kStage, map, half * 64, now_row, head, now, bar);
+      at_stage.on();
     }
     if (!ok) {  // (never seen.  No copy may outlive the CTA: those on their way end, or take their time)
       if (lane == 0) s_abort = 1;
@@ -224,42 +252,46 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int k = t < L::kStages ? 0 : t - L::kStages; k < t; ++k)
         mbar_wait_warp(&bars.full[k % L::kStages], (k / L::kStages) & 1, kWaitTimeoutNs, &go_on);
     }
-  } else if (warp == kRowWarps + 1) {
+  } else if (warp == kRowWarps + 2) {
     // ---- products ----
-    if (lane == 0) {
+    if (elect_one()) {
       constexpr uint32_t qk = product<T>(kSlots, false), pv = product<T>(D, true);
-      Cursor ahead = at;
-      int segment = 0;
-      const auto scores = [&](int t, bool first) {
-        if (first) ok = ok && wait(&bars.queries, segment++ & 1);
-        ok = ok && wait(&bars.full[t % L::kStages], (t / L::kStages) & 1);
+      const uint32_t q = matrix(q_smem, 16), k0 = matrix(stages, 16), v0 = matrix(stages + L::kKeys, kSlots * 128);
+      Place<L::kStages> ahead, here;  // of the scores, of the output
+      uint32_t team_ahead = 0, team = 0, weights_parity = 0, queries_parity = 0;
+      const auto scores = [&] {
+        ok = wait(&bars.full[ahead.st], ahead.parity);
         if (!ok) return;
         fence_after();
-        const uint32_t k = stages + (t % L::kStages) * L::kStage;
+        const uint32_t k = k0 + ahead.st * (L::kStage >> 4), d = tmem + team_ahead * kSlots;
 #pragma unroll
         for (int x = 0; x < D / 16; ++x)
-          mma_ss(tmem + (t & 1) * kSlots, matrix(q_smem + (x / 4) * kRows * 128 + (x % 4) * 32, 16),
-                 matrix(k + (x / 4) * kSlots * 128 + (x % 4) * 32, 16), qk, x > 0);
-        commit(&bars.scores[t & 1]);
+          mma_ss(d, q + (x / 4) * (kRows * 128 >> 4) + (x % 4) * 2, k + (x / 4) * (kSlots * 128 >> 4) + (x % 4) * 2, qk, x > 0);
+        commit(&bars.scores[team_ahead]);
+        team_ahead ^= 1;
+        ahead.on();
       };
-      scores(0, true);
-      unsigned begun = 0;  // teams (bits) whose output holds something of the unit
-      for (int t = 0; t < n && ok; ++t) {
-        const bool last = ahead.tile + 1 == ahead.tiles;  // of its unit
-        ahead.next(p, g);
-        if (t + 1 < n && !last) scores(t + 1, false);
-        ok = ok && wait(&bars.weights[t & 1], (t >> 1) & 1);
-        if (!ok) break;
-        fence_after();
-        const uint32_t v = stages + (t % L::kStages) * L::kStage + L::kKeys;
+      for (int left = n; left > 0 && ok;) {
+        const int len = min(left, at.tiles - at.tile);  // of the unit, in this share
+        left -= len;
+        ok = wait(&bars.queries, queries_parity);
+        queries_parity ^= 1;
+        if (ok) scores();
+        for (int u = 0; u < len && ok; ++u) {
+          if (u + 1 < len) scores();
+          ok = ok && wait(&bars.weights[team], weights_parity);
+          if (!ok) break;
+          fence_after();
+          const uint32_t v = v0 + here.st * (L::kStage >> 4), d = tmem + L::kO + team * D, w = tmem + L::kP + team * (kSlots / 2);
 #pragma unroll
-        for (int x = 0; x < kSlots / 16; ++x)
-          mma_ts(tmem + L::kO + (t & 1) * D, tmem + L::kP + (t & 1) * (kSlots / 2) + x * 8, matrix(v + x * 16 * 128, kSlots * 128), pv,
-                 x > 0 || (begun >> (t & 1) & 1));
-        commit(&bars.empty[t % L::kStages]);
-        commit(&bars.output[t & 1]);
-        begun = last ? 0 : begun | 1u << (t & 1);
-        if (t + 1 < n && last) scores(t + 1, true);
+          for (int x = 0; x < kSlots / 16; ++x) mma_ts(d, w + x * 8, v + x * (16 * 128 >> 4), pv, x > 0 || u >= 2);
+          commit(&bars.empty[here.st]);
+          commit(&bars.output[team]);
+          here.on();
+          weights_parity ^= team;
+          team ^= 1;
+        }
+        at.skip(p, g, len);
       }
       if (!ok) {
         s_abort = 1;
@@ -278,7 +310,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     RowView view = {0, 0};
     float m = -INFINITY, l = 0.f;
     bool nan = false;
-    int first_tile = 0, first_t = 0;  // of the unit in this share
     const auto all_rows = [&] { asm volatile("bar.sync 1, %0;" ::"n"(kRowWarps * 32) : "memory"); };
     // This thread's row of a unit's queries into shared memory (a team takes half of the columns).
     const auto take_queries = [&](const Cursor& u) {
@@ -300,28 +331,31 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(&bars.queries);
     };
     take_queries(at);
-    bool fresh = true;
-    for (int t = 0; t < n; ++t) {
-      if (fresh) {
-        fresh = false;
-        m = -INFINITY;
-        l = 0.f;
-        nan = at.s.bad;
-        first_tile = at.tile;
-        first_t = t;
+    Place<L::kStages> at_stage;       // of this team's next tile
+    if (team == 1) at_stage.on();
+    uint32_t parity = 0;              // of this team's scores, weights and output
+    bool any_yet = false;             // this team has had a tile
+    for (int t0 = 0; t0 < n;) {       // a unit, or what of it falls to this share
+      const int len = min(n - t0, at.tiles - at.tile), first_tile = at.tile;
+      const bool unit_ends = at.tile + len == at.tiles;
+      const int first_u = (t0 ^ team) & 1;  // this team's first tile of it
+      m = -INFINITY;
+      l = 0.f;
+      nan = at.s.bad;
+      {
         const int i = (int)(((int64_t)at.block * kRows + row) / g.group);
         const bool have = i < at.s.n;
         view.lim = at.s.ctx + (have ? i + 1 : 0);
         view.bits = have && !g.chain ? __ldg(p.tree_mask + at.s.off + i) : 0;
       }
       // (a warp whose wait has run out goes on without waiting, to the barriers that the others are at)
-      if (ok && (t & 1) == team) do {
-        const int st = t % L::kStages;
-        ok = wait(&bars.full[st], (t / L::kStages) & 1) && wait(&bars.scores[team], (t >> 1) & 1);
+      for (int u = first_u; u < len && ok; u += 2) {
+        const int st = at_stage.st;
+        ok = wait(&bars.full[st], at_stage.parity) && wait(&bars.scores[team], parity);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
-        nan |= s_lost[st] == t + 1;
+        nan |= s_lost[st] == t0 + u + 1;
         float s[kSlots];
         {
           uint32_t r0[32], r1[32];
@@ -334,8 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             s[32 + j] = __uint_as_float(r1[j]);
           }
         }
-        if (at.tile * kSlots + kSlots > at.s.ctx) {  // some slots are new tokens', or past the end
-          const int slot0 = at.tile * kSlots;
+        const int slot0 = (first_tile + u) * kSlots;
+        if (slot0 + kSlots > at.s.ctx) {  // some slots are new tokens', or past the end
 #pragma unroll
           for (int j = 0; j < kSlots; ++j) {
             const int back = slot0 + j - at.s.ctx;
@@ -400,12 +434,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             w[j] = pack<T>(a, c);
           }
         }
-        if (t >= 2) {  // the product that read this team's last weights, and added to its output, is done
-          ok = __all_sync(0xffffffffu, wait(&bars.output[team], ((t - 2) >> 1) & 1));
+        if (any_yet) {  // the product that read this team's last weights, and added to its output, is done
+          ok = __all_sync(0xffffffffu, wait(&bars.output[team], parity ^ 1));
           if (!ok) break;
           fence_after();
         }
-        if (t - 2 >= first_t && __any_sync(0xffffffffu, grows)) {
+        if (u >= 2 && __any_sync(0xffffffffu, grows)) {
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
             uint32_t r[32];
@@ -421,27 +455,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.weights[team]);
-      } while (false);
+        any_yet = true;
+        parity ^= 1;
+        at_stage.on();
+        at_stage.on();
+      }
       if (!ok && lane == 0) s_abort = 1;
 
-      const bool unit_ends = at.tile + 1 == at.tiles;
-      if (!unit_ends && t + 1 < n) {
-        at.next(p, g);
-        continue;
-      }
       // The teams' parts of the rows become one; out it goes, or into a slot.
       const Cursor was = at;
-      at.next(p, g);
+      at.skip(p, g, len);
       s_m[team][row] = m;
       s_l[team][row] = nan ? NAN : l;
       all_rows();
-      if (ok && t + 1 < n) take_queries(at);  // (the scores of the unit's last tile are done with the old ones)
-      bool part_of[2];                  // whether a team had a tile of it
+      if (ok && t0 + len < n) take_queries(at);  // (the scores of the unit's last tile are done with the old ones)
+      const int last = t0 + len - 1;
+      bool part_of[2];  // whether a team had a tile of it
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int tb = t - ((t ^ b) & 1);  // its last tile
-        part_of[b] = tb >= first_t;
-        if (ok && tb >= 0) ok = wait(&bars.output[b], (tb >> 1) & 1);
+        const int tb = last - ((last ^ b) & 1);  // its last tile
+        part_of[b] = tb >= t0;
+        if (ok && part_of[b]) ok = wait(&bars.output[b], (tb >> 1) & 1);
       }
       ok = __all_sync(0xffffffffu, ok);
       if (!ok && lane == 0) s_abort = 1;
@@ -493,16 +527,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before();
         if (nan && row == 0) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
         if (tid == 0 && starts && !unit_ends)
-          slots.joined[blockIdx.x] = {last_worker(span, blockIdx.x, span.begin + t + was.tiles - was.tile), was.b, was.block, was.head};
+          slots.joined[blockIdx.x] = {last_worker(span, blockIdx.x, span.begin + t0 + was.tiles - was.tile), was.b, was.block, was.head};
       }
       all_rows();  // (outputs, maxima and sums make room for the next unit's)
-      fresh = true;
+      t0 += len;
     }
     if (!ok && lane == 0) set_status(p.dev_status, STRIDE_DEV_TIMEOUT);
   }
   fence_before();
   __syncthreads();
-  if (warp == kRowWarps + 1) {
+  if (warp == kRowWarps + 2) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::kColumns) : "memory");
   }
@@ -540,6 +574,12 @@ bool describe(CUtensorMap* map, const void* base, const AttentionParams& p, int 
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+int page_shift(int page_size) {  // -1: not a power of two
+  for (int k = 0; k < 31; ++k)
+    if (page_size == 1 << k) return k;
+  return -1;
+}
+
 int slots_of_a_box(int page_size) {
   int box = kSlots;
   while (box > 1 && page_size % box != 0) box /= 2;
@@ -566,7 +606,7 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kern, p, k_map, v_map, box);
+  e = cudaLaunchKernelEx(&cfg, kern, p, k_map, v_map, box, page_shift(p.cache.page_size));
   if (e != cudaSuccess) return e;
   if (p.cache.table_stride * p.cache.page_size <= kSlots) return cudaGetLastError();  // (no unit has two tiles)
   return launch_attention_join(p, dtype, grid, kRows, stream);
