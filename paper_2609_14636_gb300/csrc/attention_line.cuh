@@ -68,7 +68,13 @@ struct Grouping {
 // A place in the line.
 struct Cursor {
   int32_t b, block, head, tile, tiles;
+  int32_t end;  // one past the last slot that the block's rows may see; 0 where the sequence is bad
   Seq s;
+
+  __device__ __forceinline__ void enter(const Grouping& g) {
+    end = s.bad ? 0 : g.end(s, block);
+    tiles = s.bad ? 1 : (end + g.tile - 1) / g.tile;
+  }
 
   __device__ __forceinline__ void next(const AttentionParams& p, const Grouping& g) {
     if (++tile < tiles) return;
@@ -82,7 +88,7 @@ struct Cursor {
         s = sequence(p, b);
       } while (s.n == 0);
     }
-    tiles = g.tiles(s, block);
+    enter(g);
   }
   // The place `n` tiles on, at most one past the last tile of this unit and head.
   __device__ __forceinline__ void skip(const AttentionParams& p, const Grouping& g, int n) {
@@ -168,7 +174,7 @@ __device__ __forceinline__ Cursor place_in_line(const AttentionParams& p, const 
   c.s = sequence(p, c.b);
   c.block = 0;
   while (true) {
-    c.tiles = g.tiles(c.s, c.block);
+    c.enter(g);
     const int64_t of_block = (int64_t)c.tiles * p.cache.n_heads;
     if (inside < of_block) break;
     inside -= of_block;
@@ -231,7 +237,16 @@ cudaError_t launch_attention_many(const AttentionParams& p, int dtype, int sms, 
 bool attention_many_takes(const AttentionParams& p);
 size_t attention_few_bytes(int D);
 size_t attention_many_bytes(int D);
-// Joins the cut units of a kernel of `workers` workers and blocks of `rows` rows.
-cudaError_t launch_attention_join(const AttentionParams& p, int dtype, int workers, int rows, cudaStream_t stream);
+// Joins the cut units of a kernel of `workers` workers and blocks of `rows` rows,
+// each with so many CTAs.
+cudaError_t launch_attention_join(const AttentionParams& p, int dtype, int workers, int rows, int ctas, cudaStream_t stream);
+
+// No call's line is longer (sequences are as long as the block table holds).
+inline int64_t most_tiles(const AttentionParams& p, int rows, int tile) {
+  const int64_t group = p.Hq / p.cache.n_heads, blocks = p.cache.n_seqs + p.n_tokens * group / rows;
+  const int64_t slots = p.cache.table_stride * (int64_t)p.cache.page_size, most = INT64_MAX / 4;
+  const int64_t per = slots > most / p.cache.n_heads ? most : ((slots + tile - 1) / tile) * p.cache.n_heads;
+  return per > most / blocks ? most : per * blocks;
+}
 
 }  // namespace stride

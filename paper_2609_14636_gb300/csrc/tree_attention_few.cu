@@ -13,6 +13,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "attention_line.cuh"
 #include "mbarrier.cuh"
 
@@ -96,8 +98,8 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_k
   const int row_chunks = p.D / 8;  // 16-byte chunks of a key or a value
   // Starts the copies of a tile; true where a slot has no page.
   const auto load = [&](const Cursor& u, int stage) {
-    const int end = u.s.bad ? 0 : g.end(u.s, u.block), slot = u.tile * kSlots + lane;
-    bool real = slot < end;
+    const int slot = u.tile * kSlots + lane;
+    bool real = slot < u.end;
     if (!g.chain && slot >= u.s.ctx && real) {  // a new token that no row of the unit sees is left out
       uint64_t seen = 0;
       const int i0 = u.block * kRows / g.group, i1 = min(u.s.n, ((u.block + 1) * kRows - 1) / g.group + 1);
@@ -314,8 +316,8 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)R::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  int grid = sms * (D == 128 ? 1 : 2);
-  if (grid > kMaxWorkers / kWarps) grid = kMaxWorkers / kWarps;
+  const int64_t need = (most_tiles(p, kRows, kSlots) + kWarps - 1) / kWarps;
+  const int grid = (int)std::min<int64_t>(std::min(sms * (D == 128 ? 1 : 2), kMaxWorkers / kWarps), need);
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = R::kSmem;
@@ -331,7 +333,7 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   e = cudaLaunchKernelEx(&cfg, kern, p, shift);
   if (e != cudaSuccess) return e;
   if (p.cache.table_stride * p.cache.page_size <= kSlots) return cudaGetLastError();  // (no unit has two tiles)
-  return launch_attention_join(p, dtype, grid * kWarps, kRows, stream);
+  return launch_attention_join(p, dtype, grid * kWarps, kRows, 4, stream);
 }
 
 }  // namespace

@@ -4,10 +4,12 @@
 // Blocks of 128 rows by tiles of 64 slots on the tensor cores.  One CTA on an SM
 // takes a share of the line of tiles (attention_line.cuh); its warps:
 //   8, 9  look up a tile's pages and start the tensor copies of its keys and its
-//         values (boxes of up to 64 slots by 128 bytes, swizzled), up to five tiles
+//         values (boxes of up to 64 slots by 128 bytes, swizzled), up to six tiles
 //         ahead;
 //   10    one thread issues the products: scores Q K^T of the next tile, then
 //         output += P V of this one (tcgen05, accumulators in tensor memory);
+//         The queries are an operand in tensor memory too: read from shared memory
+//         for each tile they took more of its bandwidth than the keys;
 //   0-7   two teams of a thread for each row, which take the even and the odd
 //         tiles: scores from tensor memory, running maximum and sum, weights P
 //         back into tensor memory, where the second product reads them.  Each
@@ -23,6 +25,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -52,6 +55,13 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) { tmem_store32(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -72,13 +82,6 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
 // same for all.  An address moves on by its bytes / 16.
 __device__ __forceinline__ uint32_t matrix(uint32_t addr, uint32_t next) { return (addr & 0x3ffff) >> 4 | (next >> 4) << 16; }
 constexpr uint32_t kMatrix = (1024 >> 4) | 1u << 14 | 2u << 29;
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
-  asm volatile(
-      "{\n .reg .pred p;\n .reg .b64 x, y;\n setp.ne.u32 p, %4, 0;\n mov.b64 x, {%1, %5};\n mov.b64 y, {%2, %5};\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d),
-      "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kMatrix)
-      : "memory");
-}
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
   asm volatile(
       "{\n .reg .pred p;\n .reg .b64 y;\n setp.ne.u32 p, %4, 0;\n mov.b64 y, {%2, %5};\n"
@@ -117,14 +120,13 @@ __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi) {
 template <int D>
 struct Plan {
   static constexpr int kHalves = D / 64;                    // 128-byte column groups of a row
-  static constexpr int kQ = kHalves * kRows * 128;          // bytes
-  static constexpr int kKeys = kHalves * kSlots * 128;
+  static constexpr int kKeys = kHalves * kSlots * 128;      // bytes
   static constexpr int kStage = 2 * kKeys;                  // keys, then values
-  static constexpr int kStages = 5;
-  static constexpr size_t kSmem = kQ + (size_t)kStages * kStage + 1024;  // (the base rounded up to 1,024)
-  // columns of tensor memory: scores, outputs, weights of the two teams
-  static constexpr int kO = 2 * kSlots, kP = kO + 2 * D, kColumns = 512;
-  static_assert(kP + kSlots <= kColumns, "tensor memory");
+  static constexpr int kStages = 6;
+  static constexpr size_t kSmem = (size_t)kStages * kStage + 1024;  // (the base rounded up to 1,024)
+  // columns of tensor memory: scores, outputs, weights of the two teams; queries
+  static constexpr int kO = 2 * kSlots, kP = kO + 2 * D, kQ = kP + kSlots, kColumns = 512;
+  static_assert(kQ + D / 2 <= kColumns, "tensor memory");
 };
 
 // A place in the ring of stages, and the parity of its barriers' phase.
@@ -168,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const Grouping g = {p.Hq / p.cache.n_heads, kRows, kSlots, p.tree_mask == nullptr};
   const PagedCache& pc = p.cache;
-  const uint32_t q_smem = (smem_u32(dyn) + 1023) & ~1023u, stages = q_smem + L::kQ;
+  const uint32_t stages = (smem_u32(dyn) + 1023) & ~1023u;
 
   if (tid == 0) {
     for (int i = 0; i < L::kStages; ++i) {
@@ -210,8 +212,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- copies ----
     const int boxes = kSlots / box;  // of a tile's slots: at most 8, so that a lane has one copy
     const bool values = warp == kRowWarps + 1;
-    const int bx = lane % boxes, half = lane / boxes;
-    const uint32_t dst = stages + (values ? L::kKeys : 0) + half * kSlots * 128 + bx * box * 128;
+    const int bx = lane & (boxes - 1);  // (a lane looks up a box; lanes past the last repeat the first ones')
+    const uint32_t dst = stages + (values ? L::kKeys : 0);
     const CUtensorMap* map = values ? &v_map : &k_map;
     // The page of this lane's box of a tile, where there is something to read, and its first row there.
     int32_t page = 0;
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool some = false;
     const auto look_up = [&](const Cursor& u) {
       const int slot = u.tile * kSlots + bx * box;
-      some = half < L::kHalves && !u.s.bad && slot < g.end(u.s, u.block);
+      some = slot < u.end;
       if (some) {
         const int e = page_shift >= 0 ? slot >> page_shift : slot / pc.page_size;
         row = slot - e * pc.page_size;
@@ -239,11 +241,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
       }
       if (__any_sync(0xffffffffu, lost) && lane == 0) s_lost[at_stage.st] = t + 1;
-      const unsigned who = __ballot_sync(0xffffffffu, real);
-      uint64_t* bar = &bars.full[at_stage.st];
-      if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * box * 128));
+      const unsigned who = __ballot_sync(0xffffffffu, real) & ((1u << boxes) - 1);
+      int pages[8], rows[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        pages[x] = __shfl_sync(0xffffffffu, now, x);
+        rows[x] = __shfl_sync(0xffffffffu, now_row, x);
+      }
+      if (elect_one()) {
+        uint64_t* bar = &bars.full[at_stage.st];
+        const uint32_t to = dst + at_stage.st * L::kStage;
+        mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * L::kHalves * box * 128));
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (who >> x & 1)
+#pragma unroll
+            for (int half = 0; half < L::kHalves; ++half)
+              copy_box(to + half * kSlots * 128 + x * box * 128, map, half * 64, rows[x], head, pages[x], bar);
+      }
       __syncwarp();
-      if (real) copy_box(dst + at_stage.st * L::kStage, map, half * 64, now_row, head, now, bar);
       at_stage.on();
     }
     if (!ok) {  // (never seen.  No copy may outlive the CTA: those on their way end, or take their time)
@@ -256,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- products ----
     if (elect_one()) {
       constexpr uint32_t qk = product<T>(kSlots, false), pv = product<T>(D, true);
-      const uint32_t q = matrix(q_smem, 16), k0 = matrix(stages, 16), v0 = matrix(stages + L::kKeys, kSlots * 128);
+      const uint32_t k0 = matrix(stages, 16), v0 = matrix(stages + L::kKeys, kSlots * 128);
       Place<L::kStages> ahead, here;  // of the scores, of the output
       uint32_t team_ahead = 0, team = 0, weights_parity = 0, queries_parity = 0;
       const auto scores = [&] {
@@ -266,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t k = k0 + ahead.st * (L::kStage >> 4), d = tmem + team_ahead * kSlots;
 #pragma unroll
         for (int x = 0; x < D / 16; ++x)
-          mma_ss(d, q + (x / 4) * (kRows * 128 >> 4) + (x % 4) * 2, k + (x / 4) * (kSlots * 128 >> 4) + (x % 4) * 2, qk, x > 0);
+          mma_ts(d, tmem + L::kQ + x * 8, k + (x / 4) * (kSlots * 128 >> 4) + (x % 4) * 2, qk, x > 0);
         commit(&bars.scores[team_ahead]);
         team_ahead ^= 1;
         ahead.on();
@@ -311,22 +327,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     float m = -INFINITY, l = 0.f;
     bool nan = false;
     const auto all_rows = [&] { asm volatile("bar.sync 1, %0;" ::"n"(kRowWarps * 32) : "memory"); };
-    // This thread's row of a unit's queries into shared memory (a team takes half of the columns).
+    // This thread's row of a unit's queries into tensor memory (a team takes half of the columns).
     const auto take_queries = [&](const Cursor& u) {
       const int64_t rr = (int64_t)u.block * kRows + row;
       const int i = (int)(rr / g.group);
       const bool have = i < u.s.n;
       const T* q = static_cast<const T*>(p.q) + (u.s.off + (have ? i : 0)) * p.q_tok + (u.head * g.group + rr % g.group) * p.q_head;
+      uint32_t x[D / 4];
 #pragma unroll
-      for (int x = 0; x < D / 16; ++x) {
-        const int c = team * (D / 16) + x;
+      for (int c = 0; c < D / 16; ++c) {
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (have && c * 8 < p.D) v = *reinterpret_cast<const uint4*>(q + c * 8);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + (c / 8) * kRows * 128 + row * 128 + (((c % 8) ^ (row & 7)) << 4)),
-                     "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-                     : "memory");
+        const int col = team * (D / 2) + c * 8;
+        if (have && col < p.D) v = *reinterpret_cast<const uint4*>(q + col);
+        x[4 * c] = v.x;
+        x[4 * c + 1] = v.y;
+        x[4 * c + 2] = v.z;
+        x[4 * c + 3] = v.w;
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      tmem_store(my + L::kQ + team * (D / 4), x);
+      tmem_wait_store();
+      fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars.queries);
     };
@@ -377,8 +398,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!seen) s[j] = -INFINITY;
           }
           // values that no row uses become zeros
-          const int end = at.s.bad ? 0 : g.end(at.s, at.block), slot = slot0 + (row & 63), back = slot - at.s.ctx;
-          bool out = slot >= end;
+          const int slot = slot0 + (row & 63), back = slot - at.s.ctx;
+          bool out = slot >= at.end;
           if (!out && !g.chain && back >= 0) {
             uint64_t any = 0;
             const int i0 = (int)((int64_t)at.block * kRows / g.group), i1 = min(at.s.n, (int)(((int64_t)(at.block + 1) * kRows - 1) / g.group) + 1);
@@ -596,7 +617,7 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  const int grid = sms < kMaxWorkers ? sms : kMaxWorkers;
+  const int grid = (int)std::min<int64_t>(std::min(sms, kMaxWorkers), most_tiles(p, kRows, kSlots));
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = L::kSmem;
@@ -609,7 +630,7 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   e = cudaLaunchKernelEx(&cfg, kern, p, k_map, v_map, box, page_shift(p.cache.page_size));
   if (e != cudaSuccess) return e;
   if (p.cache.table_stride * p.cache.page_size <= kSlots) return cudaGetLastError();  // (no unit has two tiles)
-  return launch_attention_join(p, dtype, grid, kRows, stream);
+  return launch_attention_join(p, dtype, grid, kRows, 16, stream);
 }
 
 }  // namespace
