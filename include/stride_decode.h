@@ -153,7 +153,8 @@ STRIDE_API size_t stride_tree_attention_workspace_size(int64_t n_tokens, int32_t
  * out 0, lse -inf.  A slot without a page: STRIDE_DEV_BAD_LAYOUT and NaN rows.
  *
  * Types BF16, F16; D a multiple of 8, at most STRIDE_MAX_ATTENTION_DIM; the caches' base and strides whole 16-byte
- * vectors (q and out too).  lse: float [n_tokens, n_heads] or NULL. */
+ * vectors (q and out too); n_tokens times the group of query heads under 2^31 -
+ * 256.  lse: float [n_tokens, n_heads] or NULL. */
 STRIDE_API int stride_tree_attention(const stride_head_rows* q, const stride_head_rows* out, float* lse,
                                      int32_t dtype, int64_t n_tokens, int32_t D, float scale,
                                      const uint64_t* tree_mask, const stride_paged_cache* cache,

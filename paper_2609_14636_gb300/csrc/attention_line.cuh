@@ -44,14 +44,13 @@ __device__ __forceinline__ Seq sequence(const AttentionParams& p, int b) {
 // How rows and slots are grouped: row = token * group + head within the kv
 // head's query heads.
 struct Grouping {
-  int32_t group, rows, tile;  // query heads per kv head, rows of a block, slots of a tile
+  int32_t group, rows, tile;  // query heads per kv head, rows of a block, slots of a tile (n * group fits in 31 bits with room)
   bool chain;                 // no tree mask: each token sees the new ones up to itself
-  __device__ __forceinline__ int blocks(const Seq& s) const { return (int)(((int64_t)s.n * group + rows - 1) / rows); }
+  __device__ __forceinline__ int blocks(const Seq& s) const { return (s.n * group + rows - 1) / rows; }
   // One past the last slot that a block's rows may see.
   __device__ __forceinline__ int end(const Seq& s, int block) const {
     if (!chain) return s.ctx + s.n;
-    const int64_t last = min((int64_t)(block + 1) * rows, (int64_t)s.n * group) - 1;
-    return s.ctx + (int)(last / group) + 1;
+    return s.ctx + (min((block + 1) * rows, s.n * group) - 1) / group + 1;
   }
   __device__ __forceinline__ int tiles(const Seq& s, int block) const { return s.bad ? 1 : (end(s, block) + tile - 1) / tile; }
   // The tiles of one head of all blocks.

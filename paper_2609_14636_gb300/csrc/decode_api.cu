@@ -224,6 +224,7 @@ int stride_tree_attention(const stride_head_rows* q, const stride_head_rows* out
   if (!Q.valid(n_tokens) || !O.valid(n_tokens) || Q.r.n_heads < 1 || O.r.n_heads != Q.r.n_heads || Q.r.n_heads % cache->n_heads != 0)
     return STRIDE_ERR_INVALID_ARG;
   if (!Q.whole(n_tokens, 8, 2) || !O.whole(n_tokens, 8, 2) || !cache_whole(*cache, 8, 2)) return STRIDE_ERR_INVALID_ARG;
+  if (n_tokens * (Q.r.n_heads / cache->n_heads) > INT32_MAX - 256) return STRIDE_ERR_INVALID_ARG;
   if (n_tokens == 0) return STRIDE_OK;
   if (!workspace || workspace_bytes < attention_workspace_bytes(n_tokens, Q.r.n_heads, cache->n_heads, D) || !multiple(workspace, 256))
     return STRIDE_ERR_WORKSPACE;

@@ -6,10 +6,11 @@
 //   8, 9  look up a tile's pages and start the tensor copies of its keys and its
 //         values (boxes of up to 64 slots by 128 bytes, swizzled), up to six tiles
 //         ahead;
-//   10    one thread issues the products: scores Q K^T of the next tile, then
-//         output += P V of this one (tcgen05, accumulators in tensor memory);
-//         The queries are an operand in tensor memory too: read from shared memory
-//         for each tile they took more of its bandwidth than the keys;
+//   10    one thread issues the products: scores Q K^T two tiles ahead, as soon as
+//         their place is free, and output += P V (tcgen05, accumulators in tensor
+//         memory).  The queries are an operand in tensor memory too: read from
+//         shared memory for each tile they took more of its bandwidth than the
+//         keys;
 //   0-7   two teams of a thread for each row, which take the even and the odd
 //         tiles: scores from tensor memory, running maximum and sum, weights P
 //         back into tensor memory, where the second product reads them.  Each
@@ -71,6 +72,12 @@ __device__ __forceinline__ bool elect_one() {
   uint32_t x;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(x));
   return x != 0;
+}
+// 32 bytes at once (a thread has a row: each store takes the lines of 32 rows).
+__device__ __forceinline__ void store32(float* p, const float* v) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]),
+               "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
 }
 // The barrier's phase ends when all products issued so far by this thread are done.
 __device__ __forceinline__ void commit(uint64_t* bar) {
@@ -143,7 +150,7 @@ struct Place {
 };
 
 struct Barriers {
-  uint64_t full[8], empty[8], scores[2], weights[2], output[2], queries, drained;
+  uint64_t full[8], empty[8], scores[2], taken[2], weights[2], output[2], queries, drained;
 };
 
 // What the rows of a unit's block see of its tiles.
@@ -180,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.scores[i], 1);
+      mbar_init(&bars.taken[i], 4);
       mbar_init(&bars.weights[i], 4);
       mbar_init(&bars.output[i], 1);
     }
@@ -293,8 +301,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = wait(&bars.queries, queries_parity);
         queries_parity ^= 1;
         if (ok) scores();
+        if (ok && len > 1) scores();
         for (int u = 0; u < len && ok; ++u) {
-          if (u + 1 < len) scores();
+          if (u + 2 < len) {  // the team's next scores, as soon as it has these
+            ok = wait(&bars.taken[team], weights_parity);
+            if (!ok) break;
+            scores();
+          }
           ok = ok && wait(&bars.weights[team], weights_parity);
           if (!ok) break;
           fence_after();
@@ -327,18 +340,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     float m = -INFINITY, l = 0.f;
     bool nan = false;
     const auto all_rows = [&] { asm volatile("bar.sync 1, %0;" ::"n"(kRowWarps * 32) : "memory"); };
+    // Row `row` of a unit's block: token of the sequence, query head.
+    const auto token_of = [&](const Cursor& u) { return (int)((uint32_t)(u.block * kRows + row) / (uint32_t)g.group); };
     // This thread's row of a unit's queries into tensor memory (a team takes half of the columns).
     const auto take_queries = [&](const Cursor& u) {
-      const int64_t rr = (int64_t)u.block * kRows + row;
-      const int i = (int)(rr / g.group);
+      const int i = token_of(u);
       const bool have = i < u.s.n;
-      const T* q = static_cast<const T*>(p.q) + (u.s.off + (have ? i : 0)) * p.q_tok + (u.head * g.group + rr % g.group) * p.q_head;
+      const T* q = static_cast<const T*>(p.q) + (u.s.off + (have ? i : 0)) * p.q_tok + (u.head * g.group + u.block * kRows + row - i * g.group) * p.q_head;
       uint32_t x[D / 4];
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         uint4 v = make_uint4(0, 0, 0, 0);
         const int col = team * (D / 2) + c * 8;
-        if (have && col < p.D) v = *reinterpret_cast<const uint4*>(q + col);
+        if (have && col < p.D) v = __ldg(reinterpret_cast<const uint4*>(q + col));
         x[4 * c] = v.x;
         x[4 * c + 1] = v.y;
         x[4 * c + 2] = v.z;
@@ -364,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       l = 0.f;
       nan = at.s.bad;
       {
-        const int i = (int)(((int64_t)at.block * kRows + row) / g.group);
+        const int i = token_of(at);
         const bool have = i < at.s.n;
         view.lim = at.s.ctx + (have ? i + 1 : 0);
         view.bits = have && !g.chain ? __ldg(p.tree_mask + at.s.off + i) : 0;
@@ -383,6 +397,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_load32(r0, my_scores);
           tmem_load32(r1, my_scores + 32);
           tmem_wait_load();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars.taken[team]);
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             s[j] = __uint_as_float(r0[j]);
@@ -402,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           bool out = slot >= at.end;
           if (!out && !g.chain && back >= 0) {
             uint64_t any = 0;
-            const int i0 = (int)((int64_t)at.block * kRows / g.group), i1 = min(at.s.n, (int)(((int64_t)(at.block + 1) * kRows - 1) / g.group) + 1);
+            const int i0 = at.block * kRows / g.group, i1 = min(at.s.n, ((at.block + 1) * kRows - 1) / g.group + 1);
             for (int i = i0; i < i1; ++i) any |= __ldg(p.tree_mask + at.s.off + i);
             out = !((any >> (back & 63)) & 1);
           }
@@ -503,11 +520,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok) {
         fence_after();
         const bool starts = first_tile == 0, whole = unit_ends && starts;
-        const int64_t rr = (int64_t)was.block * kRows + row;
-        const int i = (int)(rr / g.group);
+        const int i = token_of(was);
         const bool have = i < was.s.n;
         const int64_t token = was.s.off + i;
-        const int head = was.head * g.group + (int)(rr % g.group);
+        const int head = was.head * g.group + was.block * kRows + row - i * g.group;
         float* slot = slots.of(blockIdx.x, starts);
         const float m0 = s_m[0][row], m1 = s_m[1][row], M = fmaxf(m0, m1);
         const float f0 = M == -INFINITY ? 1.f : ex2(m0 - M), f1 = M == -INFINITY ? 1.f : ex2(m1 - M);
@@ -526,8 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             v[j] = (part_of[0] ? __uint_as_float(r0[j]) * f0 : 0.f) + (part_of[1] ? __uint_as_float(r1[j]) * f1 : 0.f);
           if (have && !whole) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<float4*>(slot + (size_t)row * D + c * 32 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < 32; j += 8) store32(slot + (size_t)row * D + c * 32 + j, v + j);
           } else if (have) {
 #pragma unroll
             for (int j = 0; j < 32; j += 8) {
