@@ -4,7 +4,9 @@
 // A unit is a sequence, a block of its rows (new tokens times the query heads of
 // one key/value head) and a kv head; its tiles are runs of slots.  The units'
 // tiles, one unit after the other, form a line, of which every worker (a warp or
-// a CTA) takes an equal share whatever the sequences' lengths.  Where a unit is
+// a CTA) takes an equal share whatever the sequences' lengths: of the line's cost,
+// where a unit counts as some tiles more than it has for what it takes to start
+// and to end it (`extra`; a share has at least one tile).  Where a unit is
 // cut between workers each leaves its part (largest score, sum, unnormalised
 // output, in 32 bits) in a slot of the workspace, and the worker where it starts
 // leaves a Joined record for the kernel that joins them, in the line's order.
@@ -96,106 +98,167 @@ struct Cursor {
   }
 };
 
-// Sequences' places in the line: line[b] is the number of tiles before sequence b
-// + 1 (all heads), for the first kLineSeqs.  Returns the line's length; called by
-// all of a CTA's threads, whose warps' sums pass through part.
+// Sequences' places in the line: the tiles and the units before sequence b + 1,
+// for the first kLineSeqs, and the line's length.
+struct Line {
+  int64_t tiles[kLineSeqs];
+  int32_t units[kLineSeqs];
+  int64_t part_tiles[32];
+  int64_t part_units[32];
+};
+struct Length {
+  int64_t tiles, units;
+};
+
+// Called by all of a CTA's threads.
 template <int kThreads>
-__device__ __forceinline__ int64_t lay_line(const AttentionParams& p, const Grouping& g, int64_t* line, int64_t* part) {
+__device__ __forceinline__ Length lay_line(const AttentionParams& p, const Grouping& g, Line& line) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int64_t total = 0;
+  Length all = {0, 0};
   for (int b0 = 0; b0 < p.cache.n_seqs; b0 += kThreads) {
     const int b = b0 + tid;
-    int64_t t = 0;
+    int64_t t = 0, u = 0;
     if (b < p.cache.n_seqs) {
       const Seq s = sequence(p, b);
       if (s.bad && blockIdx.x == 0) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
       t = g.all_tiles(s) * p.cache.n_heads;
+      u = (int64_t)g.blocks(s) * p.cache.n_heads;
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, t, o);
-      if (lane >= o) t += v;
+      const int64_t v = __shfl_up_sync(0xffffffffu, t, o), w = __shfl_up_sync(0xffffffffu, u, o);
+      if (lane >= o) {
+        t += v;
+        u += w;
+      }
     }
     __syncthreads();
-    if (lane == 31) part[warp] = t;
+    if (lane == 31) {
+      line.part_tiles[warp] = t;
+      line.part_units[warp] = u;
+    }
     __syncthreads();
-    int64_t before = total;
+    t += all.tiles;
+    u += all.units;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) before += part[w];
-      total += part[w];
+      if (w < warp) {
+        t += line.part_tiles[w];
+        u += line.part_units[w];
+      }
+      all.tiles += line.part_tiles[w];
+      all.units += line.part_units[w];
     }
-    if (b < p.cache.n_seqs && b < kLineSeqs) line[b] = before + t;
+    if (b < p.cache.n_seqs && b < kLineSeqs) {
+      line.tiles[b] = t;
+      line.units[b] = (int32_t)u;
+    }
   }
   __syncthreads();
-  return total;
+  return all;
 }
 
-// The place of tile t (one that the line has), for a whole warp alike.
-__device__ __forceinline__ Cursor place_in_line(const AttentionParams& p, const Grouping& g, const int64_t* line, int64_t t) {
+// A worker's share of the line.
+struct Span {
+  int64_t begin, end, cost;  // of the worker (begin = end: none), of the line
+  int32_t workers, extra;    // that have a share; tiles that a unit counts as beyond its own
+};
+__device__ __forceinline__ Span span_of(const Length& all, int worker, int workers, int most_extra) {
+  Span s;
+  s.workers = (int)(all.tiles < workers ? all.tiles : workers);
+  const int64_t each = s.workers ? all.tiles / s.workers : 0;
+  s.extra = (int)(each <= most_extra ? (each > 0 ? each - 1 : 0) : most_extra);
+  s.cost = all.tiles + s.extra * all.units;
+  s.begin = worker < s.workers ? s.cost * worker / s.workers : 0;
+  s.end = worker < s.workers ? s.cost * (worker + 1) / s.workers : 0;
+  return s;
+}
+// The last worker that has tiles of a unit that ends at unit_end (in cost).
+__device__ __forceinline__ int last_worker(const Span& s, int worker, int64_t unit_end) {
+  int64_t last = unit_end * s.workers / s.cost;
+  if (last >= s.workers) last = s.workers - 1;
+  while (last > worker && s.cost * last / s.workers >= unit_end) --last;
+  while (s.cost * (last + 1) / s.workers < unit_end) ++last;
+  return (int)last;
+}
+
+// A place in the line by its cost, for a whole warp alike: the cursor there, the
+// cost at which its unit starts, and the tile's index in the line.
+struct Start {
+  Cursor at;
+  int64_t unit, index;
+};
+__device__ __forceinline__ Start place_in_line(const AttentionParams& p, const Grouping& g, const Line& line, const Length& all,
+                                               const Span& span, int64_t x) {
   const int lane = threadIdx.x & 31, n = p.cache.n_seqs, m = min(n, kLineSeqs);
-  Cursor c;
-  int64_t inside;
-  if (t < line[m - 1]) {
-    int lo = 0, hi = m - 1;  // the first sequence whose end lies past t
+  Start r;
+  r.index = all.tiles;
+  r.unit = x;
+  if (x >= span.cost) return r;  // (the line's end: its index alone)
+  const auto cost = [&](int b) { return line.tiles[b] + (int64_t)span.extra * line.units[b]; };
+  Cursor& c = r.at;
+  int64_t inside = 0, tiles = 0;
+  if (x < cost(m - 1)) {
+    int lo = 0, hi = m - 1;  // the first sequence whose end lies past x
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
-      if (line[mid] > t)
+      if (cost(mid) > x)
         hi = mid;
       else
         lo = mid + 1;
     }
     c.b = lo;
-    inside = t - (lo ? line[lo - 1] : 0);
+    inside = x - (lo ? cost(lo - 1) : 0);
+    tiles = lo ? line.tiles[lo - 1] : 0;
   } else {
-    int64_t before = line[m - 1];
+    int64_t before = cost(m - 1);
+    tiles = line.tiles[m - 1];
     c.b = m;
-    inside = 0;
     for (int b0 = m; b0 < n; b0 += 32) {
       const int b = b0 + lane;
-      const int64_t own = b < n ? g.all_tiles(sequence(p, b)) * p.cache.n_heads : 0;
-      int64_t incl = own;
+      int64_t own = 0, own_tiles = 0;
+      if (b < n) {
+        const Seq s = sequence(p, b);
+        own_tiles = g.all_tiles(s) * p.cache.n_heads;
+        own = own_tiles + (int64_t)span.extra * g.blocks(s) * p.cache.n_heads;
+      }
+      int64_t incl = own, incl_tiles = own_tiles;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
+        const int64_t v = __shfl_up_sync(0xffffffffu, incl, o), w = __shfl_up_sync(0xffffffffu, incl_tiles, o);
+        if (lane >= o) {
+          incl += v;
+          incl_tiles += w;
+        }
       }
-      const unsigned past = __ballot_sync(0xffffffffu, before + incl > t);
+      const unsigned past = __ballot_sync(0xffffffffu, before + incl > x);
       if (past) {
         const int l = __ffs(past) - 1;
         c.b = b0 + l;
-        inside = t - before - __shfl_sync(0xffffffffu, incl - own, l);
+        inside = x - before - __shfl_sync(0xffffffffu, incl - own, l);
+        tiles += __shfl_sync(0xffffffffu, incl_tiles - own_tiles, l);
         break;
       }
       before += __shfl_sync(0xffffffffu, incl, 31);
+      tiles += __shfl_sync(0xffffffffu, incl_tiles, 31);
     }
   }
   c.s = sequence(p, c.b);
   c.block = 0;
   while (true) {
     c.enter(g);
-    const int64_t of_block = (int64_t)c.tiles * p.cache.n_heads;
+    const int64_t of_block = (int64_t)(c.tiles + span.extra) * p.cache.n_heads;
     if (inside < of_block) break;
     inside -= of_block;
+    tiles += (int64_t)c.tiles * p.cache.n_heads;
     ++c.block;
   }
-  c.head = (int)(inside / c.tiles);
-  c.tile = (int)(inside - (int64_t)c.head * c.tiles);
-  return c;
-}
-
-// A worker's share of the line: each of the first min(workers, total) has one.
-struct Span {
-  int64_t begin, end, total;
-  int32_t workers;  // that have a share
-};
-__device__ __forceinline__ Span span_of(int64_t total, int worker, int workers) {
-  Span s;
-  s.total = total;
-  s.workers = (int)(total < workers ? total : workers);
-  s.begin = worker < s.workers ? total * worker / s.workers : 0;
-  s.end = worker < s.workers ? total * (worker + 1) / s.workers : 0;
-  return s;
+  c.head = (int)(inside / (c.tiles + span.extra));
+  const int off = (int)(inside - (int64_t)c.head * (c.tiles + span.extra));
+  c.tile = max(off - span.extra, 0);
+  r.unit = x - off;
+  r.index = tiles + (int64_t)c.head * c.tiles + c.tile;
+  return r;
 }
 
 // What a worker leaves: the unit that starts in its share and goes on in those
@@ -203,13 +266,6 @@ __device__ __forceinline__ Span span_of(int64_t total, int worker, int workers) 
 struct Joined {
   int32_t last, seq, block, head;
 };
-// The last worker that has tiles of a unit that ends at tile unit_end.
-__device__ __forceinline__ int last_worker(const Span& s, int worker, int64_t unit_end) {
-  int64_t last = unit_end * s.workers / s.total;
-  while (last > worker && s.total * last / s.workers >= unit_end) --last;
-  while (s.total * (last + 1) / s.workers < unit_end) ++last;
-  return (int)last;
-}
 
 // Workspace: a Joined per worker, then two slots a worker (of the unit that it
 // starts with and the one that it ends with, if cut): rows x D outputs, the rows'

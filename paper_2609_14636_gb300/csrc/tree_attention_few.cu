@@ -24,6 +24,7 @@ namespace {
 constexpr int kRows = 16;
 constexpr int kSlots = 32;  // of a tile: one for each lane
 constexpr int kWarps = 4;
+constexpr int kExtra = 1;   // tiles that a unit's start and end cost
 constexpr int kMaxWorkers = 2 * 152 * kWarps;
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
@@ -78,21 +79,24 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_k
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ int64_t line[kLineSeqs], part[kWarps];
+  __shared__ Line line;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const Grouping g = {p.Hq / p.cache.n_heads, kRows, kSlots, p.tree_mask == nullptr};
   const PagedCache& pc = p.cache;
   if (p.D < D)  // (columns past p.D are read as zeros: nothing writes them)
     for (uint32_t i = tid * 16; i < R::kSmem; i += kWarps * 32 * 16)
       *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
-  const int64_t total = lay_line<kWarps * 32>(p, g, line, part);
+  const Length all = lay_line<kWarps * 32>(p, g, line);
 
   const int workers = gridDim.x * kWarps, worker = blockIdx.x * kWarps + warp;
-  const Span span = span_of(total, worker, workers);
+  const Span span = span_of(all, worker, workers, kExtra);
   const Slots slots(p.workspace, workers, kRows, D);
   if (lane == 0) slots.joined[worker] = {0, 0, 0, 0};
   if (span.begin >= span.end) return;
-  Cursor at = place_in_line(p, g, line, span.begin);
+  const Start start = place_in_line(p, g, line, all, span, span.begin);
+  const int count = (int)(place_in_line(p, g, line, all, span, span.end).index - start.index);  // tiles of the share
+  Cursor at = start.at;
+  int64_t unit = start.unit;  // the cost at which the unit starts
 
   const uint32_t base = smem_u32(smem) + warp * R::kStages * R::kStage;
   const int row_chunks = p.D / 8;  // 16-byte chunks of a key or a value
@@ -134,11 +138,11 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_k
   };
 
   Cursor ahead = at;
-  int64_t next = span.begin;
+  int next = 0;
   int into = 0, from = 0;        // stages: the next to load, the next to use
   unsigned lost_in = 0;          // stages (bits) that miss a page
   const auto load_next = [&] {
-    if (next < span.end) {
+    if (next < count) {
       const bool lost = __any_sync(0xffffffffu, load(ahead, into));
       lost_in = (lost_in & ~(1u << into)) | (lost ? 1u << into : 0u);
       ahead.next(p, g);
@@ -157,7 +161,7 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_k
   bool fresh = true, nan = false;
   int first_tile = 0;
 
-  for (int64_t t = span.begin; t < span.end; ++t) {
+  for (int t = 0; t < count; ++t) {
     if (fresh) {  // a unit (or what of it falls to this warp) starts
       fresh = false;
       nan = at.s.bad;
@@ -269,7 +273,7 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_k
     from = from + 1 == R::kStages ? 0 : from + 1;
 
     const bool unit_ends = at.tile + 1 == at.tiles;
-    if (unit_ends || t + 1 == span.end) {
+    if (unit_ends || t + 1 == count) {
       const bool starts = first_tile == 0, whole = unit_ends && starts;
       float* slot = slots.of(worker, starts);
 #pragma unroll
@@ -301,9 +305,10 @@ __global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_k
       }
       if (lane == 0) {
         if (nan) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
-        if (starts && !unit_ends) slots.joined[worker] = {last_worker(span, worker, t + at.tiles - at.tile), at.b, at.block, at.head};
+        if (starts && !unit_ends) slots.joined[worker] = {last_worker(span, worker, unit + span.extra + at.tiles), at.b, at.block, at.head};
       }
       fresh = true;
+      unit += span.extra + at.tiles;
     }
     at.next(p, g);
   }

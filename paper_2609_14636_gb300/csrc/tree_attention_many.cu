@@ -40,6 +40,7 @@ constexpr int kRows = 128;
 constexpr int kSlots = 64;
 constexpr int kRowWarps = 8;
 constexpr int kThreads = (kRowWarps + 3) * 32;
+constexpr int kExtra = 4;  // tiles that a unit's start and end cost
 constexpr int kMaxWorkers = 152;
 constexpr float kGrowth = 8.f;  // log2
 
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ unsigned char dyn[];
-  __shared__ int64_t line[kLineSeqs], part[kThreads / 32];
+  __shared__ Line line;
   __shared__ Barriers bars;
   __shared__ int32_t s_lost[8];  // the tile (1-based, of the share) in a stage that has a slot without a page
   __shared__ int32_t s_abort;
@@ -197,8 +198,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  const int64_t total = lay_line<kThreads>(p, g, line, part);
-  const Span span = span_of(total, blockIdx.x, gridDim.x);
+  const Length all = lay_line<kThreads>(p, g, line);
+  const Span span = span_of(all, blockIdx.x, gridDim.x, kExtra);
   const Slots slots(p.workspace, gridDim.x, kRows, D);
   if (tid == 0) slots.joined[blockIdx.x] = {0, 0, 0, 0};
   if (span.begin >= span.end) return;  // (all threads alike)
@@ -207,11 +208,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     fence_before();
   }
-  Cursor at = place_in_line(p, g, line, span.begin);
+  const Start start = place_in_line(p, g, line, all, span, span.begin);
+  const int n = (int)(place_in_line(p, g, line, all, span, span.end).index - start.index);  // tiles of the share
+  Cursor at = start.at;
   __syncthreads();
   fence_after();
   constexpr uint32_t tmem = 0;  // (all columns are this CTA's)
-  const int n = (int)(span.end - span.begin);
   // Waits end: after two seconds, or once another warp's wait has run out.
   const auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, kWaitTimeoutNs, &s_abort); };
   bool ok = true;
@@ -370,6 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (team == 1) at_stage.on();
     uint32_t parity = 0;              // of this team's scores, weights and output
     bool any_yet = false;             // this team has had a tile
+    int64_t unit = start.unit;        // the cost at which the unit starts
     for (int t0 = 0; t0 < n;) {       // a unit, or what of it falls to this share
       const int len = min(n - t0, at.tiles - at.tile), first_tile = at.tile;
       const bool unit_ends = at.tile + len == at.tiles;
@@ -563,10 +566,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before();
         if (nan && row == 0) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
         if (tid == 0 && starts && !unit_ends)
-          slots.joined[blockIdx.x] = {last_worker(span, blockIdx.x, span.begin + t0 + was.tiles - was.tile), was.b, was.block, was.head};
+          slots.joined[blockIdx.x] = {last_worker(span, blockIdx.x, unit + span.extra + was.tiles), was.b, was.block, was.head};
       }
       all_rows();  // (outputs, maxima and sums make room for the next unit's)
       t0 += len;
+      unit += span.extra + was.tiles;
     }
     if (!ok && lane == 0) set_status(p.dev_status, STRIDE_DEV_TIMEOUT);
   }
