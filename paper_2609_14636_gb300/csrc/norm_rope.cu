@@ -50,16 +50,34 @@ __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bflo
 template <>
 __device__ __forceinline__ __half from_f32(float x) { return __float2half_rn(x); }
 
-// CH elements as one load or store.
+// CH elements as one load or store: whole words, so that none is taken apart by
+// halves.
 template <typename T, int CH>
-struct alignas(sizeof(T) * CH) Chunk {
-  T e[CH];
+struct Chunk {
+  static constexpr int kWords = CH * sizeof(T) / 4;
+  uint32_t w[kWords];
 };
 
 template <typename T, int CH>
 __device__ __forceinline__ Chunk<T, CH> load_chunk(const T* p) {
-  return *reinterpret_cast<const Chunk<T, CH>*>(p);
+  Chunk<T, CH> c;
+  if constexpr (Chunk<T, CH>::kWords == 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    c.w[0] = v.x, c.w[1] = v.y, c.w[2] = v.z, c.w[3] = v.w;
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    c.w[0] = v.x, c.w[1] = v.y;
+  }
+  return c;
 }
+template <typename T, int CH>
+__device__ __forceinline__ void save_chunk(T* p, const Chunk<T, CH>& c) {
+  if constexpr (Chunk<T, CH>::kWords == 4)
+    *reinterpret_cast<uint4*>(p) = make_uint4(c.w[0], c.w[1], c.w[2], c.w[3]);
+  else
+    *reinterpret_cast<uint2*>(p) = make_uint2(c.w[0], c.w[1]);
+}
+
 __device__ __forceinline__ float group_sum(float x, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
@@ -94,31 +112,37 @@ struct Pairs {
 template <typename T, int CH>
 __device__ __forceinline__ Pairs<CH> widen(const Chunk<T, CH>& c) {
   Pairs<CH> p;
-  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(&c);
 #pragma unroll
-    for (int i = 0; i < CH / 2; ++i) p.v[i] = make_float2(bf16_lo(w[i]), bf16_hi(w[i]));
-  } else {
-#pragma unroll
-    for (int i = 0; i < CH / 2; ++i) p.v[i] = make_float2(as_f32<T>(c.e[2 * i]), as_f32<T>(c.e[2 * i + 1]));
+  for (int i = 0; i < CH / 2; ++i) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      p.v[i] = make_float2(bf16_lo(c.w[i]), bf16_hi(c.w[i]));
+    } else if constexpr (std::is_same<T, __half>::value) {
+      __half2 h;
+      *reinterpret_cast<uint32_t*>(&h) = c.w[i];
+      p.v[i] = __half22float2(h);
+    } else {
+      p.v[i] = make_float2(__uint_as_float(c.w[2 * i]), __uint_as_float(c.w[2 * i + 1]));
+    }
   }
   return p;
 }
 template <typename T, int CH>
 __device__ __forceinline__ void store_pairs(T* out, const Pairs<CH>& p) {
   Chunk<T, CH> c;
-  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&c);
 #pragma unroll
-    for (int i = 0; i < CH / 2; ++i) h[i] = __float22bfloat162_rn(p.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < CH / 2; ++i) {
-      c.e[2 * i] = from_f32<T>(p.v[i].x);
-      c.e[2 * i + 1] = from_f32<T>(p.v[i].y);
+  for (int i = 0; i < CH / 2; ++i) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      const __nv_bfloat162 h = __float22bfloat162_rn(p.v[i]);
+      c.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    } else if constexpr (std::is_same<T, __half>::value) {
+      const __half2 h = __float22half2_rn(p.v[i]);
+      c.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+      c.w[2 * i] = __float_as_uint(p.v[i].x);
+      c.w[2 * i + 1] = __float_as_uint(p.v[i].y);
     }
   }
-  *reinterpret_cast<Chunk<T, CH>*>(out) = c;
+  save_chunk(out, c);
 }
 
 // A lane's place in a row, and its angles.
@@ -271,7 +295,7 @@ __device__ __forceinline__ Row<T> row_of(const NormRopeParams& p, int64_t token,
 
 // One warp per token and share of its heads.
 template <typename T, int CH, bool kAppend>
-__global__ void __launch_bounds__(kThreads, 5) norm_rope_kernel(const NormRopeParams p, const Shape sh) {
+__global__ void __launch_bounds__(kThreads, 6) norm_rope_kernel(const NormRopeParams p, const Shape sh) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31;
@@ -322,8 +346,8 @@ __global__ void __launch_bounds__(kThreads, 5) norm_rope_kernel(const NormRopePa
       if (h >= total || (h >= p.q.heads && !kept)) continue;
       const Row<T> r = row_of<T, kAppend>(p, token, h, slot);
       if (r.value) {
-        if (has_a) *reinterpret_cast<Chunk<T, CH>*>(r.y + l.a) = va;
-        if (has_b) *reinterpret_cast<Chunk<T, CH>*>(r.y + l.b) = vb;
+        if (has_a) save_chunk(r.y + l.a, va);
+        if (has_b) save_chunk(r.y + l.b, vb);
         continue;
       }
       if (r.w) {

@@ -4,7 +4,7 @@
 // Each byte of keys and values is used by at most 16 rows, so reading them is
 // what counts.  Every warp works alone: it has a share of the line of tiles
 // (attention_line.cuh) and a ring of stages in shared memory, which it fills with
-// 16-byte asynchronous copies two tiles ahead; a lane looks up one slot's page for
+// 16-byte asynchronous copies a tile ahead; a lane looks up one slot's page for
 // all.  (Bulk copies of a key or a value each, 256 bytes, took some 22 clocks
 // apiece however many were in flight: 3.3 TB/s.)  Rows are padded by 16 bytes,
 // which keeps ldmatrix free of bank conflicts.  16 rows by 32 slots go through mma.sync (m16n8k16: a tcgen05
@@ -23,9 +23,8 @@ namespace {
 
 constexpr int kRows = 16;
 constexpr int kSlots = 32;  // of a tile: one for each lane
-constexpr int kWarps = 4;
 constexpr int kExtra = 1;   // tiles that a unit's start and end cost
-constexpr int kMaxWorkers = 2 * 152 * kWarps;
+constexpr int kSms = 152;
 
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
@@ -69,13 +68,17 @@ template <int D>
 struct Ring {
   static constexpr int kPitch = D * 2 + 16;             // bytes of a slot's key or value
   static constexpr int kStage = 2 * kSlots * kPitch;    // keys, then values
-  static constexpr int kStages = D == 128 ? 3 : 5;
+  // what shared memory holds: the more warps the better, at two stages each (D = 128, us for 256 sequences of up to 4,096
+  // slots: 4 warps of 3 stages 481, 6 of 2 463)
+  static constexpr int kWarps = D == 128 ? 6 : 10, kStages = 2;
+  static constexpr int kMaxWorkers = kSms * kWarps;
   static constexpr size_t kSmem = (size_t)kWarps * kStages * kStage;
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kWarps * 32, D == 128 ? 1 : 2) attention_few_kernel(const AttentionParams p, const int page_shift) {
+__global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(const AttentionParams p, const int page_shift) {
   using R = Ring<D>;
+  constexpr int kWarps = R::kWarps;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ __align__(128) unsigned char smem[];
@@ -321,8 +324,9 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)R::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
+  constexpr int kWarps = R::kWarps;
   const int64_t need = (most_tiles(p, kRows, kSlots) + kWarps - 1) / kWarps;
-  const int grid = (int)std::min<int64_t>(std::min(sms * (D == 128 ? 1 : 2), kMaxWorkers / kWarps), need);
+  const int grid = (int)std::min<int64_t>(std::min(sms, kSms), need);
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = R::kSmem;
@@ -344,7 +348,8 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
 }  // namespace
 
 size_t attention_few_bytes(int D) {
-  return slots_offset(kMaxWorkers) + 2 * kMaxWorkers * slot_floats(kRows, D <= 64 ? 64 : 128) * sizeof(float);
+  const int workers = D <= 64 ? Ring<64>::kMaxWorkers : Ring<128>::kMaxWorkers;
+  return slots_offset(workers) + 2 * (size_t)workers * slot_floats(kRows, D <= 64 ? 64 : 128) * sizeof(float);
 }
 
 cudaError_t launch_attention_few(const AttentionParams& p, int dtype, int sms, cudaStream_t stream) {
