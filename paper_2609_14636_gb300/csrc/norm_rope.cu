@@ -30,7 +30,7 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kAhead = 1;  // rows of a group on their way (two: 269 us instead of 176 for both directions of 16,384 tokens)
+constexpr int kAhead = 1;  // rows of a group on their way (backward of 16,384 tokens: one 108 us, two 143)
 
 template <typename T>
 __device__ __forceinline__ float as_f32(T x);
