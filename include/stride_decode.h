@@ -150,7 +150,9 @@ STRIDE_API size_t stride_tree_attention_workspace_size(int64_t n_tokens, int32_t
  * prefix).  Else tree_mask[i] (uint64 [n_tokens]): bit j set, it sees new
  * token j of its sequence, of which there are at most STRIDE_MAX_TREE (more:
  * STRIDE_DEV_BAD_LAYOUT, that sequence's rows NaN).  A row that sees nothing:
- * out 0, lse -inf.  A slot without a page: STRIDE_DEV_BAD_LAYOUT and NaN rows.
+ * out 0, lse -inf.  Keys and values that a row does not see may hold anything,
+ * NaN and infinities too: they change nothing in it.  A slot without a page:
+ * STRIDE_DEV_BAD_LAYOUT and NaN rows.
  *
  * Types BF16, F16; D a multiple of 8, at most STRIDE_MAX_ATTENTION_DIM; the caches' base and strides whole 16-byte
  * vectors (q and out too); n_tokens times the group of query heads under 2^31 -

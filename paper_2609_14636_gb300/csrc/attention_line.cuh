@@ -12,7 +12,10 @@
 // leaves a Joined record for the kernel that joins them, in the line's order.
 #pragma once
 
+#include <cuda_bf16.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "decode_internal.h"
 #include "stride_device.cuh"
@@ -259,6 +262,59 @@ __device__ __forceinline__ Start place_in_line(const AttentionParams& p, const G
   r.unit = x - off;
   r.index = tiles + (int64_t)c.head * c.tiles + c.tile;
   return r;
+}
+
+// ---- values that are not finite ----
+// A weight of 0 times such a value is NaN in a product, so that a new token that
+// only some of a block's rows see would reach the others.  Where that can be, the
+// components that are not finite are taken out of the values' copy, and added to
+// the outputs of the rows that see them, which gives what the sum gives.
+
+// The first slot that some of a block's rows may not see.
+__device__ __forceinline__ int first_apart(const Grouping& g, const Seq& s, int block) {
+  return s.n <= 1 ? INT32_MAX : s.ctx + (g.chain ? block * g.rows / g.group + 1 : 0);
+}
+// Two components: those that are not finite become zeros.  True where one was.
+template <typename T>
+__device__ __forceinline__ bool make_finite(uint32_t& w) {
+  constexpr uint32_t kExponent = std::is_same<T, __nv_bfloat16>::value ? 0x7f807f80u : 0x7c007c00u;
+  const uint32_t wild = __vcmpeq2(w & kExponent, kExponent);
+  w &= ~wild;
+  return wild != 0;
+}
+// 16 bytes in shared memory, likewise.
+template <typename T>
+__device__ __forceinline__ bool make_finite16(uint32_t addr) {
+  uint32_t w[4];
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= make_finite<T>(w[i]);
+  if (any) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+  return any;
+}
+// Adds those of slots [j0, j1) of a sequence that a row sees (chain: below lim; tree: new tokens `bits`) to what has been
+// stored of the row, an output or a part: to components first, first + 1, then `step` on, below last.
+template <typename T>
+__device__ __noinline__ void add_wild(const AttentionParams& p, int b, int head, int ctx, int j0, int j1, int lim, uint64_t bits, T* out,
+                                      float* part, int first, int last, int step) {
+  const PagedCache& pc = p.cache;
+  for (int j = j0; j < j1; ++j) {
+    if (p.tree_mask ? !((bits >> (j - ctx)) & 1) : j >= lim) continue;
+    const int e = j / pc.page_size;
+    const int32_t page = __ldg(pc.block_table + (int64_t)b * pc.table_stride + e);
+    if (page < 0 || page >= pc.n_pages) continue;
+    const T* v = static_cast<const T*>(pc.v) + page * pc.page_stride + (j - e * pc.page_size) * pc.row_stride + head * pc.head_stride;
+    for (int c = first; c < last && c < p.D; c += step)
+      for (int x = c; x < c + 2; ++x) {
+        const float a = (float)v[x];
+        if (isfinite(a)) continue;
+        if (part)
+          part[x] += a;
+        else
+          out[x] = (T)((float)out[x] + a);
+      }
+  }
 }
 
 // What a worker leaves: the unit that starts in its share and goes on in those

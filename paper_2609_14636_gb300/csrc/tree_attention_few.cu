@@ -76,7 +76,7 @@ struct Ring {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(const AttentionParams p, const int page_shift) {
+__global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(const __grid_constant__ AttentionParams p, const int page_shift) {
   using R = Ring<D>;
   constexpr int kWarps = R::kWarps;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -161,13 +161,14 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
   int lim[2];        // chain: slots below it are seen
   uint64_t bits[2];  // tree: new tokens seen
   const float scale2 = p.scale * kLog2e;
-  bool fresh = true, nan = false;
+  bool fresh = true, nan = false, wild = false;  // wild: the unit has had values that are not finite and some rows may not see
   int first_tile = 0;
 
   for (int t = 0; t < count; ++t) {
     if (fresh) {  // a unit (or what of it falls to this warp) starts
       fresh = false;
       nan = at.s.bad;
+      wild = false;
       first_tile = at.tile;
 #pragma unroll
       for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
@@ -195,6 +196,12 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
     nan |= (lost_in >> from) & 1;
 
     const uint32_t kb = base + from * R::kStage, vb = kb + kSlots * R::kPitch;
+    if (const int apart = first_apart(g, at.s, at.block); at.tile * kSlots + kSlots > apart) {
+      bool was = false;
+      if (at.tile * kSlots + lane >= apart)
+        for (int c = 0; c < row_chunks; ++c) was |= make_finite16<T>(vb + lane * R::kPitch + c * 16);
+      wild |= __any_sync(0xffffffffu, was);  // (and the values are there for all)
+    }
     constexpr int kN = kSlots / 8;
     float s[kN][4];
 #pragma unroll
@@ -279,6 +286,7 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
     if (unit_ends || t + 1 == count) {
       const bool starts = first_tile == 0, whole = unit_ends && starts;
       float* slot = slots.of(worker, starts);
+      const int apart = max(first_apart(g, at.s, at.block), first_tile * kSlots), wild_end = min(at.end, (at.tile + 1) * kSlots);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
@@ -289,6 +297,7 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
 #pragma unroll
           for (int n = 0; n < D / 8; ++n)
             *reinterpret_cast<float2*>(slot + (size_t)r * D + n * 8 + (lane % 4) * 2) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+          if (wild) add_wild<T>(p, at.b, at.head, at.s.ctx, apart, wild_end, lim[h], bits[h], nullptr, slot + (size_t)r * D, (lane % 4) * 2, D, 8);
           if (lane % 4 == 0) {
             slot[(size_t)kRows * D + r] = m[h];
             slot[(size_t)kRows * D + kRows + r] = l[h];
@@ -303,6 +312,7 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
             const int col = n * 8 + (lane % 4) * 2;
             if (col < p.D) *reinterpret_cast<uint32_t*>(out + col) = pack<T>(o[n][2 * h] * by, o[n][2 * h + 1] * by);
           }
+          if (wild) add_wild<T>(p, at.b, at.head, at.s.ctx, apart, wild_end, lim[h], bits[h], out, nullptr, (lane % 4) * 2, D, 8);
           if (p.lse && lane % 4 == 0) p.lse[token * p.Hq + head] = l[h] == 0.f ? -INFINITY : (m[h] + log2f(l[h])) * kLn2;
         }
       }

@@ -162,7 +162,7 @@ struct RowView {
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
-    attention_many_kernel(const AttentionParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+    attention_many_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                           const int box, const int page_shift) {
   using L = Plan<D>;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ Barriers bars;
   __shared__ int32_t s_lost[8];  // the tile (1-based, of the share) in a stage that has a slot without a page
   __shared__ int32_t s_abort;
+  __shared__ int32_t s_wild;  // the last tile (1-based, of the share) with values that are not finite and some rows may not see
   __shared__ uint32_t s_tmem;
   __shared__ float s_m[2][kRows], s_l[2][kRows];  // the teams' maxima and sums, where they are joined
 
@@ -195,6 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars.queries, kRowWarps);
     mbar_init(&bars.drained, 1);
     s_abort = 0;
+    s_wild = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -426,8 +428,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = i0; i < i1; ++i) any |= __ldg(p.tree_mask + at.s.off + i);
             out = !((any >> (back & 63)) & 1);
           }
-          if (out && row / 64 < L::kHalves) {
-            const uint32_t v = stages + st * L::kStage + L::kKeys + (row / 64) * kSlots * 128 + (row & 63) * 128;
+          const uint32_t v = stages + st * L::kStage + L::kKeys + (row / 64) * kSlots * 128 + (row & 63) * 128;
+          if (row / 64 >= L::kHalves) {
+          } else if (!out && slot >= first_apart(g, at.s, at.block)) {
+            bool was = false;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) was |= make_finite16<T>(v + c * 16);
+            if (was) atomicMax(&s_wild, t0 + u + 1);
+          } else if (out) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + c * 16), "r"(0) : "memory");
           }
@@ -522,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok && lane == 0) s_abort = 1;
       if (ok) {
         fence_after();
-        const bool starts = first_tile == 0, whole = unit_ends && starts;
+        const bool starts = first_tile == 0, whole = unit_ends && starts, wild = s_wild > t0;
         const int i = token_of(was);
         const bool have = i < was.s.n;
         const int64_t token = was.s.off + i;
@@ -557,6 +565,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         }
+        if (wild && have)
+          add_wild<T>(p, was.b, was.head, was.s.ctx, max(first_apart(g, was.s, was.block), first_tile * kSlots),
+                      min(was.end, (first_tile + len) * kSlots), view.lim, view.bits, whole ? out : nullptr,
+                      whole ? nullptr : slot + (size_t)row * D, team * (D / 2), (team + 1) * (D / 2), 2);
         if (team == 0 && have && !whole) {
           slot[(size_t)kRows * D + row] = M;
           slot[(size_t)kRows * D + kRows + row] = sum;
