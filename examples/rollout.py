@@ -4,7 +4,10 @@ from the cached prefix.  Random weights; every step of attention, cache, samplin
 and scoring is the library's:
 
     projections -> stride_kv_append (norm, rotation, paged cache) -> stride_tree_attention
-    -> logits -> stride_sample -> stride_score_step_compact -> (stop, record, restart)
+    -> logits -> stride_sample -> stride_score_step_compact -> (stop, restart)
+
+The student then learns from what it wrote (the OPD loss over the kept tokens), with
+stride_qk_norm_rope and its backward pass in its layers.
 
     python examples/rollout.py
 """
@@ -164,6 +167,66 @@ def draft_step(model, ctx_len, last, seed):
     return token, accepted, logits
 
 
+class QkNormRope(torch.autograd.Function):
+    """stride_qk_norm_rope where gradients flow; q, k [N, heads, D] of a layer, norm weights [D]."""
+
+    @staticmethod
+    def forward(ctx, q, k, qn, kn, pos, cos, sin):
+        ctx.save_for_backward(q, k, qn, kn, pos, cos, sin)
+        q_out, k_out = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        stride.stride_qk_norm_rope(q, k, q_out, k_out, pos, cos, sin, qn, kn)
+        return q_out, k_out
+
+    @staticmethod
+    def backward(ctx, dq_out, dk_out):
+        q, k, qn, kn, pos, cos, sin = ctx.saved_tensors
+        dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        dqn, dkn = (torch.empty(t.shape, dtype=torch.float32, device=t.device) for t in (qn, kn))
+        work = torch.empty(stride.stride_qk_norm_rope_backward_workspace_size(len(q), q.shape[1], k.shape[1], q.shape[2]), dtype=torch.uint8, device=q.device)
+        stride.stride_qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, dq, dk, pos, cos, sin, qn, kn,
+                                            dq_weight=dqn, dk_weight=dkn, workspace=work)
+        return dq, dk, dqn.to(qn.dtype), dkn.to(kn.dtype), None, None, None
+
+
+def sequence_logits(model, tokens, qk=QkNormRope.apply):
+    """Logits [n, vocab] of one whole sequence, with gradients."""
+    s, n = model.s, len(tokens)
+    pos = torch.arange(n, dtype=torch.int32, device=tokens.device)
+    x, rows = model.embed[tokens.long()], lambda t: t.transpose(0, 1)[None]
+    norm = lambda x: x * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6).bfloat16()  # noqa: E731
+    for layer in model.layers:
+        q, k, v = (norm(x) @ layer["qkv"].T).view(n, -1, s.head_dim).split([s.heads, s.kv_heads, s.kv_heads], dim=1)
+        q, k = qk(q, k, layer["qn"], layer["kn"], pos, model.cos, model.sin)
+        y = torch.nn.functional.scaled_dot_product_attention(rows(q), rows(k), rows(v), is_causal=True, enable_gqa=True)
+        x = x + y[0].transpose(0, 1).reshape(n, -1) @ layer["out"].T
+        x = x + torch.nn.functional.silu(norm(x) @ layer["up"].T) @ layer["down"].T
+    return norm(x) @ model.head.T
+
+
+def learn(student, teacher, prompts, written, rate):
+    """One step of gradient descent on the OPD loss, -logp_S (logp_T - logp_S) over the written tokens; returns the mean
+    of logp_S - logp_T."""
+    weights = [w for layer in student.layers for w in layer.values()]
+    for w in weights:
+        w.requires_grad_(True)
+        w.grad = None
+    total, n = 0.0, sum(map(len, written))
+    for prompt, new in zip(prompts, written):
+        tokens = torch.cat([prompt, torch.tensor(new, dtype=torch.int32, device=prompt.device)])
+        at = slice(len(prompt) - 1, len(tokens) - 1)
+        logp = lambda x: x[at].float().log_softmax(-1).gather(1, tokens[len(prompt):].long()[:, None])[:, 0]  # noqa: E731
+        own = logp(sequence_logits(student, tokens))
+        with torch.no_grad():
+            d = own - logp(sequence_logits(teacher, tokens))
+        (own * d).sum().div(n).backward()
+        total += float(d.sum())
+    with torch.no_grad():
+        for w in weights:
+            w -= rate * w.grad
+            w.requires_grad_(False)
+    return total / n
+
+
 def main(B=16, turn_len=8, turns=6, prompt=40):
     shape = Shape()
     student, teacher = Model(shape, B, 1), Model(shape, B, 1)
@@ -192,6 +255,8 @@ def main(B=16, turn_len=8, turns=6, prompt=40):
     print(f"restarted after {reused.tolist()} reused tokens, {sum(map(len, second.tokens))} new ones")
     token, accepted, _ = draft_step(student, ctx_len, torch.tensor([t[-1] for t in second.tokens], dtype=torch.int32, device=dev), seed=7)
     print(f"drafted step: {int((accepted > 0).sum())} of {B} guesses accepted")
+    gap = [learn(student, teacher, prompts, first.tokens, rate=0.02) for _ in range(2)]
+    print(f"mean of log p_S - log p_T over the rollouts: {gap[0]:.4f}, after a step {gap[1]:.4f}")
     return student, teacher, prompts, first, second
 
 
