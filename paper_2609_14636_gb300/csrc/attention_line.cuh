@@ -49,7 +49,7 @@ __device__ __forceinline__ Seq sequence(const AttentionParams& p, int b) {
 // How rows and slots are grouped: row = token * group + head within the kv
 // head's query heads.
 struct Grouping {
-  int32_t group, rows, tile;  // query heads per kv head, rows of a block, slots of a tile (n * group fits in 31 bits with room)
+  int32_t group, rows, shift;  // query heads per kv head, rows of a block, 2^shift slots of a tile (n * group fits in 31 bits with room)
   bool chain;                 // no tree mask: each token sees the new ones up to itself
   __device__ __forceinline__ int blocks(const Seq& s) const { return (s.n * group + rows - 1) / rows; }
   // One past the last slot that a block's rows may see.
@@ -57,7 +57,7 @@ struct Grouping {
     if (!chain) return s.ctx + s.n;
     return s.ctx + (min((block + 1) * rows, s.n * group) - 1) / group + 1;
   }
-  __device__ __forceinline__ int tiles(const Seq& s, int block) const { return s.bad ? 1 : (end(s, block) + tile - 1) / tile; }
+  __device__ __forceinline__ int tiles(const Seq& s, int block) const { return s.bad ? 1 : (end(s, block) + (1 << shift) - 1) >> shift; }
   // The tiles of one head of all blocks.
   __device__ __forceinline__ int64_t all_tiles(const Seq& s) const {
     const int nb = blocks(s);
@@ -77,7 +77,7 @@ struct Cursor {
 
   __device__ __forceinline__ void enter(const Grouping& g) {
     end = s.bad ? 0 : g.end(s, block);
-    tiles = s.bad ? 1 : (end + g.tile - 1) / g.tile;
+    tiles = s.bad ? 1 : (end + (1 << g.shift) - 1) >> g.shift;
   }
 
   __device__ __forceinline__ void next(const AttentionParams& p, const Grouping& g) {

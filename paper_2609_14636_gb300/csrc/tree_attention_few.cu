@@ -22,7 +22,7 @@ namespace stride {
 namespace {
 
 constexpr int kRows = 16;
-constexpr int kSlots = 32;  // of a tile: one for each lane
+constexpr int kShift = 5, kSlots = 1 << kShift;  // of a tile: one for each lane
 constexpr int kExtra = 1;   // tiles that a unit's start and end cost
 constexpr int kSms = 152;
 
@@ -76,7 +76,8 @@ struct Ring {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(const __grid_constant__ AttentionParams p, const int page_shift) {
+__global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(const __grid_constant__ AttentionParams p, const int page_shift,
+                                                                              const int line_shift) {
   using R = Ring<D>;
   constexpr int kWarps = R::kWarps;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -84,21 +85,32 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Line line;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Grouping g = {p.Hq / p.cache.n_heads, kRows, kSlots, p.tree_mask == nullptr};
+  const Grouping g = {p.Hq / p.cache.n_heads, kRows, kShift, p.tree_mask == nullptr};
   const PagedCache& pc = p.cache;
   if (p.D < D)  // (columns past p.D are read as zeros: nothing writes them)
     for (uint32_t i = tid * 16; i < R::kSmem; i += kWarps * 32 * 16)
       *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
-  const Length all = lay_line<kWarps * 32>(p, g, line);
+  // (line_shift: of the slots that the line counts as a tile, kSlots or more than any unit has)
+  const bool whole_units = line_shift > kShift;
+  const Grouping lg = {g.group, kRows, line_shift, g.chain};
+  const Length all = lay_line<kWarps * 32>(p, lg, line);
 
   const int workers = gridDim.x * kWarps, worker = blockIdx.x * kWarps + warp;
-  const Span span = span_of(all, worker, workers, kExtra);
+  const Span span = span_of(all, worker, workers, whole_units ? 0 : kExtra);
   const Slots slots(p.workspace, workers, kRows, D);
   if (lane == 0) slots.joined[worker] = {0, 0, 0, 0};
   if (span.begin >= span.end) return;
-  const Start start = place_in_line(p, g, line, all, span, span.begin);
-  const int count = (int)(place_in_line(p, g, line, all, span, span.end).index - start.index);  // tiles of the share
+  const Start start = place_in_line(p, lg, line, all, span, span.begin);
+  int count = (int)(place_in_line(p, lg, line, all, span, span.end).index - start.index);  // tiles of the share
   Cursor at = start.at;
+  if (whole_units) {
+    at.enter(g);
+    Cursor c = at;
+    for (int units = count, u = count = 0; u < units; ++u) {
+      count += c.tiles;
+      c.skip(p, g, c.tiles);
+    }
+  }
   int64_t unit = start.unit;  // the cost at which the unit starts
 
   const uint32_t base = smem_u32(smem) + warp * R::kStages * R::kStage;
@@ -335,7 +347,13 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   constexpr int kWarps = R::kWarps;
-  const int64_t need = (most_tiles(p, kRows, kSlots) + kWarps - 1) / kWarps;
+  // Where no unit has more than two tiles, and each can have a warp of its own, none is cut: there is nothing to join, a launch
+  // less.  (One token over up to 38 slots, 4 kv heads, us cut / whole: 1 sequence 9.8 / 8.0, 64 11.4 / 10.8, 228, a unit for
+  // each warp, 16.5 / 17.0; 1 sequence of 100 slots, four tiles: 10.1 / 10.8.)
+  constexpr int kUncut = 30;
+  const bool whole = p.cache.table_stride * p.cache.page_size <= 2 * kSlots && 2 * most_tiles(p, kRows, 1 << kUncut) <= R::kMaxWorkers;
+  const int line_shift = whole ? kUncut : kShift;
+  const int64_t need = (most_tiles(p, kRows, 1 << line_shift) + kWarps - 1) / kWarps;
   const int grid = (int)std::min<int64_t>(std::min(sms, kSms), need);
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kWarps * 32);
@@ -349,9 +367,9 @@ cudaError_t run(const AttentionParams& p, int dtype, int sms, cudaStream_t strea
   int shift = -1;
   for (int k = 0; k < 31; ++k)
     if (p.cache.page_size == 1 << k) shift = k;
-  e = cudaLaunchKernelEx(&cfg, kern, p, shift);
+  e = cudaLaunchKernelEx(&cfg, kern, p, shift, line_shift);
   if (e != cudaSuccess) return e;
-  if (p.cache.table_stride * p.cache.page_size <= kSlots) return cudaGetLastError();  // (no unit has two tiles)
+  if (whole) return cudaGetLastError();
   return launch_attention_join(p, dtype, grid * kWarps, kRows, 4, stream);
 }
 

@@ -37,7 +37,7 @@ namespace stride {
 namespace {
 
 constexpr int kRows = 128;
-constexpr int kSlots = 64;
+constexpr int kShift = 6, kSlots = 1 << kShift;
 constexpr int kRowWarps = 8;
 constexpr int kThreads = (kRowWarps + 3) * 32;
 constexpr int kExtra = 10;  // tiles that a unit's start and end cost (32 trees of 13 tokens: 2 145 us, 6 138, 8 130, 10 128, 14 129)
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ float s_m[2][kRows], s_l[2][kRows];  // the teams' maxima and sums, where they are joined
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const Grouping g = {p.Hq / p.cache.n_heads, kRows, kSlots, p.tree_mask == nullptr};
+  const Grouping g = {p.Hq / p.cache.n_heads, kRows, kShift, p.tree_mask == nullptr};
   const PagedCache& pc = p.cache;
   const uint32_t stages = (smem_u32(dyn) + 1023) & ~1023u;
 
