@@ -7,9 +7,12 @@
 // 16-byte asynchronous copies a tile ahead; a lane looks up one slot's page for
 // all.  (Bulk copies of a key or a value each, 256 bytes, took some 22 clocks
 // apiece however many were in flight: 3.3 TB/s.)  Rows are padded by 16 bytes,
-// which keeps ldmatrix free of bank conflicts.  16 rows by 32 slots go through mma.sync (m16n8k16: a tcgen05
-// product would have 128 rows, most of them empty, and an accumulator to fetch);
-// maximum, sum and output stay in registers until the unit or the share ends.
+// which keeps ldmatrix free of bank conflicts.  16 rows by 32 slots go through
+// mma.sync (m16n8k16: a tcgen05 product would have 128 rows, most of them empty,
+// and an accumulator to fetch); maximum, sum and output stay in registers until the
+// unit or the share ends.  GB300, 32 / 8 heads of 128, bf16: 256 sequences of up to
+// 4,096 slots 467 us (5.9 TB/s), one of 131,072 102 us (5.2 TB/s), with 16 / 2
+// heads one of 37 7.7 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
