@@ -23,7 +23,9 @@ struct Rows {
   explicit Rows(const stride_head_rows* p) {
     if (p) r = *p;
   }
-  bool valid(int64_t n_tokens) const { return r.n_heads >= 0 && (r.n_heads == 0 || n_tokens == 0 || r.data); }
+  bool valid(int64_t n_tokens, size_t e) const {
+    return r.n_heads >= 0 && (r.n_heads == 0 || n_tokens == 0 || (r.data && multiple(r.data, e)));
+  }
   // Every row starts at a multiple of c elements.
   bool whole(int64_t n_tokens, int c, size_t e) const {
     if (r.n_heads == 0) return true;
@@ -44,8 +46,8 @@ int check_shape(int32_t dtype, int64_t n_tokens, int32_t D) {
   return STRIDE_OK;
 }
 
-int check_cache(const stride_paged_cache* c) {
-  if (!c || !c->k || !c->v || c->n_pages < 1 || c->page_size < 1 || c->n_heads < 1 || c->n_seqs < 1 || c->table_stride < 1 ||
+int check_cache(const stride_paged_cache* c, size_t e) {
+  if (!c || !c->k || !c->v || !multiple(c->k, e) || !multiple(c->v, e) || c->n_pages < 1 || c->page_size < 1 || c->n_heads < 1 || c->n_seqs < 1 || c->table_stride < 1 ||
       !c->block_table || !c->ctx_len || !c->tok_off)
     return STRIDE_ERR_INVALID_ARG;
   return STRIDE_OK;
@@ -114,7 +116,7 @@ int stride_qk_norm_rope(const stride_head_rows* q, const stride_head_rows* k, co
   int rc = check_shape(dtype, n_tokens, D);
   if (rc != STRIDE_OK) return rc;
   const Rows Q(q), K(k), Qo(q_out), Ko(k_out);
-  if (!how || !Q.valid(n_tokens) || !K.valid(n_tokens) || !Qo.valid(n_tokens) || !Ko.valid(n_tokens) || Q.r.n_heads != Qo.r.n_heads || K.r.n_heads != Ko.r.n_heads)
+  if (!how || !Q.valid(n_tokens, elem_bytes(dtype)) || !K.valid(n_tokens, elem_bytes(dtype)) || !Qo.valid(n_tokens, elem_bytes(dtype)) || !Ko.valid(n_tokens, elem_bytes(dtype)) || Q.r.n_heads != Qo.r.n_heads || K.r.n_heads != Ko.r.n_heads)
     return STRIDE_ERR_INVALID_ARG;
   if ((rc = check_how(*how, D)) != STRIDE_OK) return rc;
   if (n_tokens == 0 || Q.r.n_heads + K.r.n_heads == 0) return STRIDE_OK;
@@ -147,7 +149,7 @@ int stride_qk_norm_rope_backward(const stride_head_rows* dq_out, const stride_he
   int rc = check_shape(dtype, n_tokens, D);
   if (rc != STRIDE_OK) return rc;
   const Rows Q(q), K(k), Go(dq_out), Ho(dk_out), G(dq), H(dk);
-  if (!how || !Q.valid(n_tokens) || !K.valid(n_tokens) || !Go.valid(n_tokens) || !Ho.valid(n_tokens) || !G.valid(n_tokens) || !H.valid(n_tokens) || Q.r.n_heads != Go.r.n_heads ||
+  if (!how || !Q.valid(n_tokens, elem_bytes(dtype)) || !K.valid(n_tokens, elem_bytes(dtype)) || !Go.valid(n_tokens, elem_bytes(dtype)) || !Ho.valid(n_tokens, elem_bytes(dtype)) || !G.valid(n_tokens, elem_bytes(dtype)) || !H.valid(n_tokens, elem_bytes(dtype)) || Q.r.n_heads != Go.r.n_heads ||
       Q.r.n_heads != G.r.n_heads || K.r.n_heads != Ho.r.n_heads || K.r.n_heads != H.r.n_heads)
     return STRIDE_ERR_INVALID_ARG;
   if ((rc = check_how(*how, D)) != STRIDE_OK) return rc;
@@ -182,8 +184,8 @@ int stride_kv_append(const stride_head_rows* k, const stride_head_rows* v, const
   if (rc != STRIDE_OK) return rc;
   if (!how) how = &kPlain;
   const Rows K(k), V(v), Q(q), Qo(q_out);
-  if (!K.valid(n_tokens) || !V.valid(n_tokens) || !Q.valid(n_tokens) || !Qo.valid(n_tokens) || Q.r.n_heads != Qo.r.n_heads) return STRIDE_ERR_INVALID_ARG;
-  if ((rc = check_cache(cache)) != STRIDE_OK) return rc;
+  if (!K.valid(n_tokens, elem_bytes(dtype)) || !V.valid(n_tokens, elem_bytes(dtype)) || !Q.valid(n_tokens, elem_bytes(dtype)) || !Qo.valid(n_tokens, elem_bytes(dtype)) || Q.r.n_heads != Qo.r.n_heads) return STRIDE_ERR_INVALID_ARG;
+  if ((rc = check_cache(cache, elem_bytes(dtype))) != STRIDE_OK) return rc;
   if (K.r.n_heads != cache->n_heads || V.r.n_heads != cache->n_heads) return STRIDE_ERR_INVALID_ARG;
   if ((rc = check_how(*how, D)) != STRIDE_OK) return rc;
   if (n_tokens == 0) return STRIDE_OK;
@@ -219,9 +221,9 @@ int stride_tree_attention(const stride_head_rows* q, const stride_head_rows* out
   if (dtype != STRIDE_DTYPE_BF16 && dtype != STRIDE_DTYPE_F16) return STRIDE_ERR_UNSUPPORTED_DTYPE;
   if (n_tokens < 0 || n_tokens > INT32_MAX || D < 8 || D > STRIDE_MAX_ATTENTION_DIM || D % 8 != 0 || !isfinite(scale)) return STRIDE_ERR_INVALID_ARG;
   const Rows Q(q), O(out);
-  int rc = check_cache(cache);
+  int rc = check_cache(cache, elem_bytes(dtype));
   if (rc != STRIDE_OK) return rc;
-  if (!Q.valid(n_tokens) || !O.valid(n_tokens) || Q.r.n_heads < 1 || O.r.n_heads != Q.r.n_heads || Q.r.n_heads % cache->n_heads != 0)
+  if (!Q.valid(n_tokens, elem_bytes(dtype)) || !O.valid(n_tokens, elem_bytes(dtype)) || Q.r.n_heads < 1 || O.r.n_heads != Q.r.n_heads || Q.r.n_heads % cache->n_heads != 0)
     return STRIDE_ERR_INVALID_ARG;
   if (!Q.whole(n_tokens, 8, 2) || !O.whole(n_tokens, 8, 2) || !cache_whole(*cache, 8, 2)) return STRIDE_ERR_INVALID_ARG;
   if (n_tokens * (Q.r.n_heads / cache->n_heads) > INT32_MAX - 256) return STRIDE_ERR_INVALID_ARG;
@@ -254,7 +256,7 @@ int stride_tree_attention(const stride_head_rows* q, const stride_head_rows* out
 int stride_sample(const void* logits, int32_t dtype, int64_t ld, int64_t V, int32_t rows, const float* noise, int64_t ld_noise,
                   const stride_sample_params* params, int32_t* tokens, float* logp, int32_t* dev_status, void* stream) {
   if (elem_bytes(dtype) == 0) return STRIDE_ERR_UNSUPPORTED_DTYPE;
-  if (!params || rows < 0 || V < 1 || V > STRIDE_MAX_VOCAB || ld < V || (rows > 0 && (!logits || !tokens))) return STRIDE_ERR_INVALID_ARG;
+  if (!params || rows < 0 || V < 1 || V > STRIDE_MAX_VOCAB || ld < V || (rows > 0 && (!logits || !tokens || !multiple(logits, elem_bytes(dtype)) || !multiple(noise, sizeof(float))))) return STRIDE_ERR_INVALID_ARG;
   const bool greedy = !params->temperature && params->temperature_all == 0.f;
   if (!greedy && ((rows > 0 && !noise) || ld_noise < V)) return STRIDE_ERR_INVALID_ARG;
   if (!params->temperature && !(params->temperature_all >= 0.f && isfinite(params->temperature_all))) return STRIDE_ERR_INVALID_ARG;

@@ -135,3 +135,17 @@ def test_python_refuses_host_tensors(env):
     for fn in (stride.stride_qk_norm_rope_backward, stride.stride_qk_norm_rope):
         with pytest.raises(TypeError):
             fn(x)
+
+
+def test_data_between_elements(env):
+    """Rows, caches, logits and noise that no element of their type can start at."""
+    stride, decode, L = env
+    odd, r, h, c, s = ctypes.byref(rows(decode, data=DUMMY + 1)), ctypes.byref(rows(decode, heads=2)), how(decode), cache(decode), params(decode)
+    h, c, s = ctypes.byref(h), ctypes.byref(c), ctypes.byref(s)
+    assert L.stride_qk_norm_rope(odd, r, odd, r, 0, 5, 64, h, None, None) == 1
+    assert L.stride_qk_norm_rope_backward(odd, r, odd, r, odd, r, 0, 5, 64, h, None, None, None, DUMMY, 1 << 30, None) == 1
+    assert L.stride_kv_append(r, r, odd, odd, 0, 5, 64, h, c, None, None) == 1
+    assert L.stride_kv_append(r, r, None, None, 0, 5, 64, h, ctypes.byref(cache(decode, k=DUMMY + 1)), None, None) == 1
+    assert L.stride_tree_attention(r, odd, None, 0, 5, 64, 1.0, None, c, None, DUMMY, 1 << 30, None) == 1
+    for x, noise, dtype in ((DUMMY + 1, DUMMY, 0), (DUMMY + 2, DUMMY, 1), (DUMMY, DUMMY + 2, 0)):
+        assert L.stride_sample(x, dtype, 100, 100, 2, noise, 100, s, DUMMY, None, None, None) == 1
