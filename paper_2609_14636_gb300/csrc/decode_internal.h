@@ -88,6 +88,7 @@ struct SampleParams {
   int32_t* tokens;
   float* logp;
   int32_t* dev_status;
+  bool long_first;  // rows without a top_k are started first
 };
 cudaError_t launch_sample(const SampleParams& p, int dtype, int sms, cudaStream_t stream);
 

@@ -147,6 +147,7 @@ struct Shared {
   uint64_t wm[kWarps];
   int32_t cutoff;
   uint32_t count, bound;
+  int32_t first_row;
   Pick pick;
   float pivot[kMaxCluster][kPivots], part[kWarps][kPivots];
 };
@@ -1010,6 +1011,28 @@ __device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& s
   exact_race(p, sh, noise, q.r, weight, true, best, kept, cluster);
 }
 
+// The n-th row of the call (of kThreads at most) if those without a top_k, which
+// take several times as long as the others, come first: started last, they were what
+// the call waited for.
+__device__ __forceinline__ int32_t long_first(const SampleParams& p, int32_t n) {
+  Shared& s = shared();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int32_t k = tid < p.rows ? __ldg(p.how.top_k + tid) : 1;
+  const bool is_long = k <= 0 || k >= p.V;
+  const unsigned those = __ballot_sync(0xffffffffu, is_long);
+  if (lane == 0) s.wc[warp] = __popc(those);
+  __syncthreads();
+  int32_t before = __popc(those & ((1u << lane) - 1)), all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += s.wc[w];
+    all += s.wc[w];
+  }
+  if (tid < p.rows && (is_long ? before : all + tid - before) == n) s.first_row = tid;
+  __syncthreads();
+  return s.first_row;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -1018,7 +1041,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int32_t r = blockIdx.x / C;
+  const int32_t r = p.long_first ? long_first(p, blockIdx.x / C) : blockIdx.x / C;
   constexpr int N = Vec<T>::N;
 
   Share<T> sh;
@@ -1248,13 +1271,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 }
 
 template <typename T>
-cudaError_t run(const SampleParams& p, int sms, cudaStream_t stream) {
+cudaError_t run(SampleParams p, int sms, cudaStream_t stream) {
   // CTAs of a row: 8 where all run at once (two on an SM), 4 up to two rows an SM, else 1; at least a vector per thread.
   // us a call on rows of 151,936 bf16 logits, with 8 / 4 / 2 / 1: 1 row, top_k 50: 10.0 / 11.3 / 13.3 / 18.4; 64 rows: 24.8 /
   // 14.6 / 16.8 / 27.0; 256 rows of mixed parameters, a few with a top_p over the tail: 131 / 106 / 139 / 226; 512 uncut rows of
   // 32,000 fp32: 144 / 80.5 / 60.4 / 47.7.
   int C = (int64_t)p.rows * kMaxCluster <= 2 * sms ? kMaxCluster : p.rows <= 2 * sms ? 4 : 1;
   while (C > 1 && p.V < C * kThreads * Vec<T>::N) C /= 2;
+  p.long_first = p.how.top_k && p.rows <= kThreads && (int64_t)p.rows * C > 2 * sms;  // (several waves of CTAs)
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)p.rows * C));
   cfg.blockDim = dim3(kThreads);

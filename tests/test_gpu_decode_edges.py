@@ -111,3 +111,16 @@ def test_sample_numbers_of_rows(env, rows):  # noqa: F811
     top_p = rng.choice([0.2, 0.9, 0.999, 1.0], rows)
     min_p = rng.choice([0.0, 0.01], rows)
     check_sample(torch, stride, x, noise, T, top_k, top_p, min_p)
+
+
+@pytest.mark.parametrize("rows", [130, 512])
+def test_sample_rows_without_top_k_among_others(env, rows):  # noqa: F811
+    """More rows than the GPU takes at once, in any order of kinds."""
+    torch, stride, dev = env
+    V = 20_001
+    rng = np.random.default_rng(rows)
+    x, noise = logits(torch, rows, V, "bf16", rows)
+    top_k = rng.choice([0, 1, 40, V, V - 1, -3], rows, p=[0.3, 0.2, 0.3, 0.1, 0.05, 0.05])
+    top_k[0] = top_k[-1] = 0
+    T, top_p = np.full(rows, 0.9, np.float32), rng.choice([0.5, 0.95, 1.0], rows)
+    check_sample(torch, stride, x, noise, T, top_k, top_p, 0.0)
