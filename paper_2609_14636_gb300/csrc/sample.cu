@@ -6,7 +6,7 @@
 //   token = argmax over the kept of w_i / noise_i (an exponential race).
 //
 // A row belongs to a thread-block cluster of 1 to 8 CTAs, each of which takes a
-// share of it: as many CTAs as run at once.  The row comes from memory once;
+// share of it (run() below says how many).  The row comes from memory once;
 // what is read again comes from L2.  Three ways:
 // - nothing is cut off: the race is run while the row streams in, each thread's
 //   ratios relative to the largest logit it has met;
@@ -28,8 +28,8 @@
 //   counting.  One more pass races what is kept.
 //   All sums that atomics make are integers: their order changes nothing.
 // Noise is read for kept tokens alone.  GB300, rows of 151,936 bf16 logits: one row
-// with a top_k of 50 10 us, 256 of them 51 (1.5 TB/s); 256 rows of mixed parameters
-// 113; 512 uncut rows of 32,000 fp32 48 (2.7 TB/s).
+// with a top_k of 50 10 us, 256 of them 33 (2.4 TB/s); 256 rows of mixed parameters
+// 87; 512 uncut rows of 32,000 fp32 46 (2.9 TB/s).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1272,11 +1272,24 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
 template <typename T>
 cudaError_t run(SampleParams p, int sms, cudaStream_t stream) {
-  // CTAs of a row: 8 where all run at once (two on an SM), 4 up to two rows an SM, else 1; at least a vector per thread.
-  // us a call on rows of 151,936 bf16 logits, with 8 / 4 / 2 / 1: 1 row, top_k 50: 10.0 / 11.3 / 13.3 / 18.4; 64 rows: 24.8 /
-  // 14.6 / 16.8 / 27.0; 256 rows of mixed parameters, a few with a top_p over the tail: 131 / 106 / 139 / 226; 512 uncut rows of
-  // 32,000 fp32: 144 / 80.5 / 60.4 / 47.7.
-  int C = (int64_t)p.rows * kMaxCluster <= 2 * sms ? kMaxCluster : p.rows <= 2 * sms ? 4 : 1;
+  // CTAs of a row: 8 where all run at once (two on an SM); else, at least a vector per thread,
+  // - with a top_k of each row's own, 4 up to the 512 rows that long_first() orders: the longest row counts (us, rows of 151,936
+  //   bf16 logits, with 8 / 4 / 2 / 1, 90 rows of mixed parameters: 46 / 47 / 67 / 112; 256: 87 / 88 / 129 / 217; 500: 160 /
+  //   110 / 140 / 233);
+  // - with one small top_k for all, what runs at once (top_k 50, 64 rows: 25 / 15 / 17 / 27; 90: 30 / 23 / 17 / 29; 256: 75 / 46 /
+  //   34 / 35; 500: 144 / 86 / 69 / 62);
+  // - else 4 up to two rows an SM, and 1 (top_p 0.9, 90 rows: 133 / 110 / 156 / 272; 256: 318 / 231 / 220 / 307; 512 uncut rows of
+  //   32,000 fp32: 144 / 81 / 60 / 48).
+  const int64_t rows = p.rows, at_once = 2 * sms;
+  int C = 1;
+  if (rows * kMaxCluster <= at_once)
+    C = kMaxCluster;
+  else if (p.how.top_k)
+    C = rows <= kThreads ? 4 : 1;
+  else if (p.how.top_k_all > 0 && p.how.top_k_all <= 128)
+    C = rows * 4 <= at_once ? 4 : rows <= at_once ? 2 : 1;
+  else
+    C = rows <= at_once ? 4 : 1;
   while (C > 1 && p.V < C * kThreads * Vec<T>::N) C /= 2;
   p.long_first = p.how.top_k && p.rows <= kThreads && (int64_t)p.rows * C > 2 * sms;  // (several waves of CTAs)
   cudaLaunchConfig_t cfg = {};
