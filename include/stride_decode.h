@@ -125,7 +125,8 @@ STRIDE_API int stride_qk_norm_rope_backward(const stride_head_rows* dq_out, cons
  * q_out = rotated, normed q.  Types BF16, F16, F32, the cache's and the rows'
  * alike; D <= STRIDE_MAX_HEAD_DIM; how NULL: plain copies.  A token whose slot
  * the block table does not hold (no such entry, or a page outside
- * [0, n_pages)) is not written and sets STRIDE_DEV_BAD_LAYOUT.  Slots of two
+ * [0, n_pages)), of no sequence, or of one of a negative ctx_len is not written
+ * and sets STRIDE_DEV_BAD_LAYOUT.  Slots of two
  * tokens must differ. */
 STRIDE_API int stride_kv_append(const stride_head_rows* k, const stride_head_rows* v,
                                 const stride_head_rows* q, const stride_head_rows* q_out,

@@ -17,7 +17,7 @@
 // four components divides, or of more than 512 (fp32: 256), go by single
 // components, a warp each.  GB300, 16,384 tokens, 32 + 8 heads of 128, bf16:
 // forward 65 us (5.2 TB/s), backward 108 (4.7 TB/s); 13 sequences of 640 tokens
-// into pages 33 us (4.1 TB/s); 256 tokens 4.4 us.
+// into pages 30.5 us (4.4 TB/s); 256 tokens 4.4 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -257,7 +257,7 @@ __device__ __forceinline__ int64_t slot_of(const PagedCache& c, int64_t token, i
     ctx = __ldg(c.ctx_len + b);
   }
   const int64_t slot = (int64_t)ctx + (token - first);
-  kept = slot >= 0 && slot <= INT32_MAX && token < end;
+  kept = ctx >= 0 && token >= first && token < end && slot <= INT32_MAX;
   const int32_t at = kept ? (int32_t)slot : 0, entry = at / c.page_size;
   int32_t page = -1;
   if (kept && entry < c.table_stride) page = __ldg(c.block_table + (int64_t)b * c.table_stride + entry);
@@ -694,7 +694,9 @@ cudaError_t run_forward(const NormRopeParams& p, bool append, int sms, cudaStrea
   Shape sh = {group_lanes(p.D, CH), rows};
   if constexpr (CH > 1) {
     const int groups = 32 / sh.lanes, most = (rows + groups - 1) / groups;  // one pass over the heads per warp
-    const int64_t share = ((int64_t)sms * 64 + p.n_tokens - 1) / p.n_tokens;
+    // as many warps as run at once, if there are so few tokens: what a token needs is then read once (640 tokens each of 13
+    // sequences, warps an SM: 24 30.5 us, 48 to 64 33.0, 192 41.0; 256 tokens: 16 5.0, 24 to 192 4.4)
+    const int64_t share = ((int64_t)sms * 24 + p.n_tokens - 1) / p.n_tokens;
     sh.warps_per_token = (int)(share < 1 ? 1 : share > most ? most : share);
   }
   const int64_t blocks = (p.n_tokens * sh.warps_per_token + kWarps - 1) / kWarps;

@@ -99,6 +99,38 @@ def test_attention_of_many_rows_over_long_prefixes(env, D, dtype, page):  # noqa
     check_attention(torch, stride, c, q, [m for n in n_new for m in random_tree(rng, n)], D ** -0.5, dtype)
 
 
+def test_rotation_tables_anywhere(env):  # noqa: F811
+    """Tables that start between 16-byte vectors give the same bits, forward and backward."""
+    torch, stride, dev = env
+    N, D, g = 37, 128, gen(torch, 4)
+    q, k, dq_out, dk_out = ((torch.randn((N, h, D), generator=g, device=dev)).bfloat16() for h in (3, 1, 3, 1))
+    w, pos = torch.randn(D, generator=g, device=dev).bfloat16(), torch.randint(0, 50, (N,), generator=g, device=dev).int()
+    angle = torch.arange(50, device=dev)[:, None] * torch.linspace(1, 0.01, D // 2, device=dev)
+    cos, sin = angle.cos(), angle.sin()
+    got = []
+    for shift in (0, 1):
+        c, s = (torch.cat([t.new_zeros(shift), t.flatten()])[shift:].view(t.shape) for t in (cos, sin))
+        assert c.data_ptr() % 16 == 4 * shift
+        out = [torch.empty_like(t) for t in (q, k, q, k)]
+        ws = torch.empty(stride.stride_qk_norm_rope_backward_workspace_size(N, 3, 1, D), dtype=torch.uint8, device=dev)
+        stride.stride_qk_norm_rope(q, k, *out[:2], pos, c, s, w, w)
+        stride.stride_qk_norm_rope_backward(dq_out, dk_out, q, k, *out[2:], pos, c, s, w, w, workspace=ws)
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_append_of_a_negative_length(env):  # noqa: F811
+    """Its tokens are not written, not those either that a sum would put into a slot; the other sequences' are."""
+    torch, stride, dev = env
+    c = Paged(torch, [2, 3, 4], [3, 4, 1], 1, 64, 4, "bf16", False, 1, fill=0.0)
+    k = torch.ones((8, 1, 64), dtype=torch.bfloat16, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    ctx = torch.tensor([2, -2, 4], dtype=torch.int32, device=dev)
+    stride.stride_kv_append(k, k, *c.args[:3], ctx, c.args[4], dev_status=status)
+    assert int(status) == stride.DEV_BAD_LAYOUT
+    assert float(c.k.sum()) == float(c.v.sum()) == 4 * 64
+
+
 @pytest.mark.parametrize("rows", [39, 304, 305, 700])
 def test_sample_numbers_of_rows(env, rows):  # noqa: F811
     """A row's share of the GPU changes with their number: the tokens do not."""
