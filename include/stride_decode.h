@@ -21,7 +21,9 @@
  *
  * Types: STRIDE_DTYPE_BF16 and STRIDE_DTYPE_F16 everywhere, STRIDE_DTYPE_F32
  * where a call says so.  Products, sums, norms and softmax statistics are held
- * in 32 bits; each result is rounded once to its type.
+ * in 32 bits; each result is rounded once to its type.  Attention rounds one
+ * thing more: the softmax weights that its second product takes are of the
+ * rows' type (see there).
  */
 #ifndef STRIDE_DECODE_H_
 #define STRIDE_DECODE_H_
@@ -154,6 +156,12 @@ STRIDE_API size_t stride_tree_attention_workspace_size(int64_t n_tokens, int32_t
  * out 0, lse -inf.  Keys and values that a row does not see may hold anything,
  * NaN and infinities too: they change nothing in it.  A slot without a page:
  * STRIDE_DEV_BAD_LAYOUT and NaN rows.
+ *
+ * The weights exp(s_j - max s) go into the second product rounded to the rows'
+ * type, which is the only one that its operands may have beside such values;
+ * their sum, and with it lse, takes them unrounded.  A component of out is so
+ * within u sum_j p_j |v_j| of the one that 32-bit weights give, p = softmax(s), u
+ * half a unit in the last place (2^-8 BF16, 2^-11 F16), before its own rounding.
  *
  * Types BF16, F16; D a multiple of 8, at most STRIDE_MAX_ATTENTION_DIM; the caches' base and strides whole 16-byte
  * vectors (q and out too); n_tokens times the group of query heads under 2^31 -

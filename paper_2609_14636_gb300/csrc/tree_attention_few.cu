@@ -281,7 +281,8 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
         s[n][x] = ex2(s[n][x] - ref[x >> 1]);
         l[x >> 1] += s[n][x];
       }
-    // (weights rounded to the values' type, as the product takes them; their sum is of the unrounded ones)
+    // The weights are rounded to the values' type, as mma.sync wants both operands of one type (a product of what the rounding
+    // leaves would be half as many instructions again).  Their sum is of the unrounded ones.
 #pragma unroll
     for (int k = 0; k < kN / 2; ++k) {
       const uint32_t a[4] = {pack<T>(s[2 * k][0], s[2 * k][1]), pack<T>(s[2 * k][2], s[2 * k][3]),

@@ -19,7 +19,10 @@
 //         tile waits for the other's.
 // The output is rescaled only where a row's maximum has grown by more than 2^8
 // since it was last (weights up to 256 fit both types as well as weights up to 1;
-// maximum and sum stay consistent either way).  Slots past the end, and new tokens
+// maximum and sum stay consistent either way).  The weights are rounded to the
+// values' type, as tcgen05 wants both operands of one type; their sum is of the
+// unrounded ones.  (What the rounding leaves, as a second operand, has no place in
+// tensor memory, and its product would be half as much work again.)  Slots past the end, and new tokens
 // that no row of the block sees, may hold anything: their values are zeroed in
 // shared memory before the second product, their scores are masked.  Exponentials
 // and the moves between tensor memory and registers bound it: GB300, 32 / 8 heads of
