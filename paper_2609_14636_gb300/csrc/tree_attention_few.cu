@@ -215,7 +215,8 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
       bool was = false;
       if (at.tile * kSlots + lane >= apart)
         for (int c = 0; c < row_chunks; ++c) was |= make_finite16<T>(vb + lane * R::kPitch + c * 16);
-      wild |= __any_sync(0xffffffffu, was);  // (and the values are there for all)
+      wild |= __any_sync(0xffffffffu, was);
+      __syncwarp();  // (other lanes read the values: a vote alone orders no memory)
     }
     constexpr int kN = kSlots / 8;
     float s[kN][4];
