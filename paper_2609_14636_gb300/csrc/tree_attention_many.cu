@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = __all_sync(0xffffffffu, wait(&bars.empty[at_stage.st], at_stage.parity ^ 1));
         if (!ok) break;
       }
-      if (__any_sync(0xffffffffu, lost) && lane == 0) s_lost[at_stage.st] = t + 1;
+      const bool any_lost = __any_sync(0xffffffffu, lost);
       const unsigned who = __ballot_sync(0xffffffffu, real) & ((1u << boxes) - 1);
       int pages[8], rows[8];
 #pragma unroll
@@ -269,6 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (elect_one()) {
         uint64_t* bar = &bars.full[at_stage.st];
         const uint32_t to = dst + at_stage.st * L::kStage;
+        if (any_lost) s_lost[at_stage.st] = t + 1;  // (by the thread whose arrival publishes it)
         mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * L::kHalves * box * 128));
 #pragma unroll
         for (int x = 0; x < 8; ++x)

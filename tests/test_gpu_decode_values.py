@@ -48,3 +48,24 @@ def test_every_new_value_has_a_component_that_is_not_finite(env, dtype, D):  # n
                 assert good.sum() == D - i - 1 and (y[~good] == np.inf).all()
                 assert (np.abs(y[good] - o[good]) <= u * size[good] + u * np.abs(o[good]) + 8 * 2e-6 * size[good] + 1e-30).all()
         at += n
+
+
+@pytest.mark.parametrize("page", [8, 16, 64])
+def test_missing_page_among_many_rows(env, page):  # noqa: F811
+    """Wherever in a tile the page is missing, its sequence's rows are NaN and the other sequences' keep their bits."""
+    torch, stride, dev = env
+    c = Paged(torch, [300, 700, 200], [40, 40, 40], 2, 128, page, "bf16", False, 1)
+    c.put(torch, gen(torch, 2))
+    q = torch.randn((120, 8, 128), generator=gen(torch, 3), device=dev).bfloat16()
+    good, good_lse, status = attend(torch, stride, c, q, 0.1)
+    assert status == 0 and torch.isfinite(good).all()
+    table = c.args[2].clone()
+    for entry in {0, 1, 7, 650 // page, 699 // page}:
+        for spoil in (-1, c.k.shape[0]):
+            c.args[2].copy_(table)
+            c.args[2][1, entry] = spoil
+            out, lse, status = attend(torch, stride, c, q, 0.1)
+            assert status == stride.DEV_BAD_LAYOUT
+            assert torch.isnan(out[40:80]).all() and torch.isnan(lse[40:80]).all()
+            for at in (slice(0, 40), slice(80, 120)):
+                assert torch.equal(out[at], good[at]) and torch.equal(lse[at], good_lse[at])
