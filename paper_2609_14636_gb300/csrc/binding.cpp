@@ -580,6 +580,7 @@ int sample(PyObject* const* a) {
   const at::Tensor& x = tensor(a[0]);
   need(x.dim() == 2 && (x.size(1) <= 1 || x.stride(1) == 1) && x.size(0) <= INT32_MAX);
   const int64_t rows = x.size(0), V = a[9] == Py_None ? x.size(1) : integer(a[9]);
+  need(V <= x.size(1));
   const int64_t ld = rows <= 1 && x.stride(0) < x.size(1) ? x.size(1) : x.stride(0);
   const int32_t dt = row_dtype(x.scalar_type());
   const float* noise = nullptr;

@@ -250,6 +250,8 @@ def stride_sample(logits, noise, tokens, temperature=1.0, top_k=0, top_p=1.0, mi
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [rows, V] with unit column stride")
     rows, V = logits.shape[0], logits.shape[1] if V is None else int(V)
+    if V > logits.shape[1]:
+        raise ValueError(f"V is {V}, the logits have {logits.shape[1]} columns")
     if noise is not None:
         if not isinstance(noise, torch.Tensor) or not noise.is_cuda or noise.dtype != torch.float32:
             raise TypeError("noise must be a float32 CUDA tensor")

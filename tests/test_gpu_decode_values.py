@@ -69,3 +69,15 @@ def test_missing_page_among_many_rows(env, page):  # noqa: F811
             assert torch.isnan(out[40:80]).all() and torch.isnan(lse[40:80]).all()
             for at in (slice(0, 40), slice(80, 120)):
                 assert torch.equal(out[at], good[at]) and torch.equal(lse[at], good_lse[at])
+
+
+def test_sample_of_more_columns_than_there_are(env):  # noqa: F811
+    torch, stride, dev = env
+    x = torch.zeros((4, 128), device=dev)[:, 28:]
+    tokens = torch.full((4,), 7, dtype=torch.int32, device=dev)
+    for V in (101, 128):
+        with pytest.raises(ValueError, match="V"):
+            stride.stride_sample(x, None, tokens, temperature=0, V=V)
+    assert (tokens == 7).all()
+    stride.stride_sample(x, None, tokens, temperature=0, V=100)
+    assert not tokens.any()
