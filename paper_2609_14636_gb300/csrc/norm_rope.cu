@@ -201,10 +201,13 @@ __device__ __forceinline__ void turn_to(Place<CH>& l, const NormRopeParams& p, i
 
 __device__ __forceinline__ float2 negative(float2 x) { return make_float2(-x.x, -x.y); }
 
-// (A, B) rotated by the lane's angles; back: by their negatives.
+// (A, B) rotated by the lane's angles; back: by their negatives.  Components from R
+// on stay as they are (a product with a sine of 0 would make an infinity of one NaN in
+// the other).
 template <int CH, bool kBack>
-__device__ __forceinline__ void turn(const Place<CH>& l, Pairs<CH>& A, Pairs<CH>& B, bool inter) {
+__device__ __forceinline__ void turn(const Place<CH>& l, Pairs<CH>& A, Pairs<CH>& B, int R, bool inter) {
   if (!inter) {
+    if (2 * l.a >= R) return;  // (half of R is a multiple of CH)
 #pragma unroll
     for (int i = 0; i < CH / 2; ++i) {
       const float2 a = A.v[i], b = B.v[i], c = l.c.v[i], s = kBack ? negative(l.s.v[i]) : l.s.v[i];
@@ -219,8 +222,8 @@ __device__ __forceinline__ void turn(const Place<CH>& l, Pairs<CH>& A, Pairs<CH>
       const float cb = i & 1 ? l.c.v[k].y : l.c.v[k].x, ub = i & 1 ? l.s.v[k].y : l.s.v[k].x;
       const float sa = kBack ? -ua : ua, sb = kBack ? -ub : ub;
       const float2 a = A.v[i], b = B.v[i];
-      A.v[i] = make_float2(fmaf(a.x, ca, -(a.y * sa)), fmaf(a.x, sa, a.y * ca));
-      B.v[i] = make_float2(fmaf(b.x, cb, -(b.y * sb)), fmaf(b.x, sb, b.y * cb));
+      if (l.a + 2 * i < R) A.v[i] = make_float2(fmaf(a.x, ca, -(a.y * sa)), fmaf(a.x, sa, a.y * ca));
+      if (l.b + 2 * i < R) B.v[i] = make_float2(fmaf(b.x, cb, -(b.y * sb)), fmaf(b.x, sb, b.y * cb));
     }
   }
 }
@@ -361,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 6) norm_rope_kernel(const NormRopePa
         times(A, wa);
         times(B, wb);
       }
-      if (p.rot_dim > 0) turn<CH, false>(l, A, B, inter);
+      if (p.rot_dim > 0) turn<CH, false>(l, A, B, p.rot_dim, inter);
       if (r.w || !good) {
         const float by = good ? rsqrtf(ss / (float)p.D + p.eps) : NAN;
         times(A, by);
@@ -450,7 +453,7 @@ __global__ void __launch_bounds__(kBackThreads, 4) norm_rope_backward_kernel(con
       const Pairs<CH> A = widen(next[u].xa), B = widen(next[u].xb);
       Pairs<CH> ga = widen(next[u].ya), gb = widen(next[u].yb);
       ask(next[u]);  // (a row's own loads are done before its gradient is stored: dx may be dy)
-      if (p.rot_dim > 0) turn<CH, true>(l, ga, gb, inter);  // du
+      if (p.rot_dim > 0) turn<CH, true>(l, ga, gb, p.rot_dim, inter);  // du
       if (wt) {
         const float ss = group_sum(dot(A, A, B, B), sh.lanes), r = good ? rsqrtf(ss * inv_d + p.eps) : NAN;
         const float2 rr = make_float2(r, r);

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import decode_reference as ref
-from test_gpu_decode_step import Paged, env, gen  # noqa: F401
+from test_gpu_decode_step import Paged, env, gen, qk_inputs, tables  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,69 @@ def test_sample_of_more_columns_than_there_are(env):  # noqa: F811
     assert (tokens == 7).all()
     stride.stride_sample(x, None, tokens, temperature=0, V=100)
     assert not tokens.any()
+
+
+# N, Hq, Hk, D, R, interleaved, norm, dtype, layout
+PASS_THROUGH = [
+    (5, 3, 1, 128, 64, False, False, "bf16", "plain"),
+    (5, 3, 1, 128, 64, True, False, "bf16", "fused"),
+    (7, 2, 2, 96, 36, True, False, "f16", "plain"),
+    (7, 2, 2, 80, 16, False, False, "f32", "fused"),
+    (6, 2, 1, 64, 0, False, False, "bf16", "plain"),
+    (6, 5, 1, 64, 10, True, False, "f32", "plain"),
+    (5, 3, 1, 128, 64, False, True, "bf16", "plain"),
+    (5, 3, 1, 128, 64, True, True, "f16", "fused"),
+    (9, 2, 1, 80, 40, True, True, "f32", "plain"),
+    (4, 2, 1, 51, 22, False, False, "bf16", "odd"),
+    (4, 2, 1, 51, 22, True, True, "f32", "odd"),
+]
+
+
+def the_same(got, want, tol):
+    got, good = ref.f64(got), np.isfinite(want)
+    assert np.array_equal(got[~good], want[~good], equal_nan=True), (got[~good], want[~good])
+    bad = ~(np.abs(got[good] - want[good]) <= np.broadcast_to(tol, want.shape)[good])
+    assert not bad.any(), (int(bad.sum()), got[good][bad][:4], want[good][bad][:4])
+
+
+@pytest.mark.parametrize("case", PASS_THROUGH, ids=str)
+def test_components_that_are_not_rotated_and_not_finite(env, case):  # noqa: F811
+    """An infinity or NaN past rot_dim changes nothing else, but through the norm; forward, backward and append."""
+    torch, stride, dev = env
+    N, Hq, Hk, D, R, inter, norm, dtype, layout = case
+    rows = [qk_inputs(torch, N, Hq, Hk, D, dtype, layout, s) for s in (1, 2)]
+    for t in (t for x in rows for t in x):
+        for token, comp, value in ((0, D - 1, np.inf), (1, R, -np.inf), (2, D - 3, np.nan), (2, D - 2, np.inf)):
+            t[token, -1, comp] = value
+    (q, k, v), (dyq, dyk, _) = rows
+    dt, u, g = ref.torch_dtype(dtype), ref.UNIT[dtype], gen(torch, 3)
+    cos, sin = tables(torch, N + 5, R)
+    pos = torch.randint(1, N + 5, (N,), generator=g, device=dev).int() if R else None
+    w = [(1 + 0.3 * torch.randn(D, generator=g, device=dev)).to(dt) if norm else None for _ in range(2)]
+    how = dict(pos=pos, cos=cos, sin=sin, q_weight=w[0], k_weight=w[1], eps=1e-5, interleaved=inter)
+    out, grads = ([torch.zeros_like(t, memory_format=torch.contiguous_format) for t in (q, k)] for _ in range(2))
+    dw = [torch.zeros(D, device=dev) if norm else None for _ in range(2)]
+    ws = torch.empty(stride.stride_qk_norm_rope_backward_workspace_size(N, Hq, Hk, D), dtype=torch.uint8, device=dev)
+    stride.stride_qk_norm_rope(q, k, *out, **how)
+    clean = [qk_inputs(torch, N, Hq, Hk, D, dtype, layout, s)[:2] for s in (1, 2)]  # (rows without them)
+    # (x finite, dy not: a gradient of an infinite x is NaN throughout)
+    stride.stride_qk_norm_rope_backward(dyq, dyk, *clean[0], *grads, **how, dq_weight=dw[0], dk_weight=dw[1], workspace=ws)
+    c = Paged(torch, [3], [N], Hk, D, 4, dtype, False, 1, fill=0.0)
+    q_out = torch.zeros_like(out[0])
+    stride.stride_kv_append(k, v, *c.args, q=q, q_out=q_out, **how)
+    torch.cuda.synchronize()
+    pg, row = (torch.from_numpy(a[3:]).to(dev).long() for a in c.slots(0, 3 + N))
+    assert torch.equal(torch.nan_to_num(c.k[pg, row], 9.0), torch.nan_to_num(out[1], 9.0))
+    assert torch.equal(torch.nan_to_num(c.v[pg, row], 9.0), torch.nan_to_num(v, 9.0))
+    assert torch.equal(torch.nan_to_num(q_out, 9.0), torch.nan_to_num(out[0], 9.0))
+    cs, sn = (ref.f64(t[pos.long()]) for t in (cos, sin)) if R else (None, None)
+    with np.errstate(invalid="ignore"):
+        for x, dy, x0, wt, y, dx, dwt, H in ((q, dyq, clean[0][0], w[0], out[0], grads[0], dw[0], Hq),
+                                             (k, dyk, clean[0][1], w[1], out[1], grads[1], dw[1], Hk)):
+            wt = None if wt is None else ref.f64(wt)
+            want, size = ref.norm_rope(ref.f64(x), wt, 1e-5, cs, sn, inter)
+            the_same(y, want, u * np.abs(want) + (D + 20) * 2.0 ** -24 * size)
+            want, wantw, size, sizew = ref.norm_rope_backward(ref.f64(dy), ref.f64(x0), wt, 1e-5, cs, sn, inter)
+            the_same(dx, want, u * np.abs(want) + (D + 20) * 2.0 ** -24 * size)
+            if norm:
+                the_same(dwt, wantw, 2.0 ** -24 * (D + 40 + np.sqrt(N * H)) * sizew)
