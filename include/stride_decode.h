@@ -161,7 +161,9 @@ STRIDE_API size_t stride_tree_attention_workspace_size(int64_t n_tokens, int32_t
  * type, which is the only one that its operands may have beside such values;
  * their sum, and with it lse, takes them unrounded.  A component of out is so
  * within u sum_j p_j |v_j| of the one that 32-bit weights give, p = softmax(s), u
- * half a unit in the last place (2^-8 BF16, 2^-11 F16), before its own rounding.
+ * half a unit in the last place (2^-8 BF16, 2^-11 F16), before its own rounding
+ * (F16: plus 2^-38 max p sum_j |v_j|, its weights being whole from 2^-27 of the
+ * largest on).
  *
  * Types BF16, F16; D a multiple of 8, at most STRIDE_MAX_ATTENTION_DIM; the caches' base and strides whole 16-byte
  * vectors (q and out too); n_tokens times the group of query heads under 2^31 -

@@ -62,6 +62,16 @@ __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// A factor of the weights (at most 1) that go into a product.  Half loses bits below 2^-14 and all of them below 2^-25: as they
+// are, slots that score some 17 below the largest would be lost, and a long prefix may hold its whole mass there.  Times 2^15
+// they are whole from 2^-29 on.
+template <typename T>
+constexpr float kWeight = std::is_same<T, __half>::value ? 32768.f : 1.f;
+template <typename T>
+__device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
+  return pack<T>(lo * kWeight<T>, hi * kWeight<T>);
+}
+
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {
   const int n = real ? 16 : 0;  // (0: zeros)
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -286,8 +296,8 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
     // leaves would be half as many instructions again).  Their sum is of the unrounded ones.
 #pragma unroll
     for (int k = 0; k < kN / 2; ++k) {
-      const uint32_t a[4] = {pack<T>(s[2 * k][0], s[2 * k][1]), pack<T>(s[2 * k][2], s[2 * k][3]),
-                             pack<T>(s[2 * k + 1][0], s[2 * k + 1][1]), pack<T>(s[2 * k + 1][2], s[2 * k + 1][3])};
+      const uint32_t a[4] = {pack_weights<T>(s[2 * k][0], s[2 * k][1]), pack_weights<T>(s[2 * k][2], s[2 * k][3]),
+                             pack_weights<T>(s[2 * k + 1][0], s[2 * k + 1][1]), pack_weights<T>(s[2 * k + 1][2], s[2 * k + 1][3])};
 #pragma unroll
       for (int n = 0; n < D / 8; n += 2) {
         uint32_t b[4];
@@ -313,7 +323,8 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
         if (!whole) {
 #pragma unroll
           for (int n = 0; n < D / 8; ++n)
-            *reinterpret_cast<float2*>(slot + (size_t)r * D + n * 8 + (lane % 4) * 2) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+            *reinterpret_cast<float2*>(slot + (size_t)r * D + n * 8 + (lane % 4) * 2) =
+                make_float2(o[n][2 * h] * (1.f / kWeight<T>), o[n][2 * h + 1] * (1.f / kWeight<T>));
           if (wild) add_wild<T>(p, at.b, at.head, at.s.ctx, apart, wild_end, lim[h], bits[h], nullptr, slot + (size_t)r * D, (lane % 4) * 2, D, 8);
           if (lane % 4 == 0) {
             slot[(size_t)kRows * D + r] = m[h];
@@ -322,7 +333,7 @@ __global__ void __launch_bounds__(Ring<D>::kWarps * 32, 1) attention_few_kernel(
         } else if (i < at.s.n) {
           const int64_t token = at.s.off + i;
           const int head = at.head * g.group + rr % g.group;
-          const float by = l[h] == 0.f ? 0.f : 1.f / l[h];
+          const float by = l[h] == 0.f ? 0.f : (1.f / kWeight<T>) / l[h];
           T* out = static_cast<T*>(p.out) + token * p.out_tok + head * p.out_head;
 #pragma unroll
           for (int n = 0; n < D / 8; ++n) {

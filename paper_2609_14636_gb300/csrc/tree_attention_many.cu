@@ -17,14 +17,14 @@
 //         team has scores, weights and an output of its own, as if the tiles were
 //         two sequences, joined where the unit or the share ends: nothing of one
 //         tile waits for the other's.
-// The output is rescaled only where a row's maximum has grown by more than 2^8
-// since it was last (weights up to 256 fit both types as well as weights up to 1;
-// maximum and sum stay consistent either way).  The weights are rounded to the
-// values' type, as tcgen05 wants both operands of one type; their sum is of the
-// unrounded ones.  (What the rounding leaves, as a second operand, has no place in
-// tensor memory, and its product would be half as much work again.)  Slots past the end, and new tokens
-// that no row of the block sees, may hold anything: their values are zeroed in
-// shared memory before the second product, their scores are masked.  Exponentials
+// The output is rescaled only where a row's maximum has grown by more than 2^8 (half:
+// 2^2, see kGrowth) since it was last: maximum and sum stay consistent either way.
+// The weights are rounded to the values' type, as tcgen05 wants both operands of one
+// type; their sum is of the unrounded ones.  (What the rounding leaves, as a second
+// operand, has no place in tensor memory, and its product would be half as much work
+// again.)  Slots past the end, and new tokens that no row of the block sees, may hold
+// anything: their values are zeroed in shared memory before the second product, their
+// scores are masked.  Exponentials
 // and the moves between tensor memory and registers bound it: GB300, 32 / 8 heads of
 // 128, bf16: 32 trees of 13 tokens over up to 8,000 slots 128 us (5.5 TB/s), 4 chains
 // of 511 over up to 6,000 170 us (825 TFLOP/s).
@@ -48,7 +48,6 @@ constexpr int kRowWarps = 8;
 constexpr int kThreads = (kRowWarps + 3) * 32;
 constexpr int kExtra = 10;  // tiles that a unit's start and end cost (32 trees of 13 tokens: 2 145 us, 6 138, 8 130, 10 128, 14 129)
 constexpr int kMaxWorkers = 152;
-constexpr float kGrowth = 8.f;  // log2
 
 // ---- tensor memory and tcgen05 ----
 __device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr) {
@@ -129,6 +128,20 @@ template <>
 __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// What a row's maximum may have grown by (log2) before its reference follows, so that weights are up to 2^kGrowth; a factor of
+// the weights that go into a product.  Half loses bits below 2^-14 and all of them below 2^-25: as they are, slots that score
+// some 17 below the row's reference would be lost, and a long prefix may hold its whole mass there.  So its weights go in as
+// large as they may be, which leaves them whole from 2^-27 of the largest on.
+template <typename T>
+constexpr int kGrowth = std::is_same<T, __half>::value ? 2 : 8;
+template <typename T>
+constexpr float kWeight = std::is_same<T, __half>::value ? (float)(1 << (15 - kGrowth<T>)) : 1.f;
+template <typename T>
+__device__ __forceinline__ uint32_t pack_weights(float2 e) {
+  if constexpr (kWeight<T> != 1.f) e = __fmul2_rn(e, make_float2(kWeight<T>, kWeight<T>));
+  return pack<T>(e.x, e.y);
 }
 
 template <int D>
@@ -459,8 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int j = 0; j < kSlots; ++j) mx = fmaxf(mx, s[j] == -INFINITY ? -INFINITY : s[j] * scale2);
         }
-        // the row's reference grows at its first tile that sees anything, then by 2^8 at least
-        const bool grows = mx > m + kGrowth || (m == -INFINITY && mx > -INFINITY);
+        // the row's reference grows at its first tile that sees anything, then by 2^kGrowth at least
+        const bool grows = mx > m + (float)kGrowth<T> || (m == -INFINITY && mx > -INFINITY);
         float by = 1.f;
         if (grows) {
           by = ex2(m - mx);
@@ -477,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float2 x = __ffma2_rn(make_float2(s[2 * j], s[2 * j + 1]), sc, nr);
             const float2 e = make_float2(ex2(x.x), ex2(x.y));
             sum[j & 3] = __fadd2_rn(sum[j & 3], e);
-            w[j] = pack<T>(e.x, e.y);
+            w[j] = pack_weights<T>(e);
           }
           sum[0] = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
           l = sum[0].x + sum[0].y;
@@ -487,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float a = s[2 * j] == -INFINITY ? 0.f : ex2(fmaf(s[2 * j], scale2, -ref));
             const float c = s[2 * j + 1] == -INFINITY ? 0.f : ex2(fmaf(s[2 * j + 1], scale2, -ref));
             l += a + c;
-            w[j] = pack<T>(a, c);
+            w[j] = pack_weights<T>(make_float2(a, c));
           }
         }
         if (any_yet) {  // the product that read this team's last weights, and added to its output, is done
@@ -545,6 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float* slot = slots.of(blockIdx.x, starts);
         const float m0 = s_m[0][row], m1 = s_m[1][row], M = fmaxf(m0, m1);
         const float f0 = M == -INFINITY ? 1.f : ex2(m0 - M), f1 = M == -INFINITY ? 1.f : ex2(m1 - M);
+        const float o0 = f0 * (1.f / kWeight<T>), o1 = f1 * (1.f / kWeight<T>);
         const float sum = s_l[0][row] * f0 + s_l[1][row] * f1, inv = sum == 0.f ? 0.f : 1.f / sum;
         T* out = static_cast<T*>(p.out) + (have ? token * p.out_tok + head * p.out_head : 0);
 #pragma unroll
@@ -557,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           float v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j)
-            v[j] = (part_of[0] ? __uint_as_float(r0[j]) * f0 : 0.f) + (part_of[1] ? __uint_as_float(r1[j]) * f1 : 0.f);
+            v[j] = (part_of[0] ? __uint_as_float(r0[j]) * o0 : 0.f) + (part_of[1] ? __uint_as_float(r1[j]) * o1 : 0.f);
           if (have && !whole) {
 #pragma unroll
             for (int j = 0; j < 32; j += 8) store32(slot + (size_t)row * D + c * 32 + j, v + j);

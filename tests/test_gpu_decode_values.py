@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import decode_reference as ref
-from test_gpu_decode_step import Paged, env, gen, qk_inputs, tables  # noqa: F401
+from test_gpu_decode_step import Paged, check_attention, env, gen, qk_inputs, tables  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -147,3 +147,21 @@ def test_components_that_are_not_rotated_and_not_finite(env, case):  # noqa: F81
             the_same(dx, want, u * np.abs(want) + (D + 20) * 2.0 ** -24 * size)
             if norm:
                 the_same(dwt, wantw, 2.0 ** -24 * (D + 40 + np.sqrt(N * H)) * sizew)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n_new", [1, 40], ids=["few", "many"])
+@pytest.mark.parametrize("nats", [0, 10, 18])
+@pytest.mark.parametrize("sink", ["first", "last"])
+def test_attention_of_a_long_tail_under_one_large_score(env, dtype, n_new, nats, sink):  # noqa: F811
+    """One committed slot scores far above the others and has no value: the output is the tail's."""
+    torch, stride, dev = env
+    have, D = 20_000, 64
+    c = Paged(torch, [have], [n_new], 1, D, 16, dtype, False, 1)
+    pg, row = (torch.from_numpy(a).to(dev).long() for a in c.slots(0, have + n_new))
+    c.k[pg, row], c.v[pg, row] = 0.0, (1 + 0.2 * torch.rand((have + n_new, 1, D), generator=gen(torch, 2), device=dev)).to(c.v.dtype)
+    at = 0 if sink == "first" else have - 1
+    c.k[pg[at], row[at], 0, 0], c.v[pg[at], row[at]] = float(nats), 0.0
+    q = torch.zeros((n_new, 2, D), device=dev).to(c.k.dtype)
+    q[..., 0] = 1.0
+    check_attention(torch, stride, c, q, None, 1.0, dtype)
