@@ -473,7 +473,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int j = 0; j < kSlots; ++j) mx = fmaxf(mx, s[j] == -INFINITY ? -INFINITY : s[j] * scale2);
         }
         // the row's reference grows at its first tile that sees anything, then by 2^kGrowth at least
-        const bool grows = mx > m + (float)kGrowth<T> || (m == -INFINITY && mx > -INFINITY);
+        // (a difference: a sum may round to a larger reference, and half has no room for larger weights)
+        const bool grows = mx - m > (float)kGrowth<T>;
         float by = 1.f;
         if (grows) {
           by = ex2(m - mx);

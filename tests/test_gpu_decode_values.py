@@ -165,3 +165,25 @@ def test_attention_of_a_long_tail_under_one_large_score(env, dtype, n_new, nats,
     q = torch.zeros((n_new, 2, D), device=dev).to(c.k.dtype)
     q[..., 0] = 1.0
     check_attention(torch, stride, c, q, None, 1.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_of_scores_as_large_as_their_steps(env, dtype):  # noqa: F811
+    """Scores of 2^27 in units of ln 2, where 32 bits step by 16: a row's reference follows each step."""
+    torch, stride, dev = env
+    have, n_new, D, page = 40_000, 40, 64, 16
+    scale = np.float32(16 * np.log(2))
+    scale2 = np.float32(scale * np.float32(1.4426950408889634))
+    m = [float(np.float32(np.float32(2 ** 23 + b) * scale2)) for b in range(8)]
+    low = next(b for b in range(7) if (m[b] / 16) % 2 == 1 and m[b + 1] - m[b] == 16)
+    c = Paged(torch, [have], [n_new], 1, D, page, dtype, False, 1)
+    c.put(torch, gen(torch, 2))
+    pg, row = (torch.from_numpy(a).to(dev).long() for a in c.slots(0, have + n_new))
+    c.k[pg, row] = 0.0
+    c.k[pg, row, 0, 0], c.k[pg, row, 0, 1] = 4096.0, float(low)
+    tiles = np.random.default_rng(5).permutation(have // 64)[:have // 64 // 3]
+    at = torch.from_numpy(tiles * 64 + 17).to(dev)
+    c.k[pg[at], row[at], 0, 1] = float(low + 1)
+    q = torch.zeros((n_new, 2, D), device=dev).to(c.k.dtype)
+    q[..., 0], q[..., 1] = 2048.0, 1.0
+    check_attention(torch, stride, c, q, None, float(scale), dtype)
