@@ -42,6 +42,7 @@ extern "C" {
 #define STRIDE_MAX_HEAD_DIM 1024 /* D of the norm, rotation and append calls */
 #define STRIDE_MAX_ATTENTION_DIM 128 /* D of the attention call */
 #define STRIDE_MAX_TREE 64       /* drafted tokens of a sequence under a tree mask (one bit each) */
+#define STRIDE_MAX_TOP_P_VOCAB (1 << 23) /* V of a sampling call with a top_p: its masses are sums of 64 bits in units of 2^-40 */
 
 /* Head rows [n_tokens, n_heads, D]: unit stride along D, any other strides (in
  * elements), so q, k and v may be views of one fused projection. */
@@ -187,7 +188,9 @@ typedef struct stride_sample_params {
   float min_p_all;
 } stride_sample_params;
 
-/* Samples a token of each row of logits ([rows, ld], BF16, F16 or F32).
+/* Samples a token of each row of logits ([rows, ld], BF16, F16 or F32; V at
+ * most STRIDE_MAX_VOCAB, STRIDE_MAX_TOP_P_VOCAB where a top_p is given, as an array
+ * or a number below 1, and not all rows are of temperature 0).
  *
  * With m the row's largest logit, d_i = (x_i - m) / temperature and w_i =
  * exp(d_i), tokens ordered by falling logit, equal ones by rising index:

@@ -258,6 +258,7 @@ int stride_sample(const void* logits, int32_t dtype, int64_t ld, int64_t V, int3
   if (elem_bytes(dtype) == 0) return STRIDE_ERR_UNSUPPORTED_DTYPE;
   if (!params || rows < 0 || V < 1 || V > STRIDE_MAX_VOCAB || ld < V || (rows > 0 && (!logits || !tokens || !multiple(logits, elem_bytes(dtype)) || !multiple(noise, sizeof(float))))) return STRIDE_ERR_INVALID_ARG;
   const bool greedy = !params->temperature && params->temperature_all == 0.f;
+  if (!greedy && V > STRIDE_MAX_TOP_P_VOCAB && (params->top_p || params->top_p_all < 1.f)) return STRIDE_ERR_INVALID_ARG;
   if (!greedy && ((rows > 0 && !noise) || ld_noise < V)) return STRIDE_ERR_INVALID_ARG;
   if (!params->temperature && !(params->temperature_all >= 0.f && isfinite(params->temperature_all))) return STRIDE_ERR_INVALID_ARG;
   if ((!params->top_p && isnan(params->top_p_all)) || (!params->min_p && isnan(params->min_p_all))) return STRIDE_ERR_INVALID_ARG;

@@ -51,7 +51,8 @@ constexpr int kLoads = 6;      // vectors that a thread has in flight
 constexpr int kDepth = 6;
 constexpr int kGroups = 1024;  // groups of threads at most
 constexpr int kList = 1024;    // tokens that the first CTA sorts at most
-constexpr float kOne = 1099511627776.f;  // 2^40, the fixed-point 1 of masses
+constexpr float kOne = 1099511627776.f;  // 2^40, the fixed-point 1 of masses (weights are at most 1)
+static_assert((uint64_t)STRIDE_MAX_TOP_P_VOCAB << 40 <= (uint64_t)1 << 63, "a row's mass fits in 64 bits, with room for rounding");
 constexpr int kPivots = 7;
 constexpr int kUsual = 96;     // groups that a top_p without top_k asks to reach the bound
 constexpr int kMaxCluster = 8;

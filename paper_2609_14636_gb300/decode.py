@@ -16,8 +16,8 @@ import ctypes
 import paper_2609_14636_gb300 as _s
 
 __all__ = [
-    "DTYPE_F16", "DEV_POSITION", "DEV_NO_TOKEN", "MAX_HEAD_DIM", "MAX_ATTENTION_DIM", "MAX_TREE", "stride_qk_norm_rope",
-    "stride_qk_norm_rope_backward", "stride_qk_norm_rope_backward_workspace_size", "stride_kv_append",
+    "DTYPE_F16", "DEV_POSITION", "DEV_NO_TOKEN", "MAX_HEAD_DIM", "MAX_ATTENTION_DIM", "MAX_TREE", "MAX_TOP_P_VOCAB",
+    "stride_qk_norm_rope", "stride_qk_norm_rope_backward", "stride_qk_norm_rope_backward_workspace_size", "stride_kv_append",
     "stride_tree_attention", "stride_tree_attention_workspace_size", "stride_sample",
 ]
 
@@ -26,6 +26,7 @@ DEV_POSITION, DEV_NO_TOKEN = 0x8, 0x10
 MAX_HEAD_DIM = 1024  # STRIDE_MAX_HEAD_DIM
 MAX_ATTENTION_DIM = 128  # STRIDE_MAX_ATTENTION_DIM
 MAX_TREE = 64  # STRIDE_MAX_TREE
+MAX_TOP_P_VOCAB = 1 << 23  # STRIDE_MAX_TOP_P_VOCAB
 
 _P, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 

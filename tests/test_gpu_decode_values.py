@@ -187,3 +187,21 @@ def test_attention_of_scores_as_large_as_their_steps(env, dtype):  # noqa: F811
     q = torch.zeros((n_new, 2, D), device=dev).to(c.k.dtype)
     q[..., 0], q[..., 1] = 2048.0, 1.0
     check_attention(torch, stride, c, q, None, float(scale), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sample_top_p_of_the_largest_flat_row(env, dtype):  # noqa: F811
+    """Equal logits: top_p keeps the first of them, whose masses add up to nearly 2^63 units."""
+    torch, stride, dev = env
+    V, top_p = stride.MAX_TOP_P_VOCAB, [0.8, 0.9, 0.95]
+    x = torch.full((3, V), 1.5, device=dev).to(ref.torch_dtype(dtype))
+    noise = 1 + torch.rand((3, V), generator=gen(torch, 2), device=dev)
+    kept = [int(np.ceil(p * V)) for p in top_p]
+    for r, n in enumerate(kept):  # (a hundred-thousandth to either side of the last one)
+        noise[r, n - 90], noise[r, n + 90] = 0.5, 0.1
+    tokens, logp = torch.zeros(3, dtype=torch.int32, device=dev), torch.zeros(3, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    stride.stride_sample(x, noise, tokens, top_p=torch.tensor(top_p, device=dev), logp=logp, dev_status=status)
+    assert int(status) == 0
+    assert tokens.tolist() == [n - 90 for n in kept]
+    assert (np.abs(ref.f64(logp) + np.log(kept)) <= 3e-5).all()  # (ln's own error, and the hundred-thousandth)
