@@ -775,7 +775,7 @@ __device__ __forceinline__ bool pick_among(const Share<T>& sh, const Weight& wei
   Shared& s = shared();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const Pick limit = last;
-  const bool all = limit.i < 0;  // (no limit yet)
+  const bool all = limit.key == Key<T>::of(lowest<T>());  // (no limit yet; its index alone does not say so: see tie_cutoff)
   __syncthreads();
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
@@ -887,7 +887,7 @@ __device__ __forceinline__ bool last_by_mass(const Share<T>& sh, const Weight& w
                                              cg::cluster_group& cluster) {
   const float scale = kLog2e / weight.T, want = (float)goal * (1.f / kOne);
   const Pick limit = last;
-  const bool all = limit.i < 0;  // (no limit yet)
+  const bool all = limit.key == Key<T>::of(lowest<T>());  // (no limit yet; its index alone does not say so: see tie_cutoff)
   float lo = low, hi = INFINITY, above = 0.f;  // mass(x >= hi) = above < goal <= mass(x >= lo)
   for (int pass = 0; pass < 3; ++pass) {
     const float step = ((hi < INFINITY ? hi : weight.m) - lo) * (1.f / (kPivots + 1));

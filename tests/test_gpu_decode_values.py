@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import decode_reference as ref
-from test_gpu_decode_step import Paged, check_attention, env, gen, qk_inputs, tables  # noqa: F401
+from test_gpu_decode_step import Paged, check_attention, check_sample, env, gen, qk_inputs, tables  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -205,3 +205,19 @@ def test_sample_top_p_of_the_largest_flat_row(env, dtype):  # noqa: F811
     assert int(status) == 0
     assert tokens.tolist() == [n - 90 for n in kept]
     assert (np.abs(ref.f64(logp) + np.log(kept)) <= 3e-5).all()  # (ln's own error, and the hundred-thousandth)
+
+
+def test_sample_top_p_of_what_a_top_k_leaves_of_ties(env):  # noqa: F811
+    """The last of top_k tokens is the second of four equal ones, which lie far apart, and many that are hardly smaller follow; a
+    top_p of nearly 1 keeps all that top_k leaves.  The tokens that come next would win if they were kept."""
+    torch, stride, dev = env
+    rows, V, top_k, below = 32, 40_000, 2001, 1500
+    rng = np.random.default_rng(6)
+    x, noise = torch.full((rows, V), -30.0), torch.empty((rows, V)).exponential_(generator=torch.Generator().manual_seed(7)) + 0.1
+    for r in range(rows):
+        value = np.concatenate([0.001 + rng.random(top_k - 2), np.zeros(4), -0.001 - 0.02 * rng.random(below)])
+        ties = 10 + r, 50 + r, V - 5000 - r, V - 10 - r
+        at = np.concatenate([rng.choice(np.arange(5100, V - 10_000), top_k - 2, replace=False), ties, rng.choice(np.arange(100, 4900), below, replace=False)])
+        x[r, at] = torch.from_numpy(value.astype(np.float32))
+        noise[r, at[top_k:]] = 1e-4  # (not kept)
+    check_sample(torch, stride, x.to(dev), noise.to(dev), 1.0, [top_k] * rows, [float(np.float32(1 - 2.0 ** -24))] * rows, 0.0)
