@@ -1006,7 +1006,7 @@ __device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& s
     for (int i = 0; i < N; ++i) {
       kept += w[i];
       w[i] = __fdividef(w[i], e[i]);
-      if (w[i] > best.v) best = {w[i], i0 + i};
+      if (w[i] > 0.f) take(best, w[i], i0 + i);  // (a lane's vectors come in no order of index: see each_of)
     }
   });
   exact_race(p, sh, noise, q.r, weight, true, best, kept, cluster);

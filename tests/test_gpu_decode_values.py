@@ -221,3 +221,20 @@ def test_sample_top_p_of_what_a_top_k_leaves_of_ties(env):  # noqa: F811
         x[r, at] = torch.from_numpy(value.astype(np.float32))
         noise[r, at[top_k:]] = 1e-4  # (not kept)
     check_sample(torch, stride, x.to(dev), noise.to(dev), 1.0, [top_k] * rows, [float(np.float32(1 - 2.0 ** -24))] * rows, 0.0)
+
+
+@pytest.mark.parametrize("rows,min_p,top_p", [(1, 0.5, 1.0), (305, 0.5, 1.0), (305, 0.5, 0.999)])
+def test_sample_equal_ratios(env, rows, min_p, top_p):  # noqa: F811
+    """Equal logits and equal noise, wherever they lie in a row: the lowest index is drawn."""
+    torch, stride, dev = env
+    V, rng = 151_936, np.random.default_rng(rows)
+    x = torch.randn((rows, V), generator=gen(torch, 4), device=dev).clamp_(max=4).bfloat16()
+    at = rng.integers(0, V, (rows, 3))
+    for r in range(rows):  # (in half of the rows in places that one thread comes to out of order)
+        if r % 2 == 0:
+            lane = r // 2 % 6
+            at[r] = 8 * (16_384 + 512 * lane), 8 * (512 * lane + 1) + 3, 8 * (512 * lane + 2) + 1
+    x[torch.arange(rows, device=dev)[:, None], torch.from_numpy(at).to(dev)] = 8.0
+    tokens = torch.zeros(rows, dtype=torch.int32, device=dev)
+    stride.stride_sample(x, torch.ones((rows, V), device=dev), tokens, min_p=min_p, top_p=top_p)
+    assert tokens.tolist() == at.min(1).tolist()
