@@ -309,6 +309,10 @@ struct Weight {
   __device__ __forceinline__ float operator()(float x) const { return expf(log(x)); }
 };
 
+// What a difference of logits is multiplied with for an exponent of 2.  (Below a temperature of 2^-127 the quotient is infinite,
+// and times a difference of 0 not a number: the largest finite one leaves the largest logits alone as well.)
+__device__ __forceinline__ float exponent_scale(float T) { return fminf(kLog2e / T, FLT_MAX); }
+
 __device__ __forceinline__ float block_sum(float x) {
   Shared& s = shared();
 #pragma unroll
@@ -677,7 +681,7 @@ __device__ __noinline__ void race_all(const SampleParams& p, const Share<T>& sh,
   Shared& s = shared();
   constexpr int N = Vec<T>::N, U = N == 8 ? 2 : 4;
   const int tid = threadIdx.x;
-  const float scale = kLog2e / temp;
+  const float scale = exponent_scale(temp);
   const bool whole = (reinterpret_cast<uintptr_t>(noise + sh.index(0)) & 15) == 0;
   Best best = {0.f, INT32_MAX};
   Running a;
@@ -885,7 +889,7 @@ __device__ __forceinline__ void cluster_sums(float (&sum)[kPivots], cg::cluster_
 template <typename T>
 __device__ __forceinline__ bool last_by_mass(const Share<T>& sh, const Weight& weight, float own, float low, uint64_t goal, Pick& last,
                                              cg::cluster_group& cluster) {
-  const float scale = kLog2e / weight.T, want = (float)goal * (1.f / kOne);
+  const float scale = exponent_scale(weight.T), want = (float)goal * (1.f / kOne);
   const Pick limit = last;
   const bool all = limit.key == Key<T>::of(lowest<T>());  // (no limit yet; its index alone does not say so: see tie_cutoff)
   float lo = low, hi = INFINITY, above = 0.f;  // mass(x >= hi) = above < goal <= mass(x >= lo)
@@ -992,7 +996,7 @@ __device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& s
   }
   Best best = {0.f, INT32_MAX};
   float kept = 0.f;
-  const float scale = kLog2e / q.temp;
+  const float scale = exponent_scale(q.temp);
   sh.each_of(own_key >= last.key && q.own > -INFINITY && ex2((q.own - weight.m) * scale) >= q.least, [&](int32_t v, const Vec<T>& x) {
     const int32_t i0 = sh.index(v);
     float w[N], e[N];  // (the noise of the kept ones, asked for together)
@@ -1075,7 +1079,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   if (need_all)
     sh.template each<kLoads>([&](int32_t, const Vec<T>& x) {
       float w[N];
-      run_on(a, x, w, kLog2e / temp);
+      run_on(a, x, w, exponent_scale(temp));
     });
   else
     sh.template each<kLoads>([&](int32_t, const Vec<T>& x) { a.m = max_nan(a.m, vec_max(x)); });
@@ -1120,7 +1124,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const float least = fminf(min_p, 1.f);
   const uint32_t none = Key<T>::of(lowest<T>()), first = Key<T>::of(static_cast<T>(top)), own_key = Key<T>::of(static_cast<T>(own));
   float all = 0.f, z = 0.f;  // the mass of the share's tokens, of the row's
-  if (need_all) all = block_sum(own == -INFINITY ? 0.f : a.z * ex2((own - top) * (kLog2e / temp)));
+  if (need_all) all = block_sum(own == -INFINITY ? 0.f : a.z * ex2((own - top) * exponent_scale(temp)));
 
   if (by_list) {
     // The bound: the largest key that at least `reach` of the groups reach (to within an eighth of them), by bisection;

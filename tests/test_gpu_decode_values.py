@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import decode_reference as ref
-from test_gpu_decode_step import Paged, check_attention, check_sample, env, gen, qk_inputs, tables  # noqa: F401
+from test_gpu_decode_step import Paged, check_attention, check_sample, env, gen, logits, qk_inputs, tables  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -238,3 +238,15 @@ def test_sample_equal_ratios(env, rows, min_p, top_p):  # noqa: F811
     tokens = torch.zeros(rows, dtype=torch.int32, device=dev)
     stride.stride_sample(x, torch.ones((rows, V), device=dev), tokens, min_p=min_p, top_p=top_p)
     assert tokens.tolist() == at.min(1).tolist()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T", [1e-45, 1e-40, 4e-39, 2e-38])
+def test_sample_at_the_smallest_temperatures(env, dtype, T):  # noqa: F811
+    """The largest logits alone, by their noise."""
+    torch, stride, dev = env
+    x, noise = logits(torch, 8, 5003, dtype, 5)
+    x = x.round()
+    x[::2] -= x[::2].amax(1, keepdim=True)  # (rows whose largest is 0, and others)
+    for k, p, m in ((0, 1.0, 0.0), (3, 1.0, 0.0), (2000, 0.5, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.3)):
+        check_sample(torch, stride, x, noise, [T] * 8, [k] * 8, [p] * 8, [m] * 8)
