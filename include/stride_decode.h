@@ -36,7 +36,7 @@ extern "C" {
 
 #define STRIDE_DTYPE_F16 2 /* IEEE half; this header's calls only */
 
-#define STRIDE_DEV_POSITION 0x8 /* a position outside the rotation's tables: that token's rows are NaN */
+#define STRIDE_DEV_POSITION 0x8 /* a position outside the rotation's tables: that token's rows are NaN, and sums over them */
 #define STRIDE_DEV_NO_TOKEN 0x10 /* a row that has no token to sample: token -1, NaN log-prob */
 
 #define STRIDE_MAX_HEAD_DIM 1024 /* D of the norm, rotation and append calls */
@@ -156,7 +156,9 @@ STRIDE_API size_t stride_tree_attention_workspace_size(int64_t n_tokens, int32_t
  * STRIDE_DEV_BAD_LAYOUT, that sequence's rows NaN).  A row that sees nothing:
  * out 0, lse -inf.  Keys and values that a row does not see may hold anything,
  * NaN and infinities too: they change nothing in it.  A slot without a page:
- * STRIDE_DEV_BAD_LAYOUT and NaN rows.
+ * STRIDE_DEV_BAD_LAYOUT and NaN rows.  STRIDE_DEV_TIMEOUT (a wait inside the
+ * kernel ran out: not known to happen): out and lse of the whole call hold
+ * nothing of use, and some of their rows may not have been written.
  *
  * The weights exp(s_j - max s) go into the second product rounded to the rows'
  * type, which is the only one that its operands may have beside such values;
@@ -202,10 +204,15 @@ typedef struct stride_sample_params {
  * log-probability it was drawn with (temperature 0: the first token of the
  * order, logp 0; noise is not read, and may be NULL if temperature_all is 0 and
  * no array is given).
- * A logit of -inf is never drawn (nor the type's lowest value, unless it is
- * the row's largest).  A row without a finite logit, with a NaN or +inf
- * logit, a NaN, negative or infinite temperature, a NaN top_p or min_p, or no
- * positive ratio: token -1, logp NaN, STRIDE_DEV_NO_TOKEN. */
+ * A logit of -inf is never drawn.  The type's lowest value is a logit like any
+ * other: as a mask it has weight 0 where it lies 104 temperatures or more below
+ * the row's largest logit (F16's -65504 beside logits around 0: at temperatures
+ * up to 600).  Masses, and the weights that min_p is compared with, are of
+ * approximate exponentials: a token whose weight is within 1e-5 (relative) of min_p
+ * may fall on either side, as may one before which the mass is within 1e-5 of
+ * top_p.  A row without a finite logit, with a NaN or +inf logit, a NaN, negative
+ * or infinite temperature, a NaN top_p or min_p, or no positive ratio: token -1,
+ * logp NaN, STRIDE_DEV_NO_TOKEN. */
 STRIDE_API int stride_sample(const void* logits, int32_t dtype, int64_t ld, int64_t V, int32_t rows,
                              const float* noise, int64_t ld_noise, const stride_sample_params* params,
                              int32_t* tokens, float* logp, int32_t* dev_status, void* stream);

@@ -949,7 +949,8 @@ struct Row {
   bool cut_k, cut_p;
 };
 
-// The general way: the threshold by histograms, then the race.
+// The general way: the threshold by histograms, then the race.  (Its weights are approximate, also those that min_p is compared
+// with and that the kept mass sums up: 2^-22, and the rounding of an exponent of up to 128. The winner's is computed again.)
 template <typename T>
 __device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& sh, const float* noise, const Weight& weight, const Row& q,
                                         cg::cluster_group& cluster) {
@@ -1016,9 +1017,11 @@ __device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& s
   exact_race(p, sh, noise, q.r, weight, true, best, kept, cluster);
 }
 
-// The n-th row of the call (of kThreads at most) if those without a top_k, which
-// take several times as long as the others, come first: started last, they were what
-// the call waited for.
+// The n-th row of the call (of kThreads at most: a thread tells each row's kind) if
+// those without a top_k come first.  With a top_p they take several times as long as
+// the others: started last, they were what the call waited for.  (Nothing is lost
+// where they are short after all; a row whose top_k is past the list is long, too, and
+// comes in its turn.)
 __device__ __forceinline__ int32_t long_first(const SampleParams& p, int32_t n) {
   Shared& s = shared();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;

@@ -250,3 +250,16 @@ def test_sample_at_the_smallest_temperatures(env, dtype, T):  # noqa: F811
     x[::2] -= x[::2].amax(1, keepdim=True)  # (rows whose largest is 0, and others)
     for k, p, m in ((0, 1.0, 0.0), (3, 1.0, 0.0), (2000, 0.5, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.3)):
         check_sample(torch, stride, x, noise, [T] * 8, [k] * 8, [p] * 8, [m] * 8)
+
+
+@pytest.mark.parametrize("T", [1.0, 600.0, 1000.0, 60_000.0])
+def test_sample_lowest_value_of_half(env, T):  # noqa: F811
+    """A mask of -65504 is a logit: its weight is 0 up to a temperature of 600, and counts from some 630 on."""
+    torch, stride, dev = env
+    x, noise = logits(torch, 12, 3001, "f16", 8)
+    x[:, ::3] = torch.finfo(x.dtype).min
+    noise[:, ::3] = 1e-30
+    for k, p, m in ((0, 1.0, 0.0), (2500, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 1e-4)):
+        tokens, _ = check_sample(torch, stride, x, noise, [T] * 12, [k] * 12, [p] * 12, [m] * 12)
+        if T <= 600:
+            assert (tokens % 3 != 0).all()
