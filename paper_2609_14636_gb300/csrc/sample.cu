@@ -1007,11 +1007,19 @@ __device__ __noinline__ void race_above(const SampleParams& p, const Share<T>& s
       if (!kept_by(last, Key<T>::of(x.e[i]), i0 + i) || w[i] < q.least) w[i] = 0.f;
       e[i] = w[i] > 0.f ? __ldg(noise + i0 + i) : 1.f;
     }
+    float mx = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       kept += w[i];
       w[i] = __fdividef(w[i], e[i]);
-      if (w[i] > 0.f) take(best, w[i], i0 + i);  // (a lane's vectors come in no order of index: see each_of)
+      mx = fmaxf(mx, w[i]);
+    }
+    if (mx > 0.f && mx >= best.v) {  // (a lane's vectors come in no order of index: see each_of)
+      int32_t at = INT32_MAX;
+#pragma unroll
+      for (int i = N - 1; i >= 0; --i)
+        if (w[i] == mx) at = i0 + i;
+      take(best, mx, at);
     }
   });
   exact_race(p, sh, noise, q.r, weight, true, best, kept, cluster);
