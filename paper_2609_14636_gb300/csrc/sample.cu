@@ -28,8 +28,9 @@
 //   counting.  One more pass races what is kept.
 //   All sums that atomics make are integers: their order changes nothing.
 // Noise is read for kept tokens alone.  GB300, rows of 151,936 bf16 logits: one row
-// with a top_k of 50 10 us, 256 of them 33 (2.4 TB/s); 256 rows of mixed parameters
-// 87; 512 uncut rows of 32,000 fp32 46 (2.9 TB/s).
+// with a top_k of 20 and a top_p 9.2 us; 256 with a top_k of 50 37 (2.1 TB/s); 256 of
+// mixed parameters 92; 256 with a top_p alone 233; 512 uncut rows of 32,000 fp32 45
+// (2.9 TB/s).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -123,7 +123,9 @@ size_t attention_workspace_bytes(int64_t, int, int, int D) {
 }
 
 cudaError_t launch_tree_attention(const AttentionParams& p, int dtype, int sms, cudaStream_t stream) {
-  // (rows of an ordinary sequence: only the device knows how many each has)
+  // By the mean of rows a sequence, as only the device knows how many each has.  Where they are very unequal the kernel for few
+  // rows takes long chains, too, and reads their prefixes once for 16 rows: a chain of 511 tokens over 6,000 slots 84 us, 255
+  // single tokens over 1,000 217, both in one call 542.
   const int64_t rows = ((p.n_tokens + p.cache.n_seqs - 1) / p.cache.n_seqs) * (p.Hq / p.cache.n_heads);
   if (rows > 16 && attention_many_takes(p)) return launch_attention_many(p, dtype, sms, stream);
   return launch_attention_few(p, dtype, sms, stream);

@@ -12,7 +12,7 @@
 // and an accumulator to fetch); maximum, sum and output stay in registers until the
 // unit or the share ends.  GB300, 32 / 8 heads of 128, bf16: 256 sequences of up to
 // 4,096 slots 467 us (5.9 TB/s), one of 131,072 102 us (5.2 TB/s), with 16 / 2
-// heads one of 37 7.7 us.
+// heads one of 37 7.8 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -24,10 +24,11 @@
 // operand, has no place in tensor memory, and its product would be half as much work
 // again.)  Slots past the end, and new tokens that no row of the block sees, may hold
 // anything: their values are zeroed in shared memory before the second product, their
-// scores are masked.  Exponentials
-// and the moves between tensor memory and registers bound it: GB300, 32 / 8 heads of
-// 128, bf16: 32 trees of 13 tokens over up to 8,000 slots 128 us (5.5 TB/s), 4 chains
-// of 511 over up to 6,000 170 us (825 TFLOP/s).
+// scores are masked.  What bounds it is the latency of a team's chain of steps for a
+// tile (wait, load, maximum, exponentials, store, arrive): in chains the tensor pipe
+// is 40 % busy, at 1.5 instructions a clock.  GB300, 32 / 8 heads of 128, bf16: 32
+// trees of 13 tokens over up to 8,000 slots 128 us (5.5 TB/s), 4 chains of 511 over up
+// to 6,000 170 us (825 TFLOP/s).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
