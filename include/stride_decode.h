@@ -161,16 +161,20 @@ STRIDE_API size_t stride_tree_attention_workspace_size(int64_t n_tokens, int32_t
  * nothing of use, and some of their rows may not have been written.
  *
  * The weights exp(s_j - max s) go into the second product rounded to the rows'
- * type, which is the only one that its operands may have beside such values;
- * their sum, and with it lse, takes them unrounded.  A component of out is so
+ * type (both operands of a tensor-core product are of one); their sum, and with
+ * it lse, takes them unrounded.  A component of out is so
  * within u sum_j p_j |v_j| of the one that 32-bit weights give, p = softmax(s), u
  * half a unit in the last place (2^-8 BF16, 2^-11 F16), before its own rounding
  * (F16: plus 2^-38 max p sum_j |v_j|, its weights being whole from 2^-27 of the
  * largest on).
  *
- * Types BF16, F16; D a multiple of 8, at most STRIDE_MAX_ATTENTION_DIM; the caches' base and strides whole 16-byte
- * vectors (q and out too); n_tokens times the group of query heads under 2^31 -
- * 256.  lse: float [n_tokens, n_heads] or NULL. */
+ * One kernel takes the whole call, chosen by its mean of rows a sequence: a long
+ * chain is best not in one call with many single tokens.
+ *
+ * Types BF16, F16; D a multiple of 8, at most STRIDE_MAX_ATTENTION_DIM; the
+ * caches' base and strides whole 16-byte vectors (q and out too); n_tokens times
+ * the group of query heads under 2^31 - 256.  lse: float [n_tokens, n_heads] or
+ * NULL. */
 STRIDE_API int stride_tree_attention(const stride_head_rows* q, const stride_head_rows* out, float* lse,
                                      int32_t dtype, int64_t n_tokens, int32_t D, float scale,
                                      const uint64_t* tree_mask, const stride_paged_cache* cache,
