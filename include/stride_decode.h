@@ -9,6 +9,11 @@
  *                                   and rotation on the way (serving);
  *   stride_tree_attention           attention of one token, a chain or a tree
  *                                   of drafted tokens over that cache;
+ *   stride_attention_mass           what attention weight each cached slot gets,
+ *                                   added up over steps;
+ *   stride_kv_evict                 the slots of most weight into fewer pages;
+ *   stride_logit_controls           penalties for repeated tokens, biases and
+ *                                   grammar masks on logits;
  *   stride_sample                   temperature, top-k, top-p and min-p from
  *                                   given random numbers.
  *
@@ -38,6 +43,8 @@ extern "C" {
 
 #define STRIDE_DEV_POSITION 0x8 /* a position outside the rotation's tables: that token's rows are NaN, and sums over them */
 #define STRIDE_DEV_NO_TOKEN 0x10 /* a row that has no token to sample: token -1, NaN log-prob */
+
+#define STRIDE_DEV_BAD_CONTROL 0x20 /* a row's penalty that stride_logit_controls does not take: that row is NaN */
 
 #define STRIDE_MAX_HEAD_DIM 1024 /* D of the norm, rotation and append calls */
 #define STRIDE_MAX_ATTENTION_DIM 128 /* D of the attention call */
@@ -180,6 +187,121 @@ STRIDE_API int stride_tree_attention(const stride_head_rows* q, const stride_hea
                                      const uint64_t* tree_mask, const stride_paged_cache* cache,
                                      int32_t* dev_status, void* workspace, size_t workspace_bytes,
                                      void* stream);
+
+/* Attention weight of cached slots (host struct): float [n_seqs, heads, slots]
+ * of unit stride along the slots, other strides in elements.  Slot s is the
+ * sequence's s-th, not a place in a page: sequences that share pages of a prefix
+ * have weights of their own. */
+typedef struct stride_slot_mass {
+  float* data;
+  int64_t seq_stride;
+  int64_t head_stride;
+  int64_t slots;
+} stride_slot_mass;
+
+/* Adds the attention weights of the call's new tokens to their sequences' slots.
+ * Arguments as of stride_tree_attention, after it: lse is what it wrote.  For
+ * sequence b and kv head h, over the new tokens i and the query heads g of h's
+ * group, where i sees slot j:
+ *   w_j = sum_i sum_g exp(scale * q_ig . k_j - lse_ig)
+ *   mass_j = decay * mass_j + w_j   for the ctx_len[b] committed slots
+ *            w_j                    for those of the new tokens
+ * Slots past those, and sequences without new tokens, stay as they are.  decay >= 0; with 0
+ * mass is not read (it may hold anything).  A row whose lse is -inf sees nothing
+ * and adds nothing; keys that a row does not see may hold anything and change nothing
+ * in its weights.  Sums are held in 32 bits in an order that does not depend on
+ * the other sequences of the call: the same call gives the same bits.
+ *
+ * A slot without a page: NaN and STRIDE_DEV_BAD_LAYOUT.  Sequences of a length that
+ * the block table or mass->slots does not hold, or, under a tree mask, of more than
+ * STRIDE_MAX_TREE new tokens: STRIDE_DEV_BAD_LAYOUT, their mass stays as it is.
+ * STRIDE_DEV_TIMEOUT (as of stride_tree_attention): masses of the whole call hold
+ * nothing of use.
+ *
+ * To let a prompt's last tokens alone vote, pass their rows of q and lse with ctx_len
+ * moved on over the others and a decay of 0.
+ *
+ * Types and bounds of q and the cache as of stride_tree_attention (cache->v is not
+ * used and may be NULL), n_tokens times the group of query heads at most 2^30; lse:
+ * float [n_tokens, q->n_heads]. */
+STRIDE_API int stride_attention_mass(const stride_head_rows* q, const float* lse, int32_t dtype, int64_t n_tokens,
+                                     int32_t D, float scale, const uint64_t* tree_mask,
+                                     const stride_paged_cache* cache, float decay, const stride_slot_mass* mass,
+                                     int32_t* dev_status, void* stream);
+
+/* What stride_kv_evict keeps of each sequence and kv head (host struct). */
+typedef struct stride_evict_params {
+  const int32_t* budget; /* [n_seqs] slots that remain, or NULL: budget_all for each.  Negative: the sequence is left out */
+  int32_t budget_all;
+  int32_t sink;          /* >= 0: of them, the first ones */
+  int32_t recent;        /* >= 0: of them, the last ones */
+  int32_t most;          /* slots that a row of `kept` and of mass_to holds */
+} stride_evict_params;
+
+/* Copies of each sequence of `from`, for each kv head by itself, the slots that
+ * remain into the pages of `to`, in order.
+ *
+ * With n = from->ctx_len[b] and m = min(n, budget): the first a = min(m, sink)
+ * slots, the last z = min(m - a, recent), and the m - a - z others of the largest
+ * mass (ties: the lower slot; a NaN is below every number).  Slot number i of those,
+ * counted from 0 in rising order of slots, goes to slot i of sequence b in `to`, and
+ *   kept[b, h, i] = its slot in `from`,  mass_to[b, h, i] = its mass,  new_len[b] = m.
+ * kept: int32 [n_seqs, heads, most] and required; mass_to: stride_slot_mass of at least
+ * `most` slots, nullable, not over mass.  What lies past m in kept, mass_to and the pages stays as
+ * it is, and `from` is read only: pages that several sequences share (the prefix
+ * that restarts reuse) stay whole.  So no page of `to` may be one that the call reads;
+ * the pools may be the same.  The heads' slots hold different tokens from there on,
+ * which attention does not mind (keys are rotated before they are cached): the next
+ * tokens' positions go on counting, ctx_len goes on from new_len.
+ *
+ * A sequence that is left out: new_len[b] = ctx_len[b], nothing else is touched.  A
+ * negative ctx_len, one that from's block table or mass->slots does not hold, an m above most or
+ * what to's block table holds: STRIDE_DEV_BAD_LAYOUT, new_len[b] = -1, nothing else
+ * is touched.  A slot without a page, on either side: STRIDE_DEV_BAD_LAYOUT, its row is
+ * not copied.
+ *
+ * Types BF16, F16, F32; D <= STRIDE_MAX_HEAD_DIM; `to` has from's heads and sequences (page sizes and
+ * strides may differ); tok_off of both and to->ctx_len are not used and may be NULL. */
+STRIDE_API int stride_kv_evict(const stride_paged_cache* from, const stride_slot_mass* mass, const stride_paged_cache* to,
+                               int32_t dtype, int32_t D, const stride_evict_params* how, int32_t* new_len,
+                               int32_t* kept, const stride_slot_mass* mass_to, int32_t* dev_status, void* stream);
+
+/* What stride_logit_controls does to a row of logits (host struct); every part
+ * may be absent.  Per-row numbers are arrays [rows] or, where NULL, one value for all. */
+typedef struct stride_logit_rules {
+  const int32_t* history;     /* [rows, history_stride] tokens of each row's sequence; NULL: no penalties */
+  int64_t history_stride;
+  int32_t history_most;       /* columns that a row has */
+  const int32_t* history_len; /* [rows], 0 <= history_len <= history_most */
+  const int32_t* prompt_len;  /* [rows] of which the prompt's; NULL: 0 */
+  const float* repetition;    /* > 0; 1: none */
+  float repetition_all;
+  const float* frequency;     /* 0: none */
+  float frequency_all;
+  const float* presence;      /* 0: none */
+  float presence_all;
+  const int32_t* bias_off;    /* [rows + 1] each row's entries of bias_token and bias; NULL: no biases */
+  const int32_t* bias_token;  /* [n_bias] */
+  const float* bias;          /* [n_bias] */
+  int32_t n_bias;
+  const uint32_t* allowed;    /* [rows, allowed_stride]: bit j % 32 of word j / 32 set, token j is allowed; NULL: all */
+  int64_t allowed_stride;     /* words; 0: one row for all */
+} stride_logit_rules;
+
+/* out = logits ([rows, ld], [rows, ld_out]; BF16, F16, F32; V at most STRIDE_MAX_VOCAB)
+ * with these in turn, in 32 bits, rounded once:
+ *   x = x > 0 ? x / repetition : x * repetition   tokens of the history
+ *   x = x - frequency * count - presence          tokens generated (past the prompt) `count` > 0 times
+ *   x = x + bias                                  listed tokens (of several entries the last)
+ *   x = -inf                                      tokens that are not allowed
+ * out may be logits, and must not overlap them otherwise; in place, logits that nothing applies to are
+ * not read.  Separate, the raw logits stay for the scoring call.  A negative token in a history
+ * or a list is padding.  One of V or more: STRIDE_DEV_TOKEN_RANGE, nothing else.  A
+ * row's repetition that is not positive and finite, a frequency or presence that is
+ * not finite: STRIDE_DEV_BAD_CONTROL; a history_len or a row's part of the lists out of
+ * bounds: STRIDE_DEV_BAD_LAYOUT; the row is NaN. */
+STRIDE_API int stride_logit_controls(const void* logits, int64_t ld, void* out, int64_t ld_out, int32_t dtype, int64_t V,
+                                     int32_t rows, const stride_logit_rules* rules, int32_t* dev_status, void* stream);
 
 /* A row's sampling parameters: each an array [rows] or, where that is NULL,
  * one value for all rows (host struct). */

@@ -162,7 +162,8 @@ def _native():
 
 _NATIVE_ENTRIES = ("state_init", "score_batch", "score_batch_noalloc", "score_batch_multi_teacher", "score_step",
                    "score_step_compact", "select_restart", "buffer_record", "partial_lse", "combine_partials",
-                   "scan_logprobs", "qk_norm_rope", "qk_norm_rope_backward", "kv_append", "tree_attention", "sample")
+                   "scan_logprobs", "qk_norm_rope", "qk_norm_rope_backward", "kv_append", "tree_attention", "attention_mass",
+                   "kv_evict", "logit_controls", "sample")
 
 
 def stride_status_string(code: int) -> str:

@@ -44,6 +44,9 @@ struct Entry {
   decltype(&stride_qk_norm_rope_backward) qk_norm_rope_backward;
   decltype(&stride_kv_append) kv_append;
   decltype(&stride_tree_attention) tree_attention;
+  decltype(&stride_attention_mass) attention_mass;
+  decltype(&stride_kv_evict) kv_evict;
+  decltype(&stride_logit_controls) logit_controls;
   decltype(&stride_sample) sample;
 } g_entry;
 
@@ -499,16 +502,34 @@ stride_norm_rope norm_rope(PyObject* const* a, PyObject* q_weight, PyObject* k_w
   return h;
 }
 
+// A pool and its block table, without lengths.
+stride_paged_cache pool(PyObject* k_cache, PyObject* v_cache, PyObject* table, at::ScalarType type, int64_t D) {
+  const at::Tensor &k = tensor(k_cache), &v = tensor(v_cache), &t = tensor(table);
+  need(k.dim() == 4 && v.dim() == 4 && (k.size(3) <= 1 || k.stride(3) == 1) && k.scalar_type() == type &&
+       v.scalar_type() == type && k.size(3) == D && t.dim() == 2 && t.size(0) < INT32_MAX);
+  for (int i = 0; i < 4; ++i) need(k.size(i) == v.size(i) && k.stride(i) == v.stride(i) && k.size(i) <= INT32_MAX);
+  return {k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(0), (int32_t)k.size(1),
+          (int32_t)k.size(2), (int32_t)t.size(0), dev_as<const int32_t>(table, at::kInt), t.size(1), nullptr, nullptr};
+}
+
+// The sequences of a call.
+void lengths(stride_paged_cache& c, PyObject* ctx_len, PyObject* tok_off) {
+  c.ctx_len = dev_as<const int32_t>(ctx_len, at::kInt, c.n_seqs);
+  c.tok_off = dev_as<const int32_t>(tok_off, at::kInt, (int64_t)c.n_seqs + 1);
+}
+
 // k_cache, v_cache, block_table, ctx_len, tok_off
 stride_paged_cache paged_cache(PyObject* const* a, const HeadRows& like) {
-  const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &t = tensor(a[2]);
-  need(k.dim() == 4 && v.dim() == 4 && (k.size(3) <= 1 || k.stride(3) == 1) && k.scalar_type() == like.type &&
-       v.scalar_type() == like.type && k.size(3) == like.D && t.dim() == 2 && t.size(0) < INT32_MAX);
-  for (int i = 0; i < 4; ++i) need(k.size(i) == v.size(i) && k.stride(i) == v.stride(i) && k.size(i) <= INT32_MAX);
-  const int64_t n = t.size(0);
-  return {k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(0), (int32_t)k.size(1),
-          (int32_t)k.size(2), (int32_t)n, dev_as<const int32_t>(a[2], at::kInt), t.size(1),
-          dev_as<const int32_t>(a[3], at::kInt, n), dev_as<const int32_t>(a[4], at::kInt, n + 1)};
+  stride_paged_cache c = pool(a[0], a[1], a[2], like.type, like.D);
+  lengths(c, a[3], a[4]);
+  return c;
+}
+
+stride_slot_mass slot_mass(PyObject* o, const stride_paged_cache& c) {
+  const at::Tensor& t = tensor(o);
+  need(t.scalar_type() == at::kFloat && t.dim() == 3 && t.size(0) >= c.n_seqs && t.size(1) == c.n_heads &&
+       (t.size(2) <= 1 || t.stride(2) == 1));
+  return {static_cast<float*>(t.data_ptr()), t.stride(0), t.stride(1), t.size(2)};
 }
 
 // q, k, q_out, k_out, pos, cos, sin, q_weight, k_weight, eps, interleaved, dev_status, stream
@@ -573,6 +594,117 @@ int tree_attention(PyObject* const* a) {
   return unlocked([&] {
     return g_entry.tree_attention(&q.r, &out.r, lse, dt, q.N, (int32_t)q.D, scale, mask, &cache, status, ws.p, ws.bytes, st);
   });
+}
+
+// q, lse, k_cache, block_table, ctx_len, tok_off, tree_mask, scale, mass, decay, dev_status, stream
+int attention_mass(PyObject* const* a) {
+  const HeadRows q(a[0]);
+  stride_paged_cache cache = pool(a[2], a[2], a[3], q.type, q.D);
+  lengths(cache, a[4], a[5]);
+  const int32_t dt = row_dtype(q.type);
+  const auto* lse = dev_as<const float>(a[1], at::kFloat, q.N * q.r.n_heads);
+  const auto* mask = static_cast<const uint64_t*>(dev_or_null(a[6], at::kLong, q.N));
+  const float scale = real(a[7]), decay = real(a[9]);
+  const stride_slot_mass mass = slot_mass(a[8], cache);
+  auto* status = dev_or_null_as<int32_t>(a[10], at::kInt, 1);
+  void* st = stream(a[11]);
+  return unlocked([&] {
+    return g_entry.attention_mass(&q.r, lse, dt, q.N, (int32_t)q.D, scale, mask, &cache, decay, &mass, status, st);
+  });
+}
+
+// k_cache, v_cache, block_table, ctx_len, mass, budget, k_to, v_to, to_table, new_len, kept, mass_to, sink, recent,
+// dev_status, stream
+int kv_evict(PyObject* const* a) {
+  const at::Tensor &k = tensor(a[0]), &kept = tensor(a[10]);
+  need(k.dim() == 4);
+  const at::ScalarType type = k.scalar_type();
+  const int32_t dt = row_dtype(type);
+  const int64_t D = k.size(3);
+  stride_paged_cache from = pool(a[0], a[1], a[2], type, D);
+  from.ctx_len = dev_as<const int32_t>(a[3], at::kInt, from.n_seqs);
+  const stride_paged_cache to = pool(a[6], a[7], a[8], type, D);
+  need(to.n_heads == from.n_heads && to.n_seqs == from.n_seqs && kept.dim() == 3 && kept.size(1) == from.n_heads &&
+       kept.size(2) <= INT32_MAX);
+  const stride_slot_mass mass = slot_mass(a[4], from);
+  stride_slot_mass mass_to = {};
+  if (a[11] != Py_None) mass_to = slot_mass(a[11], from);
+  stride_evict_params how = {};
+  if (THPVariable_CheckExact(a[5]))
+    how.budget = dev_as<const int32_t>(a[5], at::kInt, from.n_seqs);
+  else
+    how.budget_all = integer32(a[5]);
+  how.sink = integer32(a[12]);
+  how.recent = integer32(a[13]);
+  how.most = (int32_t)kept.size(2);
+  auto* new_len = dev_as<int32_t>(a[9], at::kInt, from.n_seqs);
+  auto* slots = dev_as<int32_t>(a[10], at::kInt, (int64_t)from.n_seqs * from.n_heads * how.most);
+  auto* status = dev_or_null_as<int32_t>(a[14], at::kInt, 1);
+  void* st = stream(a[15]);
+  const bool with_mass = a[11] != Py_None;
+  return unlocked([&] {
+    return g_entry.kv_evict(&from, &mass, &to, dt, (int32_t)D, &how, new_len, slots, with_mass ? &mass_to : nullptr, status, st);
+  });
+}
+
+// A row stride of logits [rows, >= V] (any, where there is one row).
+int64_t row_stride(const at::Tensor& t, int64_t rows, int64_t V) {
+  need(t.size(1) >= V && (t.size(1) <= 1 || t.stride(1) == 1));
+  return rows <= 1 && t.stride(0) < t.size(1) ? t.size(1) : t.stride(0);
+}
+
+// logits, out, history, history_len, prompt_len, repetition, frequency, presence, bias_off, bias_token, bias, allowed,
+// dev_status, V, stream
+int logit_controls(PyObject* const* a) {
+  const at::Tensor &x = tensor(a[0]), &o = tensor(a[1]);
+  need(x.dim() == 2 && o.scalar_type() == x.scalar_type() && o.dim() == 2 && o.size(0) == x.size(0) && x.size(0) <= INT32_MAX);
+  const int64_t rows = x.size(0), V = a[13] == Py_None ? x.size(1) : integer(a[13]);
+  const int64_t ld = row_stride(x, rows, V), ld_out = row_stride(o, rows, V);
+  const int32_t dt = row_dtype(x.scalar_type());
+  stride_logit_rules r = {};
+  if (a[2] != Py_None) {
+    const at::Tensor& h = tensor(a[2]);
+    need(h.scalar_type() == at::kInt);
+    need(h.dim() == 2 && h.size(0) >= rows && h.size(1) <= INT32_MAX && (h.size(1) <= 1 || h.stride(1) == 1));
+    r.history_stride = h.stride(0);
+    r.history_most = (int32_t)h.size(1);
+    r.history = static_cast<const int32_t*>(h.data_ptr());
+    need(r.history != nullptr);
+    r.history_len = dev_as<const int32_t>(a[3], at::kInt, rows);
+    r.prompt_len = dev_or_null_as<const int32_t>(a[4], at::kInt, rows);
+  } else {
+    need(a[3] == Py_None && a[4] == Py_None);
+  }
+  const auto each = [&](PyObject* p, const float*& array, float& all) {
+    if (THPVariable_CheckExact(p))
+      array = dev_as<const float>(p, at::kFloat, rows);
+    else
+      all = real(p);
+  };
+  each(a[5], r.repetition, r.repetition_all);
+  each(a[6], r.frequency, r.frequency_all);
+  each(a[7], r.presence, r.presence_all);
+  need((a[8] == Py_None) == (a[9] == Py_None) && (a[8] == Py_None) == (a[10] == Py_None));
+  if (a[8] != Py_None) {
+    const int64_t n = tensor(a[10]).numel();
+    need(n <= INT32_MAX);
+    r.bias_off = dev_as<const int32_t>(a[8], at::kInt, rows + 1);
+    r.bias_token = dev_as<const int32_t>(a[9], at::kInt, n);
+    r.bias = dev_as<const float>(a[10], at::kFloat);
+    r.n_bias = (int32_t)n;
+  }
+  if (a[11] != Py_None) {
+    const at::Tensor& m = tensor(a[11]);
+    need(m.scalar_type() == at::kInt && m.dim() == 2 && (m.size(0) == 1 || m.size(0) == rows) && m.size(1) >= (V + 31) / 32 &&
+         (m.size(1) <= 1 || m.stride(1) == 1));
+    r.allowed = reinterpret_cast<const uint32_t*>(m.data_ptr());
+    r.allowed_stride = m.size(0) == 1 ? 0 : m.stride(0);
+  }
+  auto* status = dev_or_null_as<int32_t>(a[12], at::kInt, 1);
+  void* st = stream(a[14]);
+  const void* const xp = x.data_ptr();
+  void* const op = o.data_ptr();
+  return unlocked([&] { return g_entry.logit_controls(xp, ld, op, ld_out, dt, V, (int32_t)rows, &r, status, st); });
 }
 
 // logits, noise, tokens, temperature, top_k, top_p, min_p, logp, dev_status, V, stream
@@ -654,6 +786,9 @@ PyMethodDef g_methods[] = {
     STRIDE_METHOD(qk_norm_rope_backward, 18),
     STRIDE_METHOD(kv_append, 18),
     STRIDE_METHOD(tree_attention, 13),
+    STRIDE_METHOD(attention_mass, 12),
+    STRIDE_METHOD(kv_evict, 16),
+    STRIDE_METHOD(logit_controls, 15),
     STRIDE_METHOD(sample, 11),
     {nullptr, nullptr, 0, nullptr},
 };

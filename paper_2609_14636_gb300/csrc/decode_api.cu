@@ -53,6 +53,12 @@ int check_cache(const stride_paged_cache* c, size_t e) {
   return STRIDE_OK;
 }
 
+int check_mass(const stride_slot_mass* m) {
+  return !m || !m->data || !multiple(m->data, sizeof(float)) || m->slots < 1 ? STRIDE_ERR_INVALID_ARG : STRIDE_OK;
+}
+
+SlotMass view(const stride_slot_mass& m) { return {m.data, m.seq_stride, m.head_stride, m.slots}; }
+
 PagedCache view(const stride_paged_cache& c) {
   return {c.k,      c.v,        c.page_stride,  c.row_stride,   c.head_stride, c.n_pages, c.page_size,
           c.n_heads, c.n_seqs, c.block_table, c.table_stride, c.ctx_len,     c.tok_off};
@@ -251,6 +257,112 @@ int stride_tree_attention(const stride_head_rows* q, const stride_head_rows* out
   p.dev_status = dev_status;
   p.workspace = workspace;
   return done(launch_tree_attention(p, dtype, sms, (cudaStream_t)stream));
+}
+
+int stride_attention_mass(const stride_head_rows* q, const float* lse, int32_t dtype, int64_t n_tokens, int32_t D, float scale,
+                          const uint64_t* tree_mask, const stride_paged_cache* cache, float decay, const stride_slot_mass* mass,
+                          int32_t* dev_status, void* stream) {
+  if (dtype != STRIDE_DTYPE_BF16 && dtype != STRIDE_DTYPE_F16) return STRIDE_ERR_UNSUPPORTED_DTYPE;
+  if (n_tokens < 0 || n_tokens > INT32_MAX || D < 8 || D > STRIDE_MAX_ATTENTION_DIM || D % 8 != 0 || !isfinite(scale)) return STRIDE_ERR_INVALID_ARG;
+  if (!cache || !(decay >= 0.f && isfinite(decay))) return STRIDE_ERR_INVALID_ARG;
+  stride_paged_cache keys = *cache;
+  keys.v = keys.k;
+  const Rows Q(q);
+  int rc = check_cache(&keys, elem_bytes(dtype));
+  if (rc != STRIDE_OK) return rc;
+  if ((rc = check_mass(mass)) != STRIDE_OK) return rc;
+  if (!Q.valid(n_tokens, elem_bytes(dtype)) || Q.r.n_heads < 1 || Q.r.n_heads % keys.n_heads != 0) return STRIDE_ERR_INVALID_ARG;
+  if (!Q.whole(n_tokens, 8, 2) || !cache_whole(keys, 8, 2)) return STRIDE_ERR_INVALID_ARG;
+  if (n_tokens * (Q.r.n_heads / keys.n_heads) > (1 << 30)) return STRIDE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return STRIDE_OK;
+  if (!lse || !multiple(lse, sizeof(float))) return STRIDE_ERR_INVALID_ARG;
+  if ((rc = check_device()) != STRIDE_OK) return rc;
+  cudaError_t e = cudaSuccess;
+  const int sms = current_device_sms(nullptr, &e);
+  if (sms <= 0) return STRIDE_ERR_CUDA;
+  MassParams p = {};
+  p.a.q = Q.r.data;
+  p.a.q_tok = Q.r.token_stride;
+  p.a.q_head = Q.r.head_stride;
+  p.a.n_tokens = n_tokens;
+  p.a.Hq = Q.r.n_heads;
+  p.a.D = D;
+  p.a.scale = scale;
+  p.a.tree_mask = tree_mask;
+  p.a.cache = view(keys);
+  p.a.dev_status = dev_status;
+  p.lse = lse;
+  p.decay = decay;
+  p.mass = view(*mass);
+  return done(launch_attention_mass(p, dtype, sms, (cudaStream_t)stream));
+}
+
+int stride_kv_evict(const stride_paged_cache* from, const stride_slot_mass* mass, const stride_paged_cache* to, int32_t dtype,
+                    int32_t D, const stride_evict_params* how, int32_t* new_len, int32_t* kept, const stride_slot_mass* mass_to,
+                    int32_t* dev_status, void* stream) {
+  const size_t es = elem_bytes(dtype);
+  if (es == 0) return STRIDE_ERR_UNSUPPORTED_DTYPE;
+  if (D < 1 || D > STRIDE_MAX_HEAD_DIM || !from || !to || !how || !new_len || !kept) return STRIDE_ERR_INVALID_ARG;
+  stride_paged_cache f = *from, t = *to;
+  f.tok_off = f.ctx_len;  // (not used)
+  t.tok_off = t.ctx_len = f.ctx_len;
+  int rc = check_cache(&f, es);
+  if (rc != STRIDE_OK) return rc;
+  if ((rc = check_cache(&t, es)) != STRIDE_OK) return rc;
+  if ((rc = check_mass(mass)) != STRIDE_OK || (mass_to && (rc = check_mass(mass_to)) != STRIDE_OK)) return rc;
+  if (f.n_heads != t.n_heads || f.n_seqs != t.n_seqs || how->sink < 0 || how->recent < 0 || how->most < 1) return STRIDE_ERR_INVALID_ARG;
+  if (mass_to && (mass_to->slots < how->most || mass_to->data == mass->data)) return STRIDE_ERR_INVALID_ARG;
+  if ((int64_t)f.n_seqs * f.n_heads > INT32_MAX / 16) return STRIDE_ERR_INVALID_ARG;
+  if ((rc = check_device()) != STRIDE_OK) return rc;
+  cudaError_t e = cudaSuccess;
+  const int sms = current_device_sms(nullptr, &e);
+  if (sms <= 0) return STRIDE_ERR_CUDA;
+  EvictParams p = {};
+  p.from = view(f);
+  p.to = view(t);
+  p.mass = view(*mass);
+  if (mass_to) p.mass_to = view(*mass_to);
+  p.row_bytes = (int32_t)(D * es);
+  p.how = *how;
+  p.new_len = new_len;
+  p.kept = kept;
+  p.dev_status = dev_status;
+  const int n = (int)(16 / es);
+  const bool whole = D % n == 0 && cache_whole(f, n, es) && cache_whole(t, n, es);
+  return done(launch_kv_evict(p, (int)es, whole ? 16 : (int)es, sms, (cudaStream_t)stream));
+}
+
+int stride_logit_controls(const void* logits, int64_t ld, void* out, int64_t ld_out, int32_t dtype, int64_t V, int32_t rows,
+                          const stride_logit_rules* rules, int32_t* dev_status, void* stream) {
+  const size_t es = elem_bytes(dtype);
+  if (es == 0) return STRIDE_ERR_UNSUPPORTED_DTYPE;
+  if (!rules || rows < 0 || V < 1 || V > STRIDE_MAX_VOCAB || ld < V || ld_out < V) return STRIDE_ERR_INVALID_ARG;
+  const stride_logit_rules& r = *rules;
+  if (rows > 0 && (!logits || !out || !multiple(logits, es) || !multiple(out, es))) return STRIDE_ERR_INVALID_ARG;
+  if (logits == out && rows > 1 && ld != ld_out) return STRIDE_ERR_INVALID_ARG;
+  if (r.history) {
+    if (r.history_most < 0 || (rows > 1 && r.history_stride < r.history_most) || !r.history_len) return STRIDE_ERR_INVALID_ARG;
+    if (!r.repetition && !(r.repetition_all > 0.f && isfinite(r.repetition_all))) return STRIDE_ERR_INVALID_ARG;
+    if ((!r.frequency && !isfinite(r.frequency_all)) || (!r.presence && !isfinite(r.presence_all))) return STRIDE_ERR_INVALID_ARG;
+  }
+  if (r.bias_off && (r.n_bias < 0 || (r.n_bias > 0 && (!r.bias_token || !r.bias)))) return STRIDE_ERR_INVALID_ARG;
+  if (r.allowed && r.allowed_stride != 0 && r.allowed_stride < (V + 31) / 32) return STRIDE_ERR_INVALID_ARG;
+  if (rows == 0) return STRIDE_OK;
+  const int dc = check_device();
+  if (dc != STRIDE_OK) return dc;
+  cudaError_t e = cudaSuccess;
+  const int sms = current_device_sms(nullptr, &e);
+  if (sms <= 0) return STRIDE_ERR_CUDA;
+  ControlParams p = {};
+  p.x = logits;
+  p.ld = ld;
+  p.out = out;
+  p.ld_out = ld_out;
+  p.V = (int32_t)V;
+  p.rows = rows;
+  p.how = r;
+  p.dev_status = dev_status;
+  return done(launch_logit_controls(p, dtype, sms, (cudaStream_t)stream));
 }
 
 int stride_sample(const void* logits, int32_t dtype, int64_t ld, int64_t V, int32_t rows, const float* noise, int64_t ld_noise,

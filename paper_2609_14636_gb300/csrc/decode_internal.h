@@ -78,6 +78,44 @@ struct AttentionParams {
 size_t attention_workspace_bytes(int64_t n_tokens, int Hq, int Hk, int D);
 cudaError_t launch_tree_attention(const AttentionParams& p, int dtype, int sms, cudaStream_t stream);
 
+struct SlotMass {
+  float* data;
+  int64_t seq_stride, head_stride, slots;
+};
+
+struct MassParams {
+  AttentionParams a;  // (no outputs)
+  const float* lse;
+  float decay;
+  SlotMass mass;
+};
+cudaError_t launch_attention_mass(const MassParams& p, int dtype, int sms, cudaStream_t stream);
+// Many rows at a time; the cache is one that attention_many_takes.
+cudaError_t launch_attention_mass_many(const MassParams& p, int dtype, int sms, cudaStream_t stream);
+
+struct EvictParams {
+  PagedCache from, to;
+  SlotMass mass, mass_to;  // (mass_to.data: nullable)
+  int32_t row_bytes;       // of a key or a value
+  stride_evict_params how;
+  int32_t* new_len;
+  int32_t* kept;
+  int32_t* dev_status;
+};
+// elem: bytes of an element; chunk: bytes per load that every row and stride is a multiple of (16, or an element).
+cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, cudaStream_t stream);
+
+struct ControlParams {
+  const void* x;
+  int64_t ld;
+  void* out;
+  int64_t ld_out;
+  int32_t V, rows;
+  stride_logit_rules how;
+  int32_t* dev_status;
+};
+cudaError_t launch_logit_controls(const ControlParams& p, int dtype, int sms, cudaStream_t stream);
+
 struct SampleParams {
   const void* x;
   int64_t ld;

@@ -1,6 +1,7 @@
 """The rollout's decode step around the scoring path (include/stride_decode.h):
 norms of queries and keys with the position rotation, the append to a paged
-cache, attention of drafted tokens over it, and sampling.
+cache, attention of drafted tokens over it, the weight that its slots got and
+their eviction by it, controls on logits, and sampling.
 
 The functions keep the C names; they take torch CUDA tensors as those of the
 package do and are part of it (``stride.stride_sample`` and so on).  Head rows
@@ -16,13 +17,14 @@ import ctypes
 import paper_2609_14636_gb300 as _s
 
 __all__ = [
-    "DTYPE_F16", "DEV_POSITION", "DEV_NO_TOKEN", "MAX_HEAD_DIM", "MAX_ATTENTION_DIM", "MAX_TREE", "MAX_TOP_P_VOCAB",
+    "DTYPE_F16", "DEV_POSITION", "DEV_NO_TOKEN", "DEV_BAD_CONTROL", "MAX_HEAD_DIM", "MAX_ATTENTION_DIM", "MAX_TREE", "MAX_TOP_P_VOCAB",
     "stride_qk_norm_rope", "stride_qk_norm_rope_backward", "stride_qk_norm_rope_backward_workspace_size", "stride_kv_append",
-    "stride_tree_attention", "stride_tree_attention_workspace_size", "stride_sample",
+    "stride_tree_attention", "stride_tree_attention_workspace_size", "stride_attention_mass", "stride_kv_evict",
+    "stride_logit_controls", "stride_sample",
 ]
 
 DTYPE_F16 = 2
-DEV_POSITION, DEV_NO_TOKEN = 0x8, 0x10
+DEV_POSITION, DEV_NO_TOKEN, DEV_BAD_CONTROL = 0x8, 0x10, 0x20
 MAX_HEAD_DIM = 1024  # STRIDE_MAX_HEAD_DIM
 MAX_ATTENTION_DIM = 128  # STRIDE_MAX_ATTENTION_DIM
 MAX_TREE = 64  # STRIDE_MAX_TREE
@@ -46,6 +48,20 @@ class _PagedCache(ctypes.Structure):
                 ("ctx_len", _P), ("tok_off", _P)]
 
 
+class _SlotMass(ctypes.Structure):
+    _fields_ = [("data", _P), ("seq_stride", _i64), ("head_stride", _i64), ("slots", _i64)]
+
+
+class _EvictParams(ctypes.Structure):
+    _fields_ = [("budget", _P), ("budget_all", _i32), ("sink", _i32), ("recent", _i32), ("most", _i32)]
+
+
+class _LogitRules(ctypes.Structure):
+    _fields_ = [("history", _P), ("history_stride", _i64), ("history_most", _i32), ("history_len", _P), ("prompt_len", _P), ("repetition", _P),
+                ("repetition_all", _f32), ("frequency", _P), ("frequency_all", _f32), ("presence", _P), ("presence_all", _f32),
+                ("bias_off", _P), ("bias_token", _P), ("bias", _P), ("n_bias", _i32), ("allowed", _P), ("allowed_stride", _i64)]
+
+
 class _SampleParams(ctypes.Structure):
     _fields_ = [("temperature", _P), ("temperature_all", _f32), ("top_k", _P), ("top_k_all", _i32), ("top_p", _P),
                 ("top_p_all", _f32), ("min_p", _P), ("min_p_all", _f32)]
@@ -54,6 +70,7 @@ class _SampleParams(ctypes.Structure):
 def declare(L) -> None:
     """The argument types of the library's functions."""
     rows, how, cache = ctypes.POINTER(_HeadRows), ctypes.POINTER(_NormRope), ctypes.POINTER(_PagedCache)
+    mass = ctypes.POINTER(_SlotMass)
     for fn, args, res in (
             ("stride_qk_norm_rope", [rows] * 4 + [_i32, _i64, _i32, how, _P, _P], ctypes.c_int),
             ("stride_qk_norm_rope_backward", [rows] * 6 + [_i32, _i64, _i32, how, _P, _P, _P, _P, _sz, _P], ctypes.c_int),
@@ -61,6 +78,9 @@ def declare(L) -> None:
             ("stride_kv_append", [rows] * 4 + [_i32, _i64, _i32, how, cache, _P, _P], ctypes.c_int),
             ("stride_tree_attention", [rows] * 2 + [_P, _i32, _i64, _i32, _f32, _P, cache, _P, _P, _sz, _P], ctypes.c_int),
             ("stride_tree_attention_workspace_size", [_i64, _i32, _i32, _i32], _sz),
+            ("stride_attention_mass", [rows, _P, _i32, _i64, _i32, _f32, _P, cache, _f32, mass, _P, _P], ctypes.c_int),
+            ("stride_kv_evict", [cache, mass, cache, _i32, _i32, ctypes.POINTER(_EvictParams), _P, _P, mass, _P, _P], ctypes.c_int),
+            ("stride_logit_controls", [_P, _i64, _P, _i64, _i32, _i64, _i32, ctypes.POINTER(_LogitRules), _P, _P], ctypes.c_int),
             ("stride_sample", [_P, _i32, _i64, _i64, _i32, _P, _i64, ctypes.POINTER(_SampleParams), _P, _P, _P, _P], ctypes.c_int)):
         getattr(L, fn).argtypes = args
         getattr(L, fn).restype = res
@@ -107,20 +127,45 @@ def _norm_rope(like, N, pos, cos, sin, q_weight, k_weight, eps, interleaved):
 
 
 def _paged_cache(k_cache, v_cache, block_table, ctx_len, tok_off, like):
+    c = _cache(k_cache, v_cache, block_table, like)
+    c.ctx_len = _s._dev(ctx_len, "ctx_len", _s._torch().int32, c.n_seqs)
+    c.tok_off = _s._dev(tok_off, "tok_off", _s._torch().int32, c.n_seqs + 1)
+    return c
+
+
+def _cache(k_cache, v_cache, block_table, like):
+    """A checked pool and its block table, without lengths."""
     torch = _s._torch()
     for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
         if not isinstance(c, torch.Tensor) or not c.is_cuda or c.dim() != 4 or (c.shape[3] > 1 and c.stride(3) != 1):
             raise TypeError(f"{name} must be a CUDA tensor [pages, page_size, heads, D] with unit stride along D")
     if (k_cache.dtype != like.dtype or v_cache.dtype != like.dtype or k_cache.shape != v_cache.shape
-            or k_cache.stride() != v_cache.stride() or k_cache.shape[3] != like.shape[2]):
+            or k_cache.stride() != v_cache.stride() or k_cache.shape[3] != like.shape[-1]):
         raise ValueError("the caches must share shape and strides with each other, dtype and D with the rows")
     if block_table.dim() != 2:
         raise ValueError("block_table must be [sequences, pages]")
     n = block_table.shape[0]
     pages, page, heads, _ = k_cache.shape
     return _PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), *k_cache.stride()[:3], pages, page, heads, n,
-                       _s._dev(block_table, "block_table", torch.int32), block_table.shape[1],
-                       _s._dev(ctx_len, "ctx_len", torch.int32, n), _s._dev(tok_off, "tok_off", torch.int32, n + 1))
+                       _s._dev(block_table, "block_table", torch.int32), block_table.shape[1], None, None)
+
+
+def _slot_mass(t, name: str, seqs: int, heads: int):
+    torch = _s._torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float32:
+        raise TypeError(f"{name} must be a float32 CUDA tensor")
+    if t.dim() != 3 or t.shape[0] < seqs or t.shape[1] != heads or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [sequences, kv heads, slots] with unit stride along the slots")
+    return _SlotMass(t.data_ptr(), t.stride(0), t.stride(1), t.shape[2])
+
+
+def _logits_rows(t, name: str, V: int):
+    """A row stride of logits [rows, >= V] (any, where there is one row)."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows, V] with unit column stride")
+    if V > t.shape[1]:
+        raise ValueError(f"V is {V}, {name} has {t.shape[1]} columns")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
 
 
 def _workspace(ws):
@@ -232,6 +277,117 @@ def stride_tree_attention(q, k_cache, v_cache, block_table, ctx_len, tok_off, tr
         ctypes.byref(_paged_cache(k_cache, v_cache, block_table, ctx_len, tok_off, q)),
         _s._dev(dev_status, "dev_status", torch.int32, 1, optional=True), *_workspace(workspace), _s._stream(stream))
     _s._check("stride_tree_attention", rc)
+
+
+def stride_attention_mass(q, lse, k_cache, block_table, ctx_len, tok_off, tree_mask, scale: float, mass, decay: float = 1.0,
+                          dev_status=None, stream=None) -> None:
+    """Adds the attention weights of the new tokens' queries [N, Hq, D] to their
+    sequences' slots: q, the cache and lse [N, Hq] as of and after
+    :func:`stride_tree_attention`.  mass float32 [sequences, kv heads, slots]
+    with unit stride along the slots: mass = decay * mass + weights for the ctx_len
+    committed slots (decay 0: whatever was there), the weights for the new
+    tokens' own."""
+    rc = (_s._NATIVE or _s._native()).attention_mass(q, lse, k_cache, block_table, ctx_len, tok_off, tree_mask, scale, mass, decay,
+                                                     dev_status, stream)
+    if rc is not None:
+        return _s._check("stride_attention_mass", rc)
+    torch, dt, N = _s._torch(), _dtype(q, "q"), q.shape[0]
+    rows, cache = _head_rows(q, "q", q), _paged_cache(k_cache, k_cache, block_table, ctx_len, tok_off, q)
+    rc = _s.lib().stride_attention_mass(
+        ctypes.byref(rows), _s._dev(lse, "lse", torch.float32, N * q.shape[1]), dt, N, q.shape[2], float(scale),
+        _s._dev(tree_mask, "tree_mask", torch.int64, N, optional=True), ctypes.byref(cache), float(decay),
+        ctypes.byref(_slot_mass(mass, "mass", cache.n_seqs, cache.n_heads)),
+        _s._dev(dev_status, "dev_status", torch.int32, 1, optional=True), _s._stream(stream))
+    _s._check("stride_attention_mass", rc)
+
+
+def stride_kv_evict(k_cache, v_cache, block_table, ctx_len, mass, budget, k_to, v_to, to_table, new_len, kept, mass_to=None,
+                    sink: int = 0, recent: int = 0, dev_status=None, stream=None) -> None:
+    """Copies of each sequence and kv head the slots that remain (up to `budget`:
+    the first `sink`, the last `recent`, of the others those of the largest mass)
+    in order into the pages of to_table in k_to, v_to (other pages of the same
+    pools, or others).  budget: a number or int32 [sequences], negative: left
+    out.  Written: int32 new_len [sequences], kept [sequences, kv heads, most]
+    (the remaining slots), float32 mass_to [sequences, kv heads, >= most] or
+    None (their masses)."""
+    rc = (_s._NATIVE or _s._native()).kv_evict(k_cache, v_cache, block_table, ctx_len, mass, budget, k_to, v_to, to_table, new_len,
+                                               kept, mass_to, sink, recent, dev_status, stream)
+    if rc is not None:
+        return _s._check("stride_kv_evict", rc)
+    torch, dt = _s._torch(), _dtype(k_cache, "k_cache")
+    if k_cache.dim() != 4 or k_to.dim() != 4:
+        raise ValueError("caches must be [pages, page_size, heads, D]")
+    like = k_cache[0]
+    source = _cache(k_cache, v_cache, block_table, like)
+    source.ctx_len = _s._dev(ctx_len, "ctx_len", torch.int32, source.n_seqs)
+    to = _cache(k_to, v_to, to_table, like)
+    if to.n_heads != source.n_heads or to.n_seqs != source.n_seqs:
+        raise ValueError("both caches must have the same heads and sequences")
+    if not isinstance(kept, torch.Tensor) or kept.dim() != 3 or kept.shape[1] != source.n_heads:
+        raise ValueError("kept must be int32 [sequences, kv heads, most]")
+    how = _EvictParams(*_each(budget, "budget", torch.int32, source.n_seqs, int), int(sink), int(recent), kept.shape[2])
+    rc = _s.lib().stride_kv_evict(
+        ctypes.byref(source), ctypes.byref(_slot_mass(mass, "mass", source.n_seqs, source.n_heads)), ctypes.byref(to), dt,
+        k_cache.shape[3], ctypes.byref(how), _s._dev(new_len, "new_len", torch.int32, source.n_seqs),
+        _s._dev(kept, "kept", torch.int32, source.n_seqs * source.n_heads * kept.shape[2]),
+        None if mass_to is None else ctypes.byref(_slot_mass(mass_to, "mass_to", source.n_seqs, source.n_heads)),
+        _s._dev(dev_status, "dev_status", torch.int32, 1, optional=True), _s._stream(stream))
+    _s._check("stride_kv_evict", rc)
+
+
+def stride_logit_controls(logits, out, history=None, history_len=None, prompt_len=None, repetition=1.0, frequency=0.0,
+                          presence=0.0, bias_off=None, bias_token=None, bias=None, allowed=None, dev_status=None,
+                          V: int | None = None, stream=None) -> None:
+    """out = logits [rows, ld] with penalties for tokens that a row's sequence
+    has, biases and a mask of allowed tokens (out may be logits).
+
+    history int32 [rows, longest] with history_len int32 [rows], of which the
+    first prompt_len (None: 0) are the prompt's: repetition divides (positive
+    logits) or multiplies, frequency (times the count) and presence are taken
+    off for the tokens past the prompt; numbers or float32 [rows].  bias_token
+    int32, bias float32: row r's entries are bias_off[r] .. bias_off[r + 1] - 1
+    (int32 [rows + 1]).  allowed int32 [rows or 1, words]: bit j % 32 of word
+    j // 32 set, token j is allowed."""
+    rc = (_s._NATIVE or _s._native()).logit_controls(logits, out, history, history_len, prompt_len, repetition, frequency, presence,
+                                                     bias_off, bias_token, bias, allowed, dev_status, V, stream)
+    if rc is not None:
+        return _s._check("stride_logit_controls", rc)
+    torch, dt = _s._torch(), _dtype(logits, "logits")
+    V = logits.shape[-1] if V is None else int(V)
+    if _dtype(out, "out") != dt or out.shape[0] != logits.shape[0]:
+        raise ValueError("out must share dtype and rows with the logits")
+    rows, ld, ld_out = logits.shape[0], _logits_rows(logits, "logits", V), _logits_rows(out, "out", V)
+    r = _LogitRules()
+    if history is not None:
+        if not isinstance(history, torch.Tensor) or not history.is_cuda or history.dtype != torch.int32:
+            raise TypeError("history must be an int32 CUDA tensor")
+        if history.dim() != 2 or history.shape[0] < rows or (history.shape[1] > 1 and history.stride(1) != 1):
+            raise ValueError("history must be [rows, longest] with unit column stride")
+        r.history, r.history_stride, r.history_most = history.data_ptr(), history.stride(0), history.shape[1]
+        r.history_len = _s._dev(history_len, "history_len", torch.int32, rows)
+        r.prompt_len = _s._dev(prompt_len, "prompt_len", torch.int32, rows, optional=True)
+    elif history_len is not None or prompt_len is not None:
+        raise ValueError("history_len and prompt_len go with a history")
+    r.repetition, r.repetition_all = _each(repetition, "repetition", torch.float32, rows, float)
+    r.frequency, r.frequency_all = _each(frequency, "frequency", torch.float32, rows, float)
+    r.presence, r.presence_all = _each(presence, "presence", torch.float32, rows, float)
+    if (bias_off is None) != (bias is None) or (bias_off is None) != (bias_token is None):
+        raise ValueError("bias_off, bias_token and bias go together")
+    if bias_off is not None:
+        r.bias_off = _s._dev(bias_off, "bias_off", torch.int32, rows + 1)
+        r.bias = _s._dev(bias, "bias", torch.float32)
+        r.bias_token = _s._dev(bias_token, "bias_token", torch.int32, bias.numel())
+        r.n_bias = bias.numel()
+    if allowed is not None:
+        if not isinstance(allowed, torch.Tensor) or not allowed.is_cuda or allowed.dtype != torch.int32:
+            raise TypeError("allowed must be an int32 CUDA tensor")
+        if allowed.dim() != 2 or allowed.shape[0] not in (1, rows) or allowed.shape[1] < (V + 31) // 32 or (
+                allowed.shape[1] > 1 and allowed.stride(1) != 1):
+            raise ValueError("allowed must be [rows or 1, (V + 31) // 32] with unit column stride")
+        r.allowed, r.allowed_stride = allowed.data_ptr(), 0 if allowed.shape[0] == 1 else allowed.stride(0)
+    rc = _s.lib().stride_logit_controls(logits.data_ptr(), ld, out.data_ptr(), ld_out, dt, V, rows, ctypes.byref(r),
+                                        _s._dev(dev_status, "dev_status", torch.int32, 1, optional=True), _s._stream(stream))
+    _s._check("stride_logit_controls", rc)
 
 
 def stride_sample(logits, noise, tokens, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logp=None, dev_status=None,
