@@ -225,6 +225,7 @@ cudaError_t run(const MassParams& p, bool few, int sms, cudaStream_t stream) {
 cudaError_t launch_attention_mass(const MassParams& p, int dtype, int sms, cudaStream_t stream) {
   // By the mean of rows a sequence, as only the device knows how many each has.
   const int64_t rows = ((p.a.n_tokens + p.a.cache.n_seqs - 1) / p.a.cache.n_seqs) * (p.a.Hq / p.a.cache.n_heads);
+  if (rows > 16 && attention_mass_many_takes(p)) return launch_attention_mass_many(p, dtype, sms, stream);
   return dtype == STRIDE_DTYPE_BF16 ? run<__nv_bfloat16>(p, rows <= 8, sms, stream) : run<__half>(p, rows <= 8, sms, stream);
 }
 

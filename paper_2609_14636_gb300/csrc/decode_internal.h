@@ -90,7 +90,8 @@ struct MassParams {
   SlotMass mass;
 };
 cudaError_t launch_attention_mass(const MassParams& p, int dtype, int sms, cudaStream_t stream);
-// Many rows at a time; the cache is one that attention_many_takes.
+// Many rows at a time, and whether it takes the call (its copies are boxes of 8 slots at least, and of whole tokens).
+bool attention_mass_many_takes(const MassParams& p);
 cudaError_t launch_attention_mass_many(const MassParams& p, int dtype, int sms, cudaStream_t stream);
 
 struct EvictParams {

@@ -75,6 +75,9 @@ MASS = [
     ([(129, 100), (0, 0), (7, 300)], 6, 2, 120, 8, "wide", False, 0.99, "bf16"),
     ([(70, 90)], 2, 1, 128, 20, "rows", False, 1.0, "f16"),
     ([(1000, 1)] * 40 + [(20, 90)], 4, 2, 64, 16, "rows", False, 1.0, "bf16"),
+    # several tiles for each CTA, odd numbers of them among them, of one block of rows or more
+    ([(3900, 40), (1200, 33), (5000, 45), (130, 60)], 32, 8, 128, 32, "rows", False, 0.9, "bf16"),
+    ([(3900, 13), (1200, 9), (5000, 11), (130, 2)], 16, 8, 120, 24, "heads", True, 1.0, "f16"),
 ]
 
 
