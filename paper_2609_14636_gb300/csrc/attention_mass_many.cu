@@ -9,12 +9,12 @@
 //        slots by 128 bytes, swizzled), some tiles ahead;
 //   17   starts the copies of the rows, a block of whole tokens at a time, and leaves
 //        what a column needs beside them: -lse, and which columns count;
-//   18   one thread issues the products;
+//   18, 19  one thread each issues a tile's products, of half of a block's columns;
 //   0-15 keys from shared memory into tensor memory, where they are the first operand
 //        of all the unit's blocks (from shared memory they would be read again for each,
 //        which is more of its bandwidth than there is); then scores from tensor
-//        memory, weights, sums.  Eight warps for each of the two tiles, four for each
-//        half of a block's columns.
+//        memory, weights, sums: four warps for each tile and half of the columns, whose
+//        waits for their next product are filled by the three others of a scheduler.
 // The rows of a unit that fit in one block are copied once for all its tiles.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -29,8 +29,9 @@ namespace {
 
 constexpr int kSlots = 128;        // of a tile
 constexpr int kCols = 128;         // rows of a block at most
+constexpr int kPart = 64;          // of them, those of a product at most
 constexpr int kTeamWarps = 8;      // of a tile's
-constexpr int kWarps = 2 * kTeamWarps + 3, kThreads = kWarps * 32;
+constexpr int kWarps = 2 * kTeamWarps + 4, kThreads = kWarps * 32;
 constexpr int kMaxStages = 12;
 constexpr int kTileCost = 4;       // what a tile costs at least, in blocks
 
@@ -46,7 +47,7 @@ struct Plan {
 };
 
 struct Barriers {
-  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], scores[2], taken[2], drained;
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][2], taken[2][2], sums[2], joined[2], drained[2];
 };
 
 // A place in a ring, and the parity of its barriers' phase.
@@ -106,6 +107,17 @@ struct Cursor2 {
   __device__ __forceinline__ bool run_ends(int by, int64_t end) const { return tile + by >= u.tiles || pos + (int64_t)by * u.cost >= end; }
 };
 
+// Columns of a block's halves.
+__device__ __forceinline__ int part_of(int cols) { return cols > kPart ? kPart : kPart / 2; }
+
+// A step, as the warps that add up its weights need it.
+struct Step {
+  int64_t mass;   // where its first slot's is
+  int32_t back;   // of the first slot: its place among the new tokens
+  int32_t n, off, blk0, blocks;
+  int32_t flags;  // tiles, 4: the share's last step of the unit, 8: the share's last
+};
+
 // Sum over the CTA's threads before this one, and of all.
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t& all, int64_t* part) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -140,8 +152,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ Barriers bars;
   __shared__ __align__(16) float s_lse[kMaxStages][kCols];  // -lse log2 e of a block's columns
   __shared__ uint32_t s_counts[kMaxStages][kCols / 32];  // columns that count
+  __shared__ Step s_step[kMaxStages];         // of the step that starts with a tile
+  __shared__ float s_sum[2][kSlots];
   __shared__ uint32_t s_lost[kMaxStages];                // boxes of a tile that have no page
-  __shared__ float s_part[2][2][kSlots];
   __shared__ int64_t s_scan[kWarps], s_pos;
   __shared__ int32_t s_seq, s_abort;
   __shared__ uint32_t s_tmem;
@@ -157,16 +170,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kMaxStages; ++i) {
       mbar_init(&bars.k_full[i], 1);
       mbar_init(&bars.k_empty[i], 2 * kTeamWarps);
-      mbar_init(&bars.q_full[i], 1);
-      mbar_init(&bars.q_empty[i], 2 * kTeamWarps + 1);
+      mbar_init(&bars.q_full[i], 2);
+      mbar_init(&bars.q_empty[i], 2 * kTeamWarps + 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.keys[0][i], kTeamWarps);
       mbar_init(&bars.keys[1][i], kTeamWarps);
-      mbar_init(&bars.scores[i], 1);
-      mbar_init(&bars.taken[i], kTeamWarps);
+      for (int j = 0; j < 2; ++j) {
+        mbar_init(&bars.read[i][j], 1);
+        mbar_init(&bars.scores[i][j], 1);
+        mbar_init(&bars.taken[i][j], kTeamWarps / 2);
+      }
+      mbar_init(&bars.sums[i], kTeamWarps / 2);
+      mbar_init(&bars.joined[i], kTeamWarps / 2);
+      mbar_init(&bars.drained[i], 1);
     }
-    mbar_init(&bars.drained, 1);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -225,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, kWaitTimeoutNs, &s_abort); };
   bool ok = true;
 
-  if (warp == kWarps - 3) {
+  if (warp == kWarps - 4) {
     // ---- copies of keys ----
     const int boxes = kSlots / box;  // of a tile: at most 16
     const int bx = lane & (boxes - 1);
@@ -247,6 +265,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (; at.pos < end; ++t) {
       const bool real = some && page >= 0 && page < pc.n_pages, lost = some && !real;
       const int now = page, now_row = row, head = at.head;
+      const int by = at.step(end);
+      const Step step = {at.b * p.mass.seq_stride + head * p.mass.head_stride + at.tile * kSlots,
+                         at.tile * kSlots - at.u.ctx,
+                         at.u.n,
+                         at.u.off,
+                         at.first_block(chain, tokens),
+                         at.u.blocks,
+                         by | (at.run_ends(by, end) ? 4 : 0) | (at.pos + (int64_t)by * at.u.cost >= end ? 8 : 0)};
       at.on(p, tokens, 1);
       if (at.pos < end) look_up(at);  // (the next tile's, on its way while this one waits for its stage)
       if (t >= k_stages) {
@@ -255,15 +281,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const unsigned mine = (1u << boxes) - 1;
       const unsigned gone = __ballot_sync(0xffffffffu, lost) & mine, who = __ballot_sync(0xffffffffu, real) & mine;
-      if (lane == 0) {
+      // (by one thread: from the lanes of a warp they are issued one after the other, at 90 clocks each)
+      uint64_t* bar = &bars.k_full[k.st];
+      const uint32_t to = k_ring + k.st * L::kStage;
+      if (elect_one()) {
         s_lost[k.st] = gone;
-        mbar_arrive_expect_tx(&bars.k_full[k.st], (uint32_t)(__popc(who) * L::kHalves * box * 128));
+        s_step[k.st] = step;
+        mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * L::kHalves * box * 128));
       }
       __syncwarp();
-      if (lane < boxes && real)
 #pragma unroll
-        for (int half = 0; half < L::kHalves; ++half)
-          copy_box(k_ring + k.st * L::kStage + half * kSlots * 128 + bx * box * 128, &k_map, half * 64, now_row, head, now, &bars.k_full[k.st]);
+      for (int x = 0; x < 16; ++x) {
+        const int from = __shfl_sync(0xffffffffu, now, x), first = __shfl_sync(0xffffffffu, now_row, x);
+        if ((who >> x & 1) && elect_one())
+#pragma unroll
+          for (int half = 0; half < L::kHalves; ++half)
+            copy_box(to + half * kSlots * 128 + x * box * 128, &k_map, half * 64, first, head, from, bar);
+      }
       __syncwarp();
       k.on(k_stages);
     }
@@ -272,85 +306,124 @@ __global__ void __launch_bounds__(kThreads, 1)
       volatile int32_t go_on = 0;
       for (int i = t < k_stages ? 0 : t - k_stages; i < t; ++i) mbar_wait_warp(&bars.k_full[i % k_stages], (i / k_stages) & 1, kWaitTimeoutNs, &go_on);
     }
-  } else if (warp == kWarps - 2) {
+  } else if (warp == kWarps - 3) {
     // ---- copies of rows ----
+    // (A block's -lse are on their way while the one before waits for its stage: fetched in turn they took longer than a block
+    // takes, 115 us for the chains instead of ...)
+    int at_lse[kCols / 32];  // of a column: where its lse is past the block's first
+#pragma unroll
+    for (int j = 0; j < kCols / 32; ++j) {
+      const int col = lane + 32 * j, i = col / group;
+      at_lse[j] = i * a.Hq + col - i * group;
+    }
     Place q;
     int t = 0;
     bool fresh = true;
-    while (at.pos < end && ok) {
-      const int by = at.step(end);
-      if (at.u.blocks > 1 || fresh)
-        for (int blk = at.first_block(chain, tokens); blk < at.u.blocks; ++blk, ++t) {
-          const int token0 = at.u.off + blk * tokens, cols = min(tokens, at.u.n - blk * tokens) * group;
-          float lse[kCols / 32];
+    // The block at hand; the next.
+    int blk = 0, by = 0;
+    const auto enter = [&] {  // the step at `at`
+      if (at.pos >= end) return false;
+      by = at.step(end);
+      blk = at.first_block(chain, tokens);
+      return true;
+    };
+    const auto fetch = [&](float (&lse)[kCols / 32]) {
+      const int cols = min(tokens, at.u.n - blk * tokens) * group;
+      const float* from = p.lse + (int64_t)(at.u.off + blk * tokens) * a.Hq + at.head * group;
 #pragma unroll
-          for (int j = 0; j < kCols / 32; ++j) {
-            const int col = lane + 32 * j, i = col / group;
-            lse[j] = -INFINITY;
-            if (col < cols) lse[j] = __ldg(p.lse + (int64_t)(token0 + i) * a.Hq + at.head * group + col - i * group);
-          }
-          if (t >= q_stages) {
-            ok = __all_sync(0xffffffffu, wait(&bars.q_empty[q.st], q.parity ^ 1));
-            if (!ok) break;
-          }
+      for (int j = 0; j < kCols / 32; ++j) {
+        lse[j] = -INFINITY;
+        if (lane + 32 * j < cols) lse[j] = __ldg(from + at_lse[j]);
+      }
+    };
+    // On to the next block that is copied; false: none.
+    const auto on = [&] {
+      if (++blk < at.u.blocks) return true;
+      while (true) {
+        fresh = at.run_ends(by, end);
+        at.on(p, tokens, by);
+        if (!enter()) return false;
+        if (at.u.blocks > 1 || fresh) return true;
+      }
+    };
+    float lse[kCols / 32], next[kCols / 32];
+    bool more = enter();
+    if (more) fetch(lse);
+    while (more) {
+      const int head = at.head * group, token0 = at.u.off + blk * tokens;
+      more = on();
+      if (more) fetch(next);
+      if (t >= q_stages) {
+        ok = __all_sync(0xffffffffu, wait(&bars.q_empty[q.st], q.parity ^ 1));
+        if (!ok) break;
+      }
+      uint64_t* bar = &bars.q_full[q.st];
+      if (elect_one()) {
+        mbar_arrive_expect_tx(bar, (uint32_t)(tokens * group * L::kHalves * 128));
 #pragma unroll
-          for (int j = 0; j < kCols / 32; ++j) {
-            const unsigned counts = __ballot_sync(0xffffffffu, lse[j] != -INFINITY);
-            s_lse[q.st][lane + 32 * j] = -lse[j] * kLog2e;
-            if (lane == 0) s_counts[q.st][j] = counts;
-          }
-          __syncwarp();
-          if (elect_one()) {
-            uint64_t* bar = &bars.q_full[q.st];
-            mbar_arrive_expect_tx(bar, (uint32_t)(tokens * group * L::kHalves * 128));
+        for (int half = 0; half < L::kHalves; ++half)
+          copy_box(q_ring + q.st * L::kStage + half * kCols * 128, &q_map, half * 64, head, token0, 0, bar);
+      }
+      __syncwarp();
 #pragma unroll
-            for (int half = 0; half < L::kHalves; ++half)
-              copy_box(q_ring + q.st * L::kStage + half * kCols * 128, &q_map, half * 64, at.head * group, token0, 0, bar);
-          }
-          __syncwarp();
-          q.on(q_stages);
-        }
-      fresh = at.run_ends(by, end);
-      at.on(p, tokens, by);
+      for (int j = 0; j < kCols / 32; ++j) {
+        const unsigned counts = __ballot_sync(0xffffffffu, lse[j] != -INFINITY);
+        s_lse[q.st][lane + 32 * j] = -lse[j] * kLog2e;
+        if (lane == 0) s_counts[q.st][j] = counts;
+        lse[j] = next[j];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+      q.on(q_stages);
+      ++t;
     }
     if (!ok) {
       if (lane == 0) s_abort = 1;
       volatile int32_t go_on = 0;
       for (int i = t < q_stages ? 0 : t - q_stages; i < t; ++i) mbar_wait_warp(&bars.q_full[i % q_stages], (i / q_stages) & 1, kWaitTimeoutNs, &go_on);
     }
-  } else if (warp == kWarps - 1) {
+  } else if (warp >= kWarps - 2) {
     // ---- products ----
     if (elect_one()) {
+      const int team = warp - (kWarps - 2);
       const uint32_t q0 = matrix(q_ring, 16);
       Place q;
-      uint32_t keys_parity = 0, taken_parity = 0, used = 0;  // bits: buffer and tile; tile
+      uint32_t keys_parity[2] = {0, 0}, taken_parity[2] = {1, 1};
       int buffer = 0;
       bool fresh = true;
       while (at.pos < end && ok) {
         const int by = at.step(end);
-        const bool many = at.u.blocks > 1, run_ends = at.run_ends(by, end);
-        const int blk0 = at.first_block(chain, tokens);
-        for (int blk = blk0; blk < at.u.blocks && ok; ++blk) {
+        const bool many = at.u.blocks > 1, run_ends = at.run_ends(by, end), mine = team < by;
+        if (mine) {
+          ok = wait(&bars.keys[buffer][team], keys_parity[buffer]);
+          keys_parity[buffer] ^= 1;
+        }
+        for (int blk = at.first_block(chain, tokens); blk < at.u.blocks && ok; ++blk) {
           if (many || fresh) ok = wait(&bars.q_full[q.st], q.parity);
-          const uint32_t idesc = product<T>((min(tokens, at.u.n - blk * tokens) * group + 15) & ~15, false);
-          for (int h = 0; h < by && ok; ++h) {
-            if (blk == blk0) {
-              ok = wait(&bars.keys[buffer][h], (keys_parity >> (2 * buffer + h)) & 1);
-              keys_parity ^= 1u << (2 * buffer + h);
-            }
-            if (used >> h & 1) {
-              ok = ok && wait(&bars.taken[h], (taken_parity >> h) & 1);
-              taken_parity ^= 1u << h;
-            }
-            if (!ok) break;
-            used |= 1u << h;
-            fence_after();
-            const uint32_t b = q0 + q.st * (L::kStage >> 4), k = tmem + (2 * buffer + h) * L::kKeys, d = tmem + L::kScores + h * kCols;
+          const int cols = min(tokens, at.u.n - blk * tokens) * group, wide = part_of(cols);
+          if (!mine) {
+            if (ok && (many || run_ends)) mbar_arrive(&bars.q_empty[q.st]);
+          } else {
 #pragma unroll
-            for (int x = 0; x < D / 16; ++x) mma_ts(d, k + x * 8, b + (x / 4) * (kCols * 128 >> 4) + (x % 4) * 2, idesc, x > 0);
-            // (the rows' stage first: whoever has seen the last scores knows that nothing more arrives)
-            if (h == by - 1 && (many || run_ends)) commit(&bars.q_empty[q.st]);
-            commit(&bars.scores[h]);
+            for (int part = 0; part < 2; ++part) {
+              const int c = part * wide;
+              if (c >= cols || !ok) break;
+              ok = wait(&bars.taken[team][part], taken_parity[part]);
+              taken_parity[part] ^= 1;
+              if (!ok) break;
+              fence_after();
+              const uint32_t idesc = product<T>((min(cols - c, wide) + 15) & ~15, false);
+              const uint32_t b = q0 + q.st * (L::kStage >> 4) + (c * 128 >> 4), k = tmem + (2 * buffer + team) * L::kKeys;
+              const uint32_t d = tmem + L::kScores + (2 * team + part) * kPart;
+#pragma unroll
+              for (int x = 0; x < D / 16; ++x) mma_ts(d, k + x * 8, b + (x / 4) * (kCols * 128 >> 4) + (x % 4) * 2, idesc, x > 0);
+              // (the stage and the keys first: whoever has seen the last scores knows that nothing more arrives)
+              if (c + wide >= cols) {
+                if (many || run_ends) commit(&bars.q_empty[q.st]);
+                if (blk + 1 >= at.u.blocks) commit(&bars.read[buffer][team]);
+              }
+              commit(&bars.scores[team][part]);
+            }
           }
           if (many || run_ends) q.on(q_stages);
         }
@@ -361,8 +434,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {
         s_abort = 1;
         volatile int32_t go_on = 0;
-        commit(&bars.drained);
-        mbar_wait(&bars.drained, 0, kWaitTimeoutNs, &go_on);
+        commit(&bars.drained[team]);
+        mbar_wait(&bars.drained[team], 0, kWaitTimeoutNs, &go_on);
       }
     }
     __syncwarp();
@@ -370,143 +443,190 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- weights ----
     const int team = (warp >> 2) & 1, part = warp >> 3, row = (warp & 3) * 32 + lane;  // tile of the step, half of the columns, slot of the tile
     const uint32_t my = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's lanes of tensor memory
-    const float scale2 = a.scale * kLog2e;
+    const uint32_t my_scores = my + L::kScores + (2 * team + part) * kPart;
+    const float2 scale2 = make_float2(a.scale * kLog2e, a.scale * kLog2e);
     Place k, q;
-    // Keys of the step's tile of this team into tensor memory (a half of the components); whether this thread's slot has no page.
+    // What is at hand of a step.
+    struct Now {
+      float* mass;                // of this thread's slot
+      int32_t back, n, off, blk0, blocks, flags;
+      bool lost;                  // the slot has no page
+    };
+    // The next step, its keys of this team's tile into tensor memory (half of the components), where products have read the ones
+    // before them.
     // Every warp waits for every tile and lets go of it, in order: a stage's barriers are never a lap ahead of a team that has
     // no tile in a step.
-    const auto convert = [&](int by, int buffer) {
-      bool lost = false;
+    uint32_t read_parity = 3;  // bits: a buffer (nothing to wait for at first)
+    const auto convert = [&](int buffer) {
+      Now x = {};
+      int by = 1;
       for (int i = 0; i < by; ++i, k.on(k_stages)) {
-        if (ok) ok = __all_sync(0xffffffffu, wait(&bars.k_full[k.st], k.parity));
-        if (!ok) continue;
-        if (i != team) {
-          if (lane == 0) mbar_arrive(&bars.k_empty[k.st]);
-          continue;
+        ok = ok && __all_sync(0xffffffffu, wait(&bars.k_full[k.st], k.parity));
+        if (!ok) return x;
+        if (i == 0) {
+          const Step& s = s_step[k.st];
+          x = {p.mass.data + s.mass + team * kSlots + row, s.back + team * kSlots + row, s.n, s.off, s.blk0, s.blocks, s.flags, false};
+          by = s.flags & 3;
         }
-        constexpr int kRegs = D / 4;  // D / 2 components
-        uint32_t x[kRegs];
-        const uint32_t from = k_ring + k.st * L::kStage + (D == 128 ? part * kSlots * 128 : 0) + row * 128;
+        if (i == team) {
+          ok = __all_sync(0xffffffffu, wait(&bars.read[buffer][team], read_parity >> buffer & 1));
+          read_parity ^= 1u << buffer;
+          if (!ok) return x;
+          fence_after();
+          constexpr int kRegs = D / 4;  // D / 2 components
+          uint32_t r[kRegs];
+          const uint32_t from = k_ring + k.st * L::kStage + (D == 128 ? part * kSlots * 128 : 0) + row * 128;
 #pragma unroll
-        for (int c = 0; c < kRegs / 4; ++c) {
-          const int chunk = (D == 128 ? 0 : part * 4) + c;
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                       : "=r"(x[4 * c]), "=r"(x[4 * c + 1]), "=r"(x[4 * c + 2]), "=r"(x[4 * c + 3])
-                       : "r"(from + ((chunk ^ (row & 7)) << 4))
-                       : "memory");
+          for (int c = 0; c < kRegs / 4; ++c) {
+            const int chunk = (D == 128 ? 0 : part * 4) + c;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(r[4 * c]), "=r"(r[4 * c + 1]), "=r"(r[4 * c + 2]), "=r"(r[4 * c + 3])
+                         : "r"(from + ((chunk ^ (row & 7)) << 4))
+                         : "memory");
+          }
+          x.lost = (s_lost[k.st] >> (row / box)) & 1;
+          tmem_store(my + (2 * buffer + team) * L::kKeys + part * kRegs, r);
         }
-        lost = (s_lost[k.st] >> (row / box)) & 1;
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.k_empty[k.st]);
-        tmem_store(my + (2 * buffer + team) * L::kKeys + part * kRegs, x);
+      }
+      if (team < by) {
         tmem_wait_store();
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.keys[buffer][team]);
       }
-      return lost;
+      return x;
     };
-    uint32_t scores_parity = 0;
+    uint32_t scores_parity = 0, sums_parity = part;  // (the second half's: the first half's have been read)
     int buffer = 0;
-    bool fresh = true, lost = false, lost_ahead = false;
-    Cursor2 ahead = at;
+    bool fresh = true;
     if (at.pos < end) {
-      lost = convert(at.step(end), 0);
-      ahead.on(p, tokens, at.step(end));
-    }
-    // (a warp whose wait has run out goes on without waiting, to the barriers that the others are at)
-    while (at.pos < end) {
-      const int by = at.step(end);
-      if (ahead.pos < end) {
-        const int next = ahead.step(end);
-        lost_ahead = convert(next, buffer ^ 1);
-        ahead.on(p, tokens, next);
-      }
-      const bool many = at.u.blocks > 1, run_ends = at.run_ends(by, end), mine = team < by;
-      const int slot0 = (at.tile + team) * kSlots, back = slot0 + row - at.u.ctx;
-      const bool whole = slot0 + kSlots <= at.u.ctx;
-      float* const mass = p.mass.data + at.b * p.mass.seq_stride + at.head * p.mass.head_stride + slot0 + row;
-      float old = 0.f;
-      if (mine && part == 0 && p.decay != 0.f && back < 0) old = *mass;
-      float2 sum[2] = {};
-      for (int blk = at.first_block(chain, tokens); blk < at.u.blocks && ok; ++blk) {
-        const int token0 = blk * tokens, cols = min(tokens, at.u.n - token0) * group;
-        const int half = (cols + 63) / 64 * 32, c0 = part * half;  // this warp's columns: 32 or 64 from c0 on
-        if (many || fresh) ok = wait(&bars.q_full[q.st], q.parity);
-        if (mine) {
-          ok = ok && wait(&bars.scores[team], scores_parity);
-          scores_parity ^= 1;
-        }
-        ok = __all_sync(0xffffffffu, ok);
+      Now now = convert(0), next = now;
+      while (ok) {
+        const bool ends = now.flags & 8;
+        if (!ends) next = convert(buffer ^ 1);
         if (!ok) break;
-        if (mine) {
-          fence_after();
-          const float2 sc = make_float2(scale2, scale2);
-          const int c1 = min(cols, c0 + half);
+        const bool many = now.blocks > 1, run_ends = now.flags & 4, mine = team < (now.flags & 3);
+        const int back = now.back, slot_back = back - row;  // (of the tile's first slot)
+        const bool whole = slot_back + kSlots <= 0;
+        float old = 0.f;
+        if (mine && part == 0 && p.decay != 0.f && back < 0) old = *now.mass;
+        float2 sum[2] = {};
+        for (int blk = now.blk0; blk < now.blocks && ok; ++blk) {
+          const int token0 = blk * tokens, cols = min(tokens, now.n - token0) * group;
+          const int wide = part_of(cols), c0 = part * wide, c1 = min(cols, c0 + wide);  // this warp's columns: up to 32 or 64
+          if (many || fresh) ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
+          if (mine && c0 < c1) {
+            ok = ok && __all_sync(0xffffffffu, wait(&bars.scores[team][part], scores_parity));
+            scores_parity ^= 1;
+            if (!ok) break;
+            fence_after();
 #pragma unroll 1
-          for (int c = c0; c < c1; c += 32) {
-            uint32_t r[32];
-            tmem_load32(r, my + L::kScores + team * kCols + c);
-            tmem_wait_load();
-            if (c + 32 >= c1) {  // (the last)
-              fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&bars.taken[team]);
-            }
-            uint32_t see = s_counts[q.st][c / 32];
-            if (!whole && back >= 0) {
-              if (chain) {  // from the first column of a token that is as far on as the slot
-                const int from = back > token0 ? min(back - token0, tokens) * group - c : 0;
-                see = from >= 32 ? 0 : from > 0 ? see >> from << from : see;
-              } else {
-                for (uint32_t left = see; left; left &= left - 1) {
-                  const int j = __ffs(left) - 1;
-                  if (back >= at.u.n || !(__ldg(a.tree_mask + at.u.off + token0 + (c + j) / group) >> back & 1)) see &= ~(1u << j);
+            for (int c = c0; c < c1; c += 32) {
+              const uint32_t from = my_scores + c - c0;
+              const float4* lse = reinterpret_cast<const float4*>(&s_lse[q.st][c]);
+              const int n = min(c1 - c, 32);  // columns
+              const bool last = c + 32 >= c1;
+              const uint32_t every = 0xffffffffu >> (32 - n);
+              uint32_t see = s_counts[q.st][c / 32];
+              bool full = see == every, none = see == 0;
+              if (!whole) {
+                if (back >= 0) {
+                  if (chain) {  // from the first column of a token that is as far on as the slot
+                    const int first = back > token0 ? min(back - token0, tokens) * group - c : 0;
+                    see = first >= 32 ? 0 : first > 0 ? see >> first << first : see;
+                  } else {
+                    const int last_token = (min(c + 32, cols) - 1) / group;
+                    uint32_t by_bits = 0;
+                    for (int i = c / group; i <= last_token; ++i) {  // (tokens with a column among these)
+                      const int first = max(i * group - c, 0), upto = min((i + 1) * group - c, 32);
+                      if (__ldg(a.tree_mask + now.off + token0 + i) >> (back & 63) & 1) by_bits |= (0xffffffffu >> (32 - (upto - first))) << first;
+                    }
+                    see &= by_bits;
+                  }
+                }
+                full = __all_sync(0xffffffffu, see == every);
+                none = __all_sync(0xffffffffu, see == 0);
+              }
+              if (none) {
+                if (last) {
+                  fence_before();
+                  __syncwarp();
+                  if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+                }
+                continue;
+              }
+              if (full && n == 32) {
+                uint32_t r[32];
+                tmem_load32(r, from);
+                tmem_wait_load();
+                if (last) {
+                  fence_before();
+                  __syncwarp();
+                  if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+                }
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                  const float4 l = lse[j / 4];
+                  const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), scale2, make_float2(l.x, l.y));
+                  const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), scale2, make_float2(l.z, l.w));
+                  sum[0] = __fadd2_rn(sum[0], make_float2(ex2(x0.x), ex2(x0.y)));
+                  sum[1] = __fadd2_rn(sum[1], make_float2(ex2(x1.x), ex2(x1.y)));
+                }
+                continue;
+              }
+              // (eight columns at a time, in a loop: unrolled with the others' this took so many registers that the whole kernel
+              // was slower: 32 trees of 13 tokens 147 us)
+#pragma unroll 1
+              for (int j = 0; j < n; j += 8) {
+                uint32_t r[8];
+                __syncwarp();
+                tmem_load8(r, from + j);
+                tmem_wait_load();
+                if (last && j + 8 >= n) {
+                  fence_before();
+                  __syncwarp();
+                  if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  const float e = ex2(fmaf(__uint_as_float(r[i]), scale2.x, reinterpret_cast<const float*>(lse)[j + i]));
+                  sum[i & 1].x += see >> (j + i) & 1 ? e : 0.f;
                 }
               }
             }
-            const float4* lse = reinterpret_cast<const float4*>(&s_lse[q.st][c]);
-            const bool all_seen = __all_sync(0xffffffffu, see == 0xffffffffu);
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 l = lse[j / 4];
-              const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), sc, make_float2(l.x, l.y));
-              const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), sc, make_float2(l.z, l.w));
-              float2 e0 = make_float2(ex2(x0.x), ex2(x0.y)), e1 = make_float2(ex2(x1.x), ex2(x1.y));
-              if (!all_seen) {
-                e0 = make_float2(see >> j & 1 ? e0.x : 0.f, see >> (j + 1) & 1 ? e0.y : 0.f);
-                e1 = make_float2(see >> (j + 2) & 1 ? e1.x : 0.f, see >> (j + 3) & 1 ? e1.y : 0.f);
-              }
-              sum[0] = __fadd2_rn(sum[0], e0);
-              sum[1] = __fadd2_rn(sum[1], e1);
-            }
           }
-          if (c0 >= c1) {  // (no columns: nothing to read)
+          if (many || run_ends) {
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.taken[team]);
+            if (lane == 0) mbar_arrive(&bars.q_empty[q.st]);
+            q.on(q_stages);
           }
         }
-        if (many || run_ends) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bars.q_empty[q.st]);
-          q.on(q_stages);
+        if (!ok) break;
+        fresh = run_ends;
+        if (mine) {  // the columns' halves meet
+          float w = (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+          ok = __all_sync(0xffffffffu, wait(part == 0 ? &bars.sums[team] : &bars.joined[team], sums_parity));
+          sums_parity ^= 1;
+          if (!ok) break;
+          if (part == 1) {
+            s_sum[team][row] = w;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.sums[team]);
+          } else {
+            w += s_sum[team][row];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.joined[team]);
+            if (back < 0 && p.decay != 0.f) w = fmaf(p.decay, old, w);
+            if (back < now.n) *now.mass = now.lost ? NAN : w;
+            if (now.lost && back < now.n) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
+          }
         }
+        if (ends) break;
+        now = next;
+        buffer ^= 1;
       }
-      if (!ok && lane == 0) s_abort = 1;
-      fresh = run_ends;
-      // the columns' halves meet
-      float w = (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
-      if (part == 1) s_part[buffer][team][row] = w;
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kTeamWarps * 32) : "memory");
-      if (mine && part == 0 && ok) {
-        w += s_part[buffer][team][row];
-        if (back < 0 && p.decay != 0.f) w = fmaf(p.decay, old, w);
-        if (back < at.u.n) *mass = lost ? NAN : w;
-        if (lost && back < at.u.n) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
-      }
-      lost = lost_ahead;
-      buffer ^= 1;
-      at.on(p, tokens, by);
     }
     if (!ok && lane == 0) {
       s_abort = 1;
