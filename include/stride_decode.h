@@ -271,7 +271,7 @@ STRIDE_API int stride_kv_evict(const stride_paged_cache* from, const stride_slot
 typedef struct stride_logit_rules {
   const int32_t* history;     /* [rows, history_stride] tokens of each row's sequence; NULL: no penalties */
   int64_t history_stride;
-  int32_t history_most;       /* columns that a row has */
+  int32_t history_most;       /* columns that a row has: below 2^30 */
   const int32_t* history_len; /* [rows], 0 <= history_len <= history_most */
   const int32_t* prompt_len;  /* [rows] of which the prompt's; NULL: 0 */
   const float* repetition;    /* > 0; 1: none */

@@ -341,7 +341,7 @@ int stride_logit_controls(const void* logits, int64_t ld, void* out, int64_t ld_
   if (rows > 0 && (!logits || !out || !multiple(logits, es) || !multiple(out, es))) return STRIDE_ERR_INVALID_ARG;
   if (logits == out && rows > 1 && ld != ld_out) return STRIDE_ERR_INVALID_ARG;
   if (r.history) {
-    if (r.history_most < 0 || (rows > 1 && r.history_stride < r.history_most) || !r.history_len) return STRIDE_ERR_INVALID_ARG;
+    if (r.history_most < 0 || r.history_most >= (1 << 30) || (rows > 1 && r.history_stride < r.history_most) || !r.history_len) return STRIDE_ERR_INVALID_ARG;
     if (!r.repetition && !(r.repetition_all > 0.f && isfinite(r.repetition_all))) return STRIDE_ERR_INVALID_ARG;
     if ((!r.frequency && !isfinite(r.frequency_all)) || (!r.presence && !isfinite(r.presence_all))) return STRIDE_ERR_INVALID_ARG;
   }

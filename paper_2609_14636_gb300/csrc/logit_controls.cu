@@ -3,14 +3,16 @@
 //
 //   x > 0 ? x / r : x r (tokens of the history), - f count - p (generated ones), + bias, -inf where not allowed
 //
-// A row is cut into slices of the vocabulary, a CTA each.  The slice's logits stream
-// through with the mask applied, which is what counts: they are on their way from the
-// start, before the history is looked at.  The few tokens that a penalty or a bias
-// applies to are then put right one by one.  How often each occurs is counted in a
-// table in shared memory with an entry for each token of the slice, of which only the
-// entries of tokens that occur are ever set to zero, so that a short history costs
-// little whatever the vocabulary.  The first thread that claims an entry writes the
-// token's logit.  Every CTA reads the whole history, and takes what falls in its slice.
+// A row is cut into slices of the vocabulary, a CTA each, as many as run at once.
+// What counts is that the slice streams through, with the mask applied: the CTA's warps
+// take runs of it in turn, the next one's logits on their way.  Half of them first
+// find what else applies to the slice: a bit for each token of the vocabulary
+// that occurs, the number of bits before each word (so that a token's place among
+// those that occur needs no search: a hash table's exchanges took 20,000
+// clocks for 4,096 tokens), and a count and a last bias at each place.  The logits listed so
+// are then put right, fetched while the slice is still in L2 (by a kernel of its
+// own after the copy they came from memory again, 61 us beside the copy's 24 for 256
+// rows of 151,936).  In place and without a mask only they are read.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -21,11 +23,6 @@
 
 namespace stride {
 namespace {
-
-constexpr int kThreads = 512;
-constexpr int kHeld = 8;      // tokens of the history that a thread keeps
-constexpr int kAhead = 6;     // vectors of logits that a thread has on their way
-constexpr uint32_t kPrompt = 0x80000000u, kClaimed = 0xffffffffu;
 
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -39,6 +36,11 @@ __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(float x) { retur
 template <>
 __device__ __forceinline__ __half rounded<__half>(float x) { return __float2half_rn(x); }
 
+__device__ __forceinline__ const uint32_t* mask_row(const stride_logit_rules& r, int row) {
+  return r.allowed ? r.allowed + row * r.allowed_stride : nullptr;
+}
+__device__ __forceinline__ bool is_allowed(const uint32_t* mask, int c) { return !mask || (__ldg(mask + (c >> 5)) >> (c & 31)) & 1; }
+
 // -inf in the places of a 16-byte vector whose bit is clear.
 template <typename T>
 __device__ __forceinline__ uint4 masked(uint4 v, uint32_t bits) {
@@ -46,32 +48,52 @@ __device__ __forceinline__ uint4 masked(uint4 v, uint32_t bits) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(T) == 4) {
-      if (!((bits >> i) & 1)) w[i] = 0xff800000u;
+      w[i] = (bits >> i) & 1 ? w[i] : 0xff800000u;
     } else {
-      constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0xfc00u : 0xff80u;
-      if (!((bits >> (2 * i)) & 1)) w[i] = (w[i] & 0xffff0000u) | kInf;
-      if (!((bits >> (2 * i + 1)) & 1)) w[i] = (w[i] & 0xffffu) | kInf << 16;
+      constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
+      const uint32_t keep = ((bits >> (2 * i)) & 1 ? 0xffffu : 0u) | ((bits >> (2 * i + 1)) & 1 ? 0xffff0000u : 0u);
+      w[i] = (w[i] & keep) | (kInf & ~keep);
     }
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Blocks: row * slices + slice.  Shared memory: `slice` counts and, where there are biases, as many places of the last entry.
+constexpr int kThreads = 512, kCounters = 256;  // threads; those that count first
+constexpr int kAhead = 4;                       // vectors of a lane in a run
+constexpr int kMostWords = 8192;                // of a slice's bits
+constexpr int kWindow = 4096;                   // places that have counts at a time
+constexpr uint32_t kPrompt = 0x80000000u, kBias = 0x40000000u;  // flags of a count
+
+// A run of a lane: kAhead vectors, 32 lanes' side by side, and the words of the mask that they need.
+struct Run {
+  int first;  // the lane's first vector; past the last: none
+  uint4 v[kAhead];
+  uint32_t lo[kAhead], hi[kAhead];
+};
+
+// Blocks: row * slices + slice.  Shared memory: the bits and their prefix sums, counts, tokens and last biases of a window.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) controls_kernel(const __grid_constant__ ControlParams p, const int slice, const int slices) {
+__global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_constant__ ControlParams p, const int slice, const int slices) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  extern __shared__ uint32_t table[];
   constexpr int kVec = 16 / (int)sizeof(T);
-  uint32_t* const count = table;
-  uint32_t* const entry = table + slice;
-  const int row = blockIdx.x / slices, tid = threadIdx.x;
+  constexpr uint32_t kFull = (1u << kVec) - 1;
+  extern __shared__ __align__(16) uint32_t smem[];
+  __shared__ int s_run, s_total, s_part[kCounters / 32];
+  const int words = slice / 32;
+  uint32_t* const bits = smem;
+  uint32_t* const before = bits + words;
+  uint32_t* const count = before + words;
+  int32_t* const token = reinterpret_cast<int32_t*>(count + kWindow);
+  uint32_t* const entry = count + 2 * kWindow;
+  const int row = blockIdx.x / slices, tid = threadIdx.x, lane = tid & 31;
   const int c0 = (blockIdx.x - row * slices) * slice, c1 = min(p.V, c0 + slice);  // (V is below 2^30 and a slice more)
   const stride_logit_rules& r = p.how;
   const T* const x = static_cast<const T*>(p.x) + row * p.ld;
   T* const out = static_cast<T*>(p.out) + row * p.ld_out;
   const bool in_place = p.x == p.out;
-  const uint32_t* const allowed = r.allowed ? r.allowed + row * r.allowed_stride : nullptr;
+  const uint32_t* const mask = mask_row(r, row);
+  if (tid == 0) s_run = 0;
 
   // ---- what applies to the row ----
   float rep = 1.f, freq = 0.f, pres = 0.f;
@@ -96,141 +118,203 @@ __global__ void __launch_bounds__(kThreads) controls_kernel(const __grid_constan
     if (tid == 0) set_status(p.dev_status, bad);
     return;
   }
-
-  // ---- logits on their way, where they are copied as whole vectors ----
-  const bool stream = !in_place || allowed;
-  const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-  const int shift = (int)(((16 - (reinterpret_cast<uintptr_t>(x + c0) & 15)) & 15) / sizeof(T));  // elements before the first vector
-  const int head = !same ? c1 : min(c1, c0 + shift);  // elements up to here, and those past the last vector, are taken one by one
-  const int vecs = (c1 - head) / kVec;
-  uint4 v[kAhead];
-#pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
-    const int i = tid + u * kThreads;
-    if (stream && i < vecs) v[u] = *(reinterpret_cast<const uint4*>(x + head) + i);
-  }
-
-  // ---- counts ----
   const int32_t* const history = r.history + row * r.history_stride;
-  const uint32_t wide = (uint32_t)(c1 - c0);
-  int held[kHeld];
-#pragma unroll
-  for (int u = 0; u < kHeld; ++u) {
-    const int i = tid + u * kThreads;
-    held[u] = i < n ? __ldg(history + i) : -1;
-  }
-  // f(i, place in the slice) for this thread's tokens of the history that are in the slice
-  const auto each = [&](auto&& f) {
-#pragma unroll
-    for (int u = 0; u < kHeld; ++u)
-      if (held[u] >= 0 && (uint32_t)(held[u] - c0) < wide) f(tid + u * kThreads, held[u] - c0);
-    for (int64_t i = tid + kHeld * kThreads; i < n; i += kThreads) {
-      const int t = __ldg(history + i);
-      if (t >= 0 && (uint32_t)(t - c0) < wide) f((int)i, t - c0);
-    }
-  };
-  const auto each_bias = [&](auto&& f) {
-    for (int64_t i = tid; i < biases; i += kThreads) {
-      const int t = __ldg(r.bias_token + bias0 + i);
-      if (t >= 0 && (uint32_t)(t - c0) < wide) f((uint32_t)i + 1, t - c0);
-      if (c0 == 0 && t >= p.V) set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
-    }
-  };
-  if (c0 == 0) {
-#pragma unroll
-    for (int u = 0; u < kHeld; ++u)
-      if (held[u] >= p.V) set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
-    for (int64_t i = tid + kHeld * kThreads; i < n; i += kThreads)
-      if (__ldg(history + i) >= p.V) set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
-  }
+  const int32_t* const bias_token = r.bias_token + bias0;
   const bool any = n > 0 || biases > 0;
-  if (any) {
-    each([&](int, int t) {
-      count[t] = 0;
-      if (biases) entry[t] = 0;
-    });
-    each_bias([&](uint32_t, int t) {
-      count[t] = 0;
-      entry[t] = 0;
-    });
-    __syncthreads();
-    each([&](int i, int t) {
+  // f(i, place in the slice) for this thread's tokens of a list, of `by` threads
+  const auto each = [&](const int32_t* list, int len, int me, int by, auto&& f) {
+    constexpr int kOnce = 8;
+    for (int64_t i0 = me; i0 < len; i0 += kOnce * by) {
+      int t[kOnce];
+#pragma unroll
+      for (int u = 0; u < kOnce; ++u) t[u] = i0 + (int64_t)u * by < len ? __ldg(list + i0 + (int64_t)u * by) : -1;
+#pragma unroll
+      for (int u = 0; u < kOnce; ++u) f((int)(i0 + u * by), t[u]);
+    }
+  };
+  const auto inside = [&](int t) { return t >= c0 && t < c1; };
+  const auto place = [&](int t) { return before[t >> 5] + __popc(bits[t >> 5] & ((1u << (t & 31)) - 1)); };
+  // Counts, tokens and biases of places w0 .. w0 + kWindow - 1, by all of `by` threads; `sync` between its steps.
+  const auto fill = [&](uint32_t w0, int me, int by, auto&& sync) {
+    for (int i = me; i < kWindow / 4; i += by) {
+      reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+      if (biases) reinterpret_cast<uint4*>(entry)[i] = make_uint4(0, 0, 0, 0);
+    }
+    sync();
+    each(history, n, me, by, [&](int i, int t) {
+      if (!inside(t)) return;
+      const uint32_t k = place(t - c0) - w0;
+      if (k >= kWindow) return;
+      token[k] = t;
       if (i < prompt)
-        atomicOr(&count[t], kPrompt);
+        atomicOr(&count[k], kPrompt);
       else
-        atomicAdd(&count[t], 1u);
+        atomicAdd(&count[k], 1u);
     });
-    each_bias([&](uint32_t i, int t) { atomicMax(&entry[t], i); });
+    each(bias_token, biases, me, by, [&](int i, int t) {
+      if (!inside(t)) return;
+      const uint32_t k = place(t - c0) - w0;
+      if (k >= kWindow) return;
+      token[k] = t;
+      atomicOr(&count[k], kBias);
+      atomicMax(&entry[k], (uint32_t)i + 1);  // (of several entries the last)
+    });
+  };
+  __syncthreads();
+
+  // ---- which tokens occur, and how often ----
+  if (any && tid < kCounters) {
+    const auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kCounters) : "memory"); };
+    for (int i = tid; i < words / 4; i += kCounters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
+    sync();
+    const auto set = [&](int, int t) {
+      if (inside(t))
+        atomicOr(&bits[(t - c0) >> 5], 1u << ((t - c0) & 31));
+      else if (t >= p.V && c0 == 0)
+        set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
+    };
+    each(history, n, tid, kCounters, set);
+    each(bias_token, biases, tid, kCounters, set);
+    sync();
+    int base = 0;  // bits before the words at hand
+    for (int i0 = 0; i0 < words; i0 += kCounters) {
+      const int i = i0 + tid, own = i < words ? __popc(bits[i]) : 0;
+      int upto = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      if (lane == 31) s_part[tid >> 5] = upto;
+      sync();
+      int all = 0;
+#pragma unroll
+      for (int w = 0; w < kCounters / 32; ++w) {
+        if (w < tid >> 5) upto += s_part[w];
+        all += s_part[w];
+      }
+      if (i < words) before[i] = base + upto - own;
+      base += all;
+      sync();
+    }
+    if (tid == 0) s_total = base;
+    fill(0, tid, kCounters, sync);
   }
 
   // ---- the slice with the mask ----
-  const auto bits_from = [&](int c) {  // of columns c, c + 1, ... of a vector
-    const uint32_t lo = __ldg(allowed + (c >> 5));
-    const int s = c & 31;
-    return s + kVec > 32 && ((c >> 5) + 1) * 32 < p.V ? __funnelshift_r(lo, __ldg(allowed + (c >> 5) + 1), s) : lo >> s;
-  };
-  if (stream) {
-    constexpr uint32_t kFull = (1u << kVec) - 1;
-    for (int i0 = tid; i0 < vecs; i0 += kAhead * kThreads) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(x + c0);
+  if (in_place && !mask) {
+  } else if (((at ^ reinterpret_cast<uintptr_t>(out + c0)) & 15) != 0) {  // no vector of one is one of the other
+    T v[8];
+    for (int c = c0 + tid; c < c1; c += 8 * kThreads) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int i = i0 + u * kThreads;
-        if (i0 != tid && i < vecs) v[u] = *(reinterpret_cast<const uint4*>(x + head) + i);
+      for (int u = 0; u < 8; ++u)
+        if (c + u * kThreads < c1) v[u] = x[c + u * kThreads];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (c + u * kThreads < c1) out[c + u * kThreads] = is_allowed(mask, c + u * kThreads) ? v[u] : rounded<T>(-INFINITY);
+    }
+  } else {
+    const int head = min(c1, c0 + (int)(((16 - (at & 15)) & 15) / sizeof(T))), vecs = (c1 - head) / kVec;
+    const auto take = [&](Run& u) {  // the next run
+      int k = 0;
+      if (lane == 0) k = atomicAdd(&s_run, 1);
+      u.first = __shfl_sync(0xffffffffu, k, 0) * 32 * kAhead + lane;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = u.first + 32 * j;
+        if (i < vecs) u.v[j] = *(reinterpret_cast<const uint4*>(x + head) + i);
       }
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int i = i0 + u * kThreads;
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = u.first + 32 * j, c = head + i * kVec, w = c >> 5;
+        u.lo[j] = u.hi[j] = 0xffffffffu;
+        if (!mask || i >= vecs) continue;
+        u.lo[j] = __ldg(mask + w);
+        if ((c & 31) + kVec > 32 && (w + 1) * 32 < p.V) u.hi[j] = __ldg(mask + w + 1);
+      }
+    };
+    const auto put = [&](const Run& u) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = u.first + 32 * j;
         if (i >= vecs) continue;
-        const uint32_t bits = allowed ? bits_from(head + i * kVec) & kFull : kFull;
-        if (bits != kFull)
-          v[u] = masked<T>(v[u], bits);
-        else if (in_place)
-          continue;
-        *(reinterpret_cast<uint4*>(out + head) + i) = v[u];
+        const uint32_t ok = __funnelshift_r(u.lo[j], u.hi[j], (head + i * kVec) & 31) & kFull;
+        if (!(in_place && ok == kFull)) *(reinterpret_cast<uint4*>(out + head) + i) = masked<T>(u.v[j], ok);
       }
+    };
+    Run a, b;
+    take(a);
+    while (__any_sync(0xffffffffu, a.first < vecs)) {
+      take(b);
+      put(a);
+      if (!__any_sync(0xffffffffu, b.first < vecs)) break;
+      take(a);
+      put(b);
     }
     const auto one = [&](int c) {
-      const bool ok = !allowed || (__ldg(allowed + (c >> 5)) >> (c & 31)) & 1;
-      if (!ok)
+      if (!is_allowed(mask, c))
         out[c] = rounded<T>(-INFINITY);
       else if (!in_place)
         out[c] = x[c];
     };
-    for (int c = c0 + tid; c < head; c += kThreads) one(c);
-    for (int c = head + vecs * kVec + tid; c < c1; c += kThreads) one(c);
+    if (c0 + tid < head) one(c0 + tid);
+    const int tail = head + vecs * kVec + tid;
+    if (tail < c1) one(tail);
   }
   if (!any) return;
   __syncthreads();
 
   // ---- the tokens that something applies to ----
-  const auto fix = [&](int t) {
-    const uint32_t seen = atomicExch(&count[t], kClaimed);
-    if (seen == kClaimed) return;
-    const int c = c0 + t;
-    if (allowed && !((__ldg(allowed + (c >> 5)) >> (c & 31)) & 1)) return;
-    float y = value(x[c]);
-    if (seen) y = y > 0.f ? __fdiv_rn(y, rep) : y * rep;
-    const uint32_t made = seen & ~kPrompt;
-    if (made) y = y - freq * (float)made - pres;
-    if (biases && entry[t]) y += __ldg(r.bias + bias0 + entry[t] - 1);
-    out[c] = rounded<T>(y);
-  };
-  each([&](int, int t) { fix(t); });
-  each_bias([&](uint32_t, int t) { fix(t); });
+  const auto sync = [] { __syncthreads(); };
+  for (int w0 = 0;; w0 += kWindow) {
+    const int here = min(kWindow, s_total - w0);
+    constexpr int kOnce = 4;  // logits of a thread on their way
+    for (int i0 = tid; i0 < here; i0 += kOnce * kThreads) {
+      float y[kOnce], bias[kOnce];
+      uint32_t word[kOnce];
+#pragma unroll
+      for (int u = 0; u < kOnce; ++u) {
+        const int i = i0 + u * kThreads;
+        if (i >= here) continue;
+        const int t = token[i];
+        y[u] = value(x[t]);
+        word[u] = mask ? __ldg(mask + (t >> 5)) : 0xffffffffu;
+        bias[u] = count[i] & kBias ? __ldg(r.bias + bias0 + entry[i] - 1) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kOnce; ++u) {
+        const int i = i0 + u * kThreads;
+        if (i >= here) continue;
+        const int t = token[i];
+        if (!(word[u] >> (t & 31) & 1)) continue;
+        const uint32_t seen = count[i], made = seen & ~(kPrompt | kBias);
+        if (seen & ~kBias) y[u] = y[u] > 0.f ? __fdiv_rn(y[u], rep) : y[u] * rep;
+        if (made) y[u] = y[u] - freq * (float)made - pres;
+        if (seen & kBias) y[u] += bias[u];
+        out[t] = rounded<T>(y[u]);
+      }
+    }
+    if (w0 + kWindow >= s_total) break;
+    __syncthreads();
+    fill(w0 + kWindow, tid, kThreads, sync);
+    __syncthreads();
+  }
 }
 
 template <typename T>
-cudaError_t run(const ControlParams& p, cudaStream_t stream) {
-  // entries of a slice's tables: two CTAs on an SM
-  const int per = p.how.bias_off ? 8 : 4, most = 98304 / per;
-  const int about = (p.V + most - 1) / most, slice = ((p.V + about - 1) / about + 63) & ~63, slices = (p.V + slice - 1) / slice;
+cudaError_t run(const ControlParams& p, int sms, cudaStream_t stream) {
+  // as many slices as run at once, of 8,192 tokens at least and as many as there are bits for at most
+  const int64_t most = (int64_t)p.V + 8191, wanted = std::max<int64_t>(1, 2 * sms / p.rows);
+  const int64_t about = std::max<int64_t>(std::min<int64_t>(wanted, most / 8192), (p.V + kMostWords * 32 - 1) / (kMostWords * 32));
+  const int slice = (int)(((p.V + about - 1) / about + 1023) & ~1023), slices = (p.V + slice - 1) / slice;
   if ((int64_t)slices * p.rows > INT32_MAX) return cudaErrorInvalidValue;
   const auto kern = controls_kernel<T>;
-  const size_t smem = p.how.history || p.how.bias_off ? (size_t)slice * per : 0;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 98304 + 1024);
+  const size_t smem = p.how.history || p.how.bias_off ? (size_t)slice / 4 + kWindow * (p.how.bias_off ? 12 : 8) : 0;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostWords * 8 + kWindow * 12);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.rows * slices);
+  cfg.gridDim = dim3((unsigned)slices * p.rows);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -245,10 +329,10 @@ cudaError_t run(const ControlParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_logit_controls(const ControlParams& p, int dtype, int, cudaStream_t stream) {
-  if (dtype == STRIDE_DTYPE_BF16) return run<__nv_bfloat16>(p, stream);
-  if (dtype == STRIDE_DTYPE_F16) return run<__half>(p, stream);
-  return run<float>(p, stream);
+cudaError_t launch_logit_controls(const ControlParams& p, int dtype, int sms, cudaStream_t stream) {
+  if (dtype == STRIDE_DTYPE_BF16) return run<__nv_bfloat16>(p, sms, stream);
+  if (dtype == STRIDE_DTYPE_F16) return run<__half>(p, sms, stream);
+  return run<float>(p, sms, stream);
 }
 
 }  // namespace stride

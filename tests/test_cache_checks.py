@@ -67,7 +67,7 @@ def test_evict(env, bad):  # noqa: F811
 @pytest.mark.parametrize("bad,code", [
     (dict(dtype=3), 2), (dict(V=0), 1), (dict(V=2 ** 30 + 1, ld=2 ** 31, ld_out=2 ** 31), 1), (dict(ld=99), 1), (dict(ld_out=99), 1),
     (dict(rows=-1), 1), (dict(logits=None), 1), (dict(out=None), 1), (dict(logits=DUMMY + 1), 1), (dict(out=DUMMY + 1), 1),
-    (dict(out=DUMMY, ld_out=104), 1), (dict(history_len=None), 1), (dict(history_most=-1), 1), (dict(history_stride=9), 1),
+    (dict(out=DUMMY, ld_out=104), 1), (dict(history_len=None), 1), (dict(history_most=-1), 1), (dict(history_most=2 ** 30, history_stride=2 ** 30), 1), (dict(history_stride=9), 1),
     (dict(repetition_all=0.0), 1), (dict(repetition_all=-1.0), 1), (dict(repetition_all=math.nan), 1), (dict(repetition_all=math.inf), 1),
     (dict(frequency_all=math.nan), 1), (dict(presence_all=math.inf), 1), (dict(n_bias=-1), 1), (dict(bias=None), 1),
     (dict(bias_token=None), 1), (dict(allowed_stride=3), 1), (dict(rows=0), 0), (dict(rows=0, logits=None, out=None), 0)])
