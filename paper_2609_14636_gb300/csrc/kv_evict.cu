@@ -3,10 +3,9 @@
 //
 // Two kernels.  The first finds, for each sequence and kv head, which slots remain:
 // the m-th largest mass digit by digit (its ordered bits, eight at a time, counted
-// in shared memory), then the slots above it and the first ones equal to it,
+// in shared memory, with a cluster's counts added up in distributed shared memory), then the slots above it and the first ones equal to it,
 // numbered by a prefix sum in the slots' order.  A unit (sequence, head) is taken by a
-// cluster of CTAs, more where there are fewer units; their counts meet in
-// distributed shared memory.  The masses stay in registers from the first digit on,
+// cluster of CTAs, more where there are fewer units.  The masses stay in registers from the first digit on,
 // as far as they fit.  The second copies the rows, which is what counts: pages are
 // looked up and offsets computed once for a CTA's rows, then threads move 16 bytes at
 // a time, several loads each on their way.
@@ -23,8 +22,10 @@ namespace stride {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kHeld = 16;  // masses of a thread that stay in registers
 constexpr int kMaxCluster = 16;
+// Copies of the first digit's counts, by lane: nearly all masses have one of a few exponents, and lanes that count alike wait for
+// one another.
+constexpr int kCopies = 8;
 
 // Rises with x; a NaN is below all, zeros are alike.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -50,13 +51,15 @@ __device__ __forceinline__ Plan plan_of(const EvictParams& p, int b) {
   return r;
 }
 
-// Blocks: unit * cluster + rank.
-__global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant__ EvictParams p) {
+// Blocks: unit * cluster + rank.  kHeld: masses of a thread that stay in registers.
+template <int kHeld>
+__global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) select_kernel(const __grid_constant__ EvictParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  __shared__ uint32_t s_count[4][256];  // of each digit's pass
-  __shared__ uint32_t s_sum[256];       // a pass's counts of all CTAs
-  __shared__ int2 s_total;              // slots above the threshold, equal to it, of this CTA
+  __shared__ __align__(16) uint32_t s_first[256 * kCopies];  // the first digit's counts, a digit's copies side by side
+  __shared__ uint32_t s_count[4][256];                       // of each digit's pass
+  __shared__ uint32_t s_part[8], s_digit, s_left;
+  __shared__ int2 s_total;  // slots above the threshold, equal to it, of this CTA
   __shared__ int2 s_warp[kWarps];
   const cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -73,124 +76,156 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
   if (head == 0 && rank == 0 && tid == 0) p.new_len[b] = plan.m;
 
   const float* mass = p.mass.data + b * p.mass.seq_stride + head * p.mass.head_stride;
-  // A warp's slots: a run of `steps` times 32.
-  const int steps = (plan.n + C * kThreads - 1) / (C * kThreads);
-  const int64_t first = (int64_t)(rank * kWarps + warp) * steps * 32 + lane;
-  const int lo = plan.sink, hi = plan.n - plan.recent;  // between them the masses decide
-  float held[kHeld];
+  // A warp's slots: a run of `steps` times 32.  (Below 2^31 and some thousands: unsigned.)
+  const int steps = (int)(((int64_t)plan.n + C * kThreads - 1) / (C * kThreads));
+  const uint32_t first = (uint32_t)(rank * kWarps + warp) * steps * 32 + lane, n = plan.n;
+  const uint32_t lo = plan.sink, between = plan.n - plan.recent - plan.sink;  // from lo on, so many slots that the masses decide about
+  int need = plan.m - plan.sink - plan.recent;                                // that remain of them
+  const bool all = need == (int)between, decide = !all && need > 0;
+  // The first kHeld of this lane's masses, in order, and which of them are still to be decided about; later ones are read again.
+  uint32_t held[kHeld], open = 0;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
-    const int64_t slot = first + j * 32;
-    held[j] = j < steps && slot < plan.n ? __ldg(mass + slot) : 0.f;
+    const uint32_t slot = first + j * 32;
+    float x = 0.f;
+    if (decide && j < steps && slot - lo < between) {
+      x = __ldg(mass + slot);
+      open |= 1u << j;
+    }
+    held[j] = ordered(x);
   }
-  // f(j, slot, mass) for each of this lane's slots below n.
-  const auto each = [&](auto&& f) {
+  // f(key) for the keys of this lane's undecided slots that share the threshold's bits above `shift` + 8
+  uint32_t threshold = 0;
+  const auto each = [&](int shift, auto&& f) {
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) f(j, first + j * 32, held[j]);
+    for (int j = 0; j < kHeld; ++j)
+      if (open >> j & 1) {
+        if (shift < 24 && (held[j] ^ threshold) >> (shift + 8))
+          open &= ~(1u << j);
+        else
+          f(held[j]);
+      }
     for (int j = kHeld; j < steps; ++j) {
-      const int64_t slot = first + j * 32;
-      f(j, slot, slot < plan.n ? __ldg(mass + slot) : 0.f);
+      const uint32_t slot = first + j * 32;
+      if (slot - lo >= between) continue;
+      const uint32_t key = ordered(__ldg(mass + slot));
+      if (shift == 24 || (key ^ threshold) >> (shift + 8) == 0) f(key);
     }
   };
-
-  int need = plan.m - plan.sink - plan.recent;  // of those between
-  const bool all = need == hi - lo, none = need == 0;
-  uint32_t threshold = 0;
-  if (!all && !none) {
-    for (int i = tid; i < 4 * 256; i += kThreads) s_count[i / 256][i % 256] = 0;
+  const auto cluster_sync = [&] {
+    if (C > 1)
+      cluster.sync();
+    else
+      __syncthreads();
+  };
+  if (decide) {
+    for (int i = tid; i < 256 * kCopies; i += kThreads) s_first[i] = 0;
+    for (int i = tid; i < 3 * 256; i += kThreads) s_count[1 + i / 256][i % 256] = 0;
     __syncthreads();
-#pragma unroll
+    each(24, [&](uint32_t key) { atomicAdd(&s_first[(key >> 24) * kCopies + (lane & (kCopies - 1))], 1u); });
+    __syncthreads();
+    if (tid < 256) {
+      const uint4 u = reinterpret_cast<const uint4*>(s_first)[2 * tid], v = reinterpret_cast<const uint4*>(s_first)[2 * tid + 1];
+      s_count[0][tid] = u.x + u.y + u.z + u.w + v.x + v.y + v.z + v.w;
+    }
+#pragma unroll 1
     for (int pass = 0; pass < 4; ++pass) {
       const int shift = 24 - 8 * pass;
-      each([&](int j, int64_t slot, float x) {
-        if (j >= steps || slot < lo || slot >= hi) return;
-        const uint32_t key = ordered(x);
-        if (pass == 0 || (key ^ threshold) >> (shift + 8) == 0) atomicAdd(&s_count[pass][(key >> shift) & 255], 1u);
-      });
-      cluster.sync();
+      if (pass > 0) each(shift, [&](uint32_t key) { atomicAdd(&s_count[pass][(key >> shift) & 255], 1u); });
+      cluster_sync();
+      // the digit at which the counts from the top reach `need`: a thread has a digit, the highest first
+      const int digit = 255 - tid;
+      uint32_t sum = 0, upto = 0;
       if (tid < 256) {
-        uint32_t sum = 0;
-        for (int r = 0; r < C; ++r) sum += *cluster.map_shared_rank(&s_count[pass][tid], r);
-        s_sum[tid] = sum;
+        if (C == 1) {
+          sum = s_count[pass][digit];
+        } else {
+#pragma unroll
+          for (int r = 0; r < kMaxCluster; ++r)
+            if (r < C) sum += *cluster.map_shared_rank(&s_count[pass][digit], r);
+        }
+        upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += v;
+        }
+        if (lane == 31) s_part[warp] = upto;
       }
       __syncthreads();
-      // the digit at which the counts from the top reach `need`, found by each warp: a lane has eight digits
-      uint32_t c[8], own = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        c[i] = s_sum[255 - (lane * 8 + i)];
-        own += c[i];
-      }
-      uint32_t upto = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-      }
-      const int l = __ffs(__ballot_sync(0xffffffffu, upto >= (uint32_t)need)) - 1;
-      uint32_t above = upto - own;
-      int digit = 0, left = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (above < (uint32_t)need && above + c[i] >= (uint32_t)need) {
-          digit = 255 - (lane * 8 + i);
-          left = need - (int)above;
+      if (tid < 256) {
+        for (int w = 0; w < warp; ++w) upto += s_part[w];
+        if (upto >= (uint32_t)need && upto - sum < (uint32_t)need) {
+          s_digit = digit;
+          s_left = need - (upto - sum);
         }
-        above += c[i];
       }
-      threshold |= (uint32_t)__shfl_sync(0xffffffffu, digit, l) << shift;
-      need = __shfl_sync(0xffffffffu, left, l);
-      __syncthreads();  // (s_sum is read)
+      __syncthreads();
+      threshold |= s_digit << shift;
+      need = (int)s_left;
+      // (the next write of these is behind two barriers)
     }
   }
   // `need` of those equal to the threshold remain, the first ones.
-  const auto above = [&](int64_t slot, float x) {
-    return slot < plan.n && (slot < lo || slot >= hi || all || (!none && ordered(x) > threshold));
+  const auto above = [&](uint32_t slot, uint32_t key) {
+    return slot < n && (slot - lo >= between || all || (decide && key > threshold));
   };
-  const auto equal = [&](int64_t slot, float x) { return slot >= lo && slot < hi && !all && !none && ordered(x) == threshold; };
+  const auto equal = [&](uint32_t slot, uint32_t key) { return decide && slot - lo < between && key == threshold; };
+  uint32_t ups = 0, eqs = 0;  // bits: the first kHeld slots
   int2 mine = make_int2(0, 0);
-  each([&](int j, int64_t slot, float x) {
-    if (j >= steps) return;
-    mine.x += __popc(__ballot_sync(0xffffffffu, above(slot, x)));
-    mine.y += __popc(__ballot_sync(0xffffffffu, equal(slot, x)));
-  });
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    if (j >= steps) break;
+    const uint32_t slot = first + j * 32;
+    if (above(slot, held[j])) ups |= 1u << j;
+    if (equal(slot, held[j])) eqs |= 1u << j;
+  }
+  mine.x = __popc(ups);
+  mine.y = __popc(eqs);
+  for (int j = kHeld; j < steps; ++j) {
+    const uint32_t slot = first + j * 32, key = slot < n ? ordered(__ldg(mass + slot)) : 0;
+    mine.x += above(slot, key);
+    mine.y += equal(slot, key);
+  }
+  mine.x = __reduce_add_sync(0xffffffffu, mine.x);
+  mine.y = __reduce_add_sync(0xffffffffu, mine.y);
   if (lane == 0) s_warp[warp] = mine;
   __syncthreads();
-  if (tid == 0) {
-    int2 sum = make_int2(0, 0);
-    for (int w = 0; w < kWarps; ++w) {
-      const int2 v = s_warp[w];
-      s_warp[w] = sum;
-      sum.x += v.x;
-      sum.y += v.y;
-    }
-    s_total = sum;
+  int2 before = make_int2(0, 0);
+  for (int w = 0; w < warp; ++w) {
+    before.x += s_warp[w].x;
+    before.y += s_warp[w].y;
   }
-  if (C > 1)
+  if (tid == kThreads - 1) s_total = make_int2(before.x + s_warp[warp].x, before.y + s_warp[warp].y);
+  if (C > 1) {
     cluster.sync();
-  else
-    __syncthreads();
-  int2 before = s_warp[warp];
-  for (int r = 0; r < rank; ++r) {
-    const int2 v = *cluster.map_shared_rank(&s_total, r);
-    before.x += v.x;
-    before.y += v.y;
+    int2 v = make_int2(0, 0);
+    if (lane < rank) v = *cluster.map_shared_rank(&s_total, lane);  // (a lane's CTA)
+    before.x += __reduce_add_sync(0xffffffffu, v.x);
+    before.y += __reduce_add_sync(0xffffffffu, v.y);
   }
-  const int64_t row = (int64_t)unit * p.how.most;
-  float* mass_to = p.mass_to.data ? p.mass_to.data + b * p.mass_to.seq_stride + head * p.mass_to.head_stride : nullptr;
-  each([&](int j, int64_t slot, float x) {
-    if (j >= steps) return;
-    const bool up = above(slot, x), eq = equal(slot, x);
-    const unsigned ups = __ballot_sync(0xffffffffu, up), eqs = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1;
-    const int e = before.y + __popc(eqs & below);
+  int32_t* const kept = p.kept + (int64_t)unit * p.how.most;
+  float* const mass_to = p.mass_to.data ? p.mass_to.data + b * p.mass_to.seq_stride + head * p.mass_to.head_stride : nullptr;
+  const auto put = [&](uint32_t slot, bool up, bool eq) {
+    const unsigned up_lanes = __ballot_sync(0xffffffffu, up), eq_lanes = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1;
+    const int e = before.y + __popc(eq_lanes & below);
     if (up || (eq && e < need)) {
-      const int i = before.x + __popc(ups & below) + min(e, need);
-      p.kept[row + i] = (int32_t)slot;
-      if (mass_to) mass_to[i] = x;
+      const int i = before.x + __popc(up_lanes & below) + min(e, need);
+      kept[i] = (int32_t)slot;
+      if (mass_to) mass_to[i] = __ldg(mass + slot);
     }
-    before.x += __popc(ups);
-    before.y += __popc(eqs);
-  });
+    before.x += __popc(up_lanes);
+    before.y += __popc(eq_lanes);
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    if (j >= steps) break;
+    put(first + j * 32, ups >> j & 1, eqs >> j & 1);
+  }
+  for (int j = kHeld; j < steps; ++j) {
+    const uint32_t slot = first + j * 32, key = slot < n ? ordered(__ldg(mass + slot)) : 0;
+    put(slot, above(slot, key), equal(slot, key));
+  }
   if (C > 1) cluster.sync();  // (no CTA leaves while its counts may be read)
 }
 
@@ -251,7 +286,8 @@ cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, 
   const int64_t slots = std::min<int64_t>(p.mass.slots, p.from.table_stride * (int64_t)p.from.page_size);
   int C = 1;
   while (C < kMaxCluster && (int64_t)units * C * 2 <= sms && slots > (int64_t)C * kThreads * 2) C *= 2;
-  cudaError_t e = cudaFuncSetAttribute(select_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  const int64_t held = (slots + C * kThreads - 1) / (C * kThreads);  // masses of a thread at most
+  cudaError_t e = cudaFuncSetAttribute(held <= 8 ? select_kernel<8> : select_kernel<16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(units * C);
@@ -265,7 +301,8 @@ cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, 
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, select_kernel, p);
+  // (sequences of up to 4,096 slots a CTA: half the registers, half as many CTAs again)
+  e = cudaLaunchKernelEx(&cfg, held <= 8 ? select_kernel<8> : select_kernel<16>, p);
   if (e != cudaSuccess) return e;
   const int64_t most = std::min<int64_t>(std::min<int64_t>(p.how.most, slots), p.to.table_stride * (int64_t)p.to.page_size);
   const int64_t parts = std::min<int64_t>((most + kRows - 1) / kRows, ((int64_t)sms * 64 + units - 1) / units);

@@ -58,10 +58,10 @@ __device__ __forceinline__ uint4 masked(uint4 v, uint32_t bits) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-constexpr int kThreads = 512, kCounters = 256;  // threads; those that count first
-constexpr int kAhead = 4;                       // vectors of a lane in a run
-constexpr int kMostWords = 8192;                // of a slice's bits
-constexpr int kWindow = 4096;                   // places that have counts at a time
+constexpr int kThreads = 512;
+constexpr int kAhead = 3;         // vectors of a lane in a run (256 rows of 151,936, us: 2 40.6, 3 40.2, 4 43.1)
+constexpr int kMostWords = 8192;  // of a slice's bits
+constexpr int kWindow = 4096;     // places that have counts at a time
 constexpr uint32_t kPrompt = 0x80000000u, kBias = 0x40000000u;  // flags of a count
 
 // A run of a lane: kAhead vectors, 32 lanes' side by side, and the words of the mask that they need.
@@ -71,15 +71,16 @@ struct Run {
   uint32_t lo[kAhead], hi[kAhead];
 };
 
-// Blocks: row * slices + slice.  Shared memory: the bits and their prefix sums, counts, tokens and last biases of a window.
+// Blocks: row * slices + slice; counters: threads (256 or all) that count first.  Shared memory: the bits and their prefix sums, counts, tokens and last biases of a window.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_constant__ ControlParams p, const int slice, const int slices) {
+__global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_constant__ ControlParams p, const int slice, const int slices,
+                                                                const int counters) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int kVec = 16 / (int)sizeof(T);
   constexpr uint32_t kFull = (1u << kVec) - 1;
   extern __shared__ __align__(16) uint32_t smem[];
-  __shared__ int s_run, s_total, s_part[kCounters / 32];
+  __shared__ int s_run, s_total, s_part[kThreads / 32];
   const int words = slice / 32;
   uint32_t* const bits = smem;
   uint32_t* const before = bits + words;
@@ -163,9 +164,9 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   __syncthreads();
 
   // ---- which tokens occur, and how often ----
-  if (any && tid < kCounters) {
-    const auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kCounters) : "memory"); };
-    for (int i = tid; i < words / 4; i += kCounters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
+  if (any && tid < counters) {
+    const auto sync = [&] { asm volatile("bar.sync 1, %0;" ::"r"(counters) : "memory"); };
+    for (int i = tid; i < words / 4; i += counters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
     sync();
     const auto set = [&](int, int t) {
       if (inside(t))
@@ -173,11 +174,11 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       else if (t >= p.V && c0 == 0)
         set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
     };
-    each(history, n, tid, kCounters, set);
-    each(bias_token, biases, tid, kCounters, set);
+    each(history, n, tid, counters, set);
+    each(bias_token, biases, tid, counters, set);
     sync();
     int base = 0;  // bits before the words at hand
-    for (int i0 = 0; i0 < words; i0 += kCounters) {
+    for (int i0 = 0; i0 < words; i0 += counters) {
       const int i = i0 + tid, own = i < words ? __popc(bits[i]) : 0;
       int upto = own;
 #pragma unroll
@@ -189,16 +190,17 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       sync();
       int all = 0;
 #pragma unroll
-      for (int w = 0; w < kCounters / 32; ++w) {
-        if (w < tid >> 5) upto += s_part[w];
-        all += s_part[w];
+      for (int w = 0; w < kThreads / 32; ++w) {
+        const int v = w < counters >> 5 ? s_part[w] : 0;
+        if (w < tid >> 5) upto += v;
+        all += v;
       }
       if (i < words) before[i] = base + upto - own;
       base += all;
       sync();
     }
     if (tid == 0) s_total = base;
-    fill(0, tid, kCounters, sync);
+    fill(0, tid, counters, sync);
   }
 
   // ---- the slice with the mask ----
@@ -304,8 +306,9 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
 
 template <typename T>
 cudaError_t run(const ControlParams& p, int sms, cudaStream_t stream) {
-  // as many slices as run at once, of 8,192 tokens at least and as many as there are bits for at most
-  const int64_t most = (int64_t)p.V + 8191, wanted = std::max<int64_t>(1, 2 * sms / p.rows);
+  // twice as many slices as run at once (256 rows of 151,936, us: as many 45, twice 43, four times 46), of 8,192 tokens at least
+  // and as many as there are bits for at most
+  const int64_t most = (int64_t)p.V + 8191, wanted = std::max<int64_t>(1, 4 * sms / p.rows);
   const int64_t about = std::max<int64_t>(std::min<int64_t>(wanted, most / 8192), (p.V + kMostWords * 32 - 1) / (kMostWords * 32));
   const int slice = (int)(((p.V + about - 1) / about + 1023) & ~1023), slices = (p.V + slice - 1) / slice;
   if ((int64_t)slices * p.rows > INT32_MAX) return cudaErrorInvalidValue;
@@ -323,7 +326,9 @@ cudaError_t run(const ControlParams& p, int sms, cudaStream_t stream) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kern, p, slice, slices);
+  // where a CTA has an SM to itself nothing is gained by streaming early (one row: 256 of them 8.1 us, all 7.2; 256 rows: 43, 48)
+  const int counters = (int64_t)slices * p.rows <= sms ? kThreads : kThreads / 2;
+  e = cudaLaunchKernelEx(&cfg, kern, p, slice, slices, counters);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
