@@ -32,6 +32,9 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t b = x == 0.f ? 0 : __float_as_uint(x);
   return isnan(x) ? 0 : (b >> 31) ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float mass_of(uint32_t key) {
+  return key == 0 ? NAN : __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
+}
 
 // What remains of a sequence.
 struct Plan {
@@ -83,16 +86,20 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) select_kernel(co
   int need = plan.m - plan.sink - plan.recent;                                // that remain of them
   const bool all = need == (int)between, decide = !all && need > 0;
   // The first kHeld of this lane's masses, in order, and which of them are still to be decided about; later ones are read again.
+  // (All on their way at once: a load behind each slot's own branch took 19,000 clocks for sixteen.)
   uint32_t held[kHeld], open = 0;
+  const uint32_t end = n > 0 ? n - 1 : 0;
+  if (n > 0) {
+    float x[kHeld];
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j) {
-    const uint32_t slot = first + j * 32;
-    float x = 0.f;
-    if (decide && j < steps && slot - lo < between) {
-      x = __ldg(mass + slot);
-      open |= 1u << j;
-    }
-    held[j] = ordered(x);
+    for (int j = 0; j < kHeld; ++j) x[j] = __ldg(mass + min(first + j * 32, end));
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) held[j] = ordered(x[j]);
+  }
+  if (decide) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (j < steps && first + j * 32 - lo < between) open |= 1u << j;
   }
   // f(key) for the keys of this lane's undecided slots that share the threshold's bits above `shift` + 8
   uint32_t threshold = 0;
@@ -140,9 +147,13 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) select_kernel(co
         if (C == 1) {
           sum = s_count[pass][digit];
         } else {
+          for (int r0 = 0; r0 < C; r0 += 8) {  // (eight CTAs' on their way at once; C is a power of two)
+            uint32_t v[8];
 #pragma unroll
-          for (int r = 0; r < kMaxCluster; ++r)
-            if (r < C) sum += *cluster.map_shared_rank(&s_count[pass][digit], r);
+            for (int r = 0; r < 8; ++r) v[r] = *cluster.map_shared_rank(&s_count[pass][digit], (r0 + r) & (C - 1));
+#pragma unroll
+            for (int r = 0; r < 8; ++r) sum += r0 + r < C ? v[r] : 0;
+          }
         }
         upto = sum;
 #pragma unroll
@@ -206,13 +217,13 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) select_kernel(co
   }
   int32_t* const kept = p.kept + (int64_t)unit * p.how.most;
   float* const mass_to = p.mass_to.data ? p.mass_to.data + b * p.mass_to.seq_stride + head * p.mass_to.head_stride : nullptr;
-  const auto put = [&](uint32_t slot, bool up, bool eq) {
+  const auto put = [&](uint32_t slot, uint32_t key, bool up, bool eq) {
     const unsigned up_lanes = __ballot_sync(0xffffffffu, up), eq_lanes = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1;
     const int e = before.y + __popc(eq_lanes & below);
     if (up || (eq && e < need)) {
       const int i = before.x + __popc(up_lanes & below) + min(e, need);
       kept[i] = (int32_t)slot;
-      if (mass_to) mass_to[i] = __ldg(mass + slot);
+      if (mass_to) mass_to[i] = mass_of(key);
     }
     before.x += __popc(up_lanes);
     before.y += __popc(eq_lanes);
@@ -220,11 +231,11 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) select_kernel(co
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
     if (j >= steps) break;
-    put(first + j * 32, ups >> j & 1, eqs >> j & 1);
+    put(first + j * 32, held[j], ups >> j & 1, eqs >> j & 1);
   }
   for (int j = kHeld; j < steps; ++j) {
     const uint32_t slot = first + j * 32, key = slot < n ? ordered(__ldg(mass + slot)) : 0;
-    put(slot, above(slot, key), equal(slot, key));
+    put(slot, key, above(slot, key), equal(slot, key));
   }
   if (C > 1) cluster.sync();  // (no CTA leaves while its counts may be read)
 }
