@@ -11,25 +11,27 @@
 //
 // This kernel takes up to 16 rows at a time, where reading the keys is what counts.
 // Every warp has a share of the line of tiles (attention_line.cuh; a unit is a
-// sequence and a kv head) and loads a tile of 16 slots, two rows of keys for each
-// quad of lanes, straight into the registers of mma.sync's first operand (m16n8k16):
-// the order of the summed components is free as long as both operands have the
-// same, so a lane takes whole 16-byte vectors and no shuffle or shared memory is
-// needed.  The next tile's keys are on their way meanwhile.  The rows are the
-// second operand and stay in registers where a unit has no more than the kernel takes
-// at once; a result's two columns are added in the lane, the quad's by shuffles.
+// sequence and a kv head) and takes 16 slots of it at a time through a ring of stages in
+// shared memory, filled by asynchronous copies some tiles ahead.  A lane copies what
+// it will need itself, whole 16-byte vectors of two keys: mma.sync's first operand
+// (m16n8k16), as the order of the summed components is free where both operands have
+// the same.  So there is no exchange between lanes and nothing to wait for but the lane's
+// own copies.  (Held in registers a tile ahead: 248 us for 256 sequences of up to 4,096
+// slots, as registers bound what is on its way.)  The rows are the second operand and stay
+// in registers where a unit has no more than the kernel takes at once; a result's two
+// columns are added in the lane, the quad's by shuffles.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 
 #include "attention_line.cuh"
+#include "mbarrier.cuh"
 
 namespace stride {
 namespace {
 
 constexpr int kShift = 4, kSlots = 1 << kShift;
-constexpr int kWarps = 16;
 constexpr int kExtra = 1;  // tiles that a unit's start costs
 
 template <typename T>
@@ -47,16 +49,25 @@ __device__ __forceinline__ void mma<__half>(float (&c)[4], uint32_t a0, uint32_t
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// What a lane holds of a tile: 16-byte chunks t, t + 4, ... (t its place in the quad) of the keys of slots s and s + 8 of the
-// tile, s the quad; their old masses (the quad's first and second lane).
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {
+  const int n = real ? 16 : 0;  // (0: zeros)
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool real) {
+  const int n = real ? 4 : 0;
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+
+// Warps of a CTA and their rings.  A stage: 16-byte chunks t, t + 4, ... (t its place in the quad) of the keys of slots s and s + 8
+// of the tile (s the quad) of each lane, side by side for the warp; the old masses of the slots.
 template <int kVec>
-struct Tile {
-  uint4 k[2][kVec];
-  float old;
-  bool lost[2];
+struct Ring {
+  static constexpr int kWarps = 16, kStages = kVec == 4 ? 3 : 5;
+  static constexpr int kStage = 2 * kVec * 512 + 64;
+  static constexpr size_t kSmem = (size_t)kWarps * kStages * kStage;
 };
 
-// Eight rows of a unit, likewise, and what the lane's two columns of the result need.
+// Eight rows of a unit, the same chunks of them, and what the lane's two columns of the result need.
 template <int kVec>
 struct RowGroup {
   uint4 q[kVec];
@@ -66,9 +77,12 @@ struct RowGroup {
 
 // kVec: chunks of a key that a lane has (D up to 32 kVec); kGroups: groups of eight rows taken at once.
 template <typename T, int kVec, int kGroups>
-__global__ void __launch_bounds__(kWarps * 32, 1) mass_few_kernel(const __grid_constant__ MassParams p, const int page_shift) {
+__global__ void __launch_bounds__(Ring<kVec>::kWarps * 32, 1) mass_few_kernel(const __grid_constant__ MassParams p, const int page_shift) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  using R = Ring<kVec>;
+  constexpr int kWarps = R::kWarps, kStages = R::kStages;
+  extern __shared__ __align__(128) unsigned char dyn[];
   __shared__ Line line;
   const AttentionParams& a = p.a;
   const PagedCache& pc = a.cache;
@@ -91,24 +105,30 @@ __global__ void __launch_bounds__(kWarps * 32, 1) mass_few_kernel(const __grid_c
       if (slot < u.end) page[r] = __ldg(pc.block_table + (int64_t)u.b * pc.table_stride + (page_shift >= 0 ? slot >> page_shift : slot / pc.page_size));
     }
   };
-  const auto load = [&](const Cursor& u, const int32_t (&page)[2], Tile<kVec>& x) {
+  const uint32_t ring = smem_u32(dyn) + warp * kStages * R::kStage;
+  // Starts the copies of a tile; its bits: whether the lane's slots have no page.
+  const auto load = [&](const Cursor& u, const int32_t (&page)[2], uint32_t stage) {
+    uint32_t lost = 0;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int slot = u.tile * kSlots + quad + 8 * r;
       const bool in = slot < u.end, real = in && page[r] >= 0 && page[r] < pc.n_pages;
-      x.lost[r] = in && !real;
+      lost |= (uint32_t)(in && !real) << r;
       const int row = page_shift >= 0 ? slot & ((1 << page_shift) - 1) : slot % pc.page_size;
-      const T* k = static_cast<const T*>(pc.k) + page[r] * pc.page_stride + row * pc.row_stride + u.head * pc.head_stride;
+      const T* k = static_cast<const T*>(pc.k) + (real ? page[r] * pc.page_stride + row * pc.row_stride + u.head * pc.head_stride : 0);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        const int c = t + 4 * i;
-        x.k[r][i] = real && c < chunks ? ld_stream(reinterpret_cast<const uint4*>(k) + c) : make_uint4(0, 0, 0, 0);
+        const bool some = real && t + 4 * i < chunks;
+        copy16(stage + (r * kVec + i) * 512 + lane * 16, some ? k + (t + 4 * i) * 8 : k, some);
       }
     }
-    x.old = 0.f;
-    const int slot = u.tile * kSlots + quad + 8 * t;
-    if (t < 2 && p.decay != 0.f && slot < u.s.ctx && slot < u.end && u.end <= p.mass.slots)
-      x.old = p.mass.data[u.b * p.mass.seq_stride + u.head * p.mass.head_stride + slot];
+    if (t < 2 && p.decay != 0.f) {
+      const int slot = u.tile * kSlots + quad + 8 * t;
+      const bool some = slot < u.s.ctx && slot < u.end && u.end <= p.mass.slots;
+      copy4(stage + 2 * kVec * 512 + (quad + 8 * t) * 4,
+            some ? p.mass.data + u.b * p.mass.seq_stride + u.head * p.mass.head_stride + slot : p.mass.data, some);
+    }
+    return lost;
   };
   RowGroup<kVec> rows[kGroups];
   const auto load_rows = [&](const Cursor& u, int row0) {
@@ -135,35 +155,50 @@ __global__ void __launch_bounds__(kWarps * 32, 1) mass_few_kernel(const __grid_c
     }
   };
 
+  // Tiles are started kStages - 1 ahead; each has a group of copies, and so has each turn when none are left.
   Cursor at = start.at, ahead = at;  // the tile at hand, the one whose pages are looked up
   int32_t page[2];
-  Tile<kVec> now, next;
+  uint32_t lost = 0;  // two bits a stage
+  int started = 0, to = 0, st = 0;
   bool fresh = true;  // a unit's first tile of the share
   look_up(ahead, page);
-  load(ahead, page, now);
-  if (n > 1) {
-    ahead.next(a, g);
-    look_up(ahead, page);
-  }
-  for (int u = 0; u < n; ++u) {
-    if (u + 1 < n) load(ahead, page, next);
-    if (u + 2 < n) {
-      ahead.next(a, g);
-      look_up(ahead, page);
+  const auto start_one = [&] {
+    if (started < n) {
+      lost = (lost & ~(3u << (2 * to))) | load(ahead, page, ring + to * R::kStage) << (2 * to);
+      if (++started < n) {
+        ahead.next(a, g);
+        look_up(ahead, page);
+      }
     }
+    to = to + 1 == kStages ? 0 : to + 1;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) start_one();
+  for (int u = 0; u < n; ++u) {
+    start_one();
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    const uint32_t stage = ring + st * R::kStage;
     const int have = at.s.n * g.group, slot0 = at.tile * kSlots + quad;
     const bool whole = slot0 - quad + kSlots <= at.s.ctx;  // all slots committed
     float w[2] = {0.f, 0.f};
     for (int row0 = 0; row0 < have; row0 += 8 * kGroups) {
       if (fresh || have > 8 * kGroups) load_rows(at, row0);
+      float scores[kGroups][4] = {};
+#pragma unroll
+      for (int x = 0; x < kVec; ++x) {
+        uint32_t k0[4], k1[4];
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(k0[0]), "=r"(k0[1]), "=r"(k0[2]), "=r"(k0[3]) : "r"(stage + x * 512 + lane * 16) : "memory");
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(k1[0]), "=r"(k1[1]), "=r"(k1[2]), "=r"(k1[3]) : "r"(stage + (kVec + x) * 512 + lane * 16) : "memory");
+#pragma unroll
+        for (int y = 0; y < kGroups; ++y) {
+          mma<T>(scores[y], k0[0], k1[0], k0[1], k1[1], rows[y].q[x].x, rows[y].q[x].y);
+          mma<T>(scores[y], k0[2], k1[2], k0[3], k1[3], rows[y].q[x].z, rows[y].q[x].w);
+        }
+      }
 #pragma unroll
       for (int y = 0; y < kGroups; ++y) {
-        float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < kVec; ++x) {
-          mma<T>(c, now.k[0][x].x, now.k[1][x].x, now.k[0][x].y, now.k[1][x].y, rows[y].q[x].x, rows[y].q[x].y);
-          mma<T>(c, now.k[0][x].z, now.k[1][x].z, now.k[0][x].w, now.k[1][x].w, rows[y].q[x].z, rows[y].q[x].w);
-        }
+        const float (&c)[4] = scores[y];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int token = rows[y].token[x];
@@ -192,16 +227,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) mass_few_kernel(const __grid_c
       if (lane == 0) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
     } else if (t < 2) {
       const int slot = slot0 + 8 * t;
-      const bool lost = t ? now.lost[1] : now.lost[0];
+      const bool gone = lost >> (2 * st + t) & 1;
       float m = t ? w[1] : w[0];
-      if (p.decay != 0.f && slot < at.s.ctx) m = fmaf(p.decay, now.old, m);
-      if (slot < at.end) p.mass.data[at.b * p.mass.seq_stride + at.head * p.mass.head_stride + slot] = lost ? NAN : m;
-      if (lost) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
+      if (p.decay != 0.f && slot < at.s.ctx) {
+        float old;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(old) : "r"(stage + 2 * kVec * 512 + (quad + 8 * t) * 4) : "memory");
+        m = fmaf(p.decay, old, m);
+      }
+      if (slot < at.end) p.mass.data[at.b * p.mass.seq_stride + at.head * p.mass.head_stride + slot] = gone ? NAN : m;
+      if (gone) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
     }
     const int b = at.b, head = at.head;
     at.next(a, g);
     fresh = at.b != b || at.head != head;
-    now = next;
+    st = st + 1 == kStages ? 0 : st + 1;
   }
 }
 
@@ -210,8 +249,22 @@ cudaError_t run(const MassParams& p, int sms, cudaStream_t stream) {
   int page_shift = -1;  // not a power of two
   for (int k = 0; k < 31; ++k)
     if (p.a.cache.page_size == 1 << k) page_shift = k;
-  const int grid = (int)std::min<int64_t>(sms, most_tiles(p.a, 1 << 30, kSlots));
-  return launch_dependent(mass_few_kernel<T, kVec, kGroups>, grid, kWarps * 32, stream, p, page_shift);
+  using R = Ring<kVec>;
+  const auto kern = mass_few_kernel<T, kVec, kGroups>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)R::kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(sms, most_tiles(p.a, 1 << 30, kSlots)));
+  cfg.blockDim = dim3(R::kWarps * 32);
+  cfg.dynamicSmemBytes = R::kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, kern, p, page_shift);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <typename T>
