@@ -58,11 +58,13 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool real) 
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 
-// Warps of a CTA and their rings.  A stage: 16-byte chunks t, t + 4, ... (t its place in the quad) of the keys of slots s and s + 8
+// Warps of a CTA, of which two share an SM, and their rings.  What is done for a tile takes as many warps as fit (one CTA, us for 256
+// sequences of up to 4,096 slots: 16 warps of 3 stages 221, 12 of 4 249, 8 of 6 334; two of 8 of 3 224, and a call of 37 slots 5.0
+// instead of 5.5).  A stage: 16-byte chunks t, t + 4, ... (t its place in the quad) of the keys of slots s and s + 8
 // of the tile (s the quad) of each lane, side by side for the warp; the old masses of the slots.
 template <int kVec>
 struct Ring {
-  static constexpr int kWarps = 16, kStages = kVec == 4 ? 3 : 5;
+  static constexpr int kWarps = 8, kStages = kVec == 4 ? 3 : 5;
   static constexpr int kStage = 2 * kVec * 512 + 64;
   static constexpr size_t kSmem = (size_t)kWarps * kStages * kStage;
 };
@@ -77,7 +79,7 @@ struct RowGroup {
 
 // kVec: chunks of a key that a lane has (D up to 32 kVec); kGroups: groups of eight rows taken at once.
 template <typename T, int kVec, int kGroups>
-__global__ void __launch_bounds__(Ring<kVec>::kWarps * 32, 1) mass_few_kernel(const __grid_constant__ MassParams p, const int page_shift) {
+__global__ void __launch_bounds__(Ring<kVec>::kWarps * 32, 2) mass_few_kernel(const __grid_constant__ MassParams p, const int page_shift) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   using R = Ring<kVec>;
@@ -254,7 +256,7 @@ cudaError_t run(const MassParams& p, int sms, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)R::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)std::min<int64_t>(sms, most_tiles(p.a, 1 << 30, kSlots)));
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(2 * sms, most_tiles(p.a, 1 << 30, kSlots)));
   cfg.blockDim = dim3(R::kWarps * 32);
   cfg.dynamicSmemBytes = R::kSmem;
   cfg.stream = stream;
