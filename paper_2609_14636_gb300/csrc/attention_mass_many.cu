@@ -47,7 +47,7 @@ struct Plan {
 };
 
 struct Barriers {
-  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][2], taken[2][2], sums[2], joined[2], drained[2];
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][2], taken[2][2], sums[2], joined[2], landed, drained[2];
 };
 
 // A place in a ring, and the parity of its barriers' phase.
@@ -140,18 +140,19 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t& all, int64_t* 
   return before + incl - v;
 }
 
-// tokens: of a block, whose rows are `tokens` times the group; k_stages: of the ring's stages, those of keys.
-template <typename T, int D>
+// tokens: of a block, whose rows are `tokens` times the group; k_stages: of the ring's stages, those of keys; both: a copy takes
+// both halves of a key's components.
+template <typename T, int D, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1)
     mass_many_kernel(const __grid_constant__ MassParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap q_map,
-                     const int box, const int page_shift, const int tokens, const int k_stages) {
+                     const int box, const int page_shift, const int tokens, const int k_stages, const bool both) {
   using L = Plan<D>;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ unsigned char dyn[];
   __shared__ Barriers bars;
   __shared__ __align__(16) float s_lse[kMaxStages][kCols];  // -lse log2 e of a block's columns
-  __shared__ uint32_t s_counts[kMaxStages][kCols / 32];  // columns that count
+  __shared__ __align__(16) uint32_t s_counts[kMaxStages][kCols / 32];  // columns that count
   __shared__ Step s_step[kMaxStages];         // of the step that starts with a tile
   __shared__ float s_sum[2][kSlots];
   __shared__ uint32_t s_lost[kMaxStages];                // boxes of a tile that have no page
@@ -178,9 +179,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars.keys[1][i], kTeamWarps);
       for (int j = 0; j < 2; ++j) {
         mbar_init(&bars.read[i][j], 1);
-        mbar_init(&bars.scores[i][j], 1);
+        mbar_init(&bars.scores[i][j], 2);
         mbar_init(&bars.taken[i][j], kTeamWarps / 2);
       }
+      if (i == 0) mbar_init(&bars.landed, 1);
       mbar_init(&bars.sums[i], kTeamWarps / 2);
       mbar_init(&bars.joined[i], kTeamWarps / 2);
       mbar_init(&bars.drained[i], 1);
@@ -247,25 +249,32 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- copies of keys ----
     const int boxes = kSlots / box;  // of a tile: at most 16
     const int bx = lane & (boxes - 1);
-    int32_t page = 0;
-    int row = 0;
-    bool some = false;
+    // The page of this lane's box of a tile, its first row there, where there is something to read; looked up two tiles ahead.
+    struct Box {
+      int32_t page, row;
+      bool some;
+    };
     const auto look_up = [&](const Cursor2& c) {
+      Box x = {0, 0, false};
+      if (c.pos >= end) return x;
       const int slot = c.tile * kSlots + bx * box;
-      some = slot < c.u.ctx + c.u.n;
-      if (some) {
+      x.some = slot < c.u.ctx + c.u.n;
+      if (x.some) {
         const int e = page_shift >= 0 ? slot >> page_shift : slot / pc.page_size;
-        row = slot - e * pc.page_size;
-        page = __ldg(pc.block_table + (int64_t)c.b * pc.table_stride + e);
+        x.row = slot - e * pc.page_size;
+        x.page = __ldg(pc.block_table + (int64_t)c.b * pc.table_stride + e);
       }
+      return x;
     };
     Place k;
     int t = 0;
-    if (at.pos < end) look_up(at);
+    Cursor2 ahead = at;
+    Box one = look_up(ahead);
+    if (ahead.pos < end) ahead.on(p, tokens, 1);
+    Box two = look_up(ahead);
     for (; at.pos < end; ++t) {
-      const bool real = some && page >= 0 && page < pc.n_pages, lost = some && !real;
-      const int now = page, now_row = row, head = at.head;
-      const int by = at.step(end);
+      const bool real = one.some && one.page >= 0 && one.page < pc.n_pages, lost = one.some && !real;
+      const int now = one.page, now_row = one.row, head = at.head, by = at.step(end);
       const Step step = {at.b * p.mass.seq_stride + head * p.mass.head_stride + at.tile * kSlots,
                          at.tile * kSlots - at.u.ctx,
                          at.u.n,
@@ -274,29 +283,45 @@ __global__ void __launch_bounds__(kThreads, 1)
                          at.u.blocks,
                          by | (at.run_ends(by, end) ? 4 : 0) | (at.pos + (int64_t)by * at.u.cost >= end ? 8 : 0)};
       at.on(p, tokens, 1);
-      if (at.pos < end) look_up(at);  // (the next tile's, on its way while this one waits for its stage)
+      if (ahead.pos < end) ahead.on(p, tokens, 1);
+      one = two;
+      two = look_up(ahead);
       if (t >= k_stages) {
         ok = __all_sync(0xffffffffu, wait(&bars.k_empty[k.st], k.parity ^ 1));
         if (!ok) break;
       }
       const unsigned mine = (1u << boxes) - 1;
       const unsigned gone = __ballot_sync(0xffffffffu, lost) & mine, who = __ballot_sync(0xffffffffu, real) & mine;
-      // (by one thread: from the lanes of a warp they are issued one after the other, at 90 clocks each)
+      // (by one thread, eight in a row: from the lanes of a warp they are issued one after the other, at 90 clocks each, and
+      // 150 where a thread is elected for each)
       uint64_t* bar = &bars.k_full[k.st];
       const uint32_t to = k_ring + k.st * L::kStage;
-      if (elect_one()) {
-        s_lost[k.st] = gone;
-        s_step[k.st] = step;
-        mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * L::kHalves * box * 128));
-      }
-      __syncwarp();
+      for (int x0 = 0; x0 < boxes; x0 += 8) {
+        int pages[8], rows[8];
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int from = __shfl_sync(0xffffffffu, now, x), first = __shfl_sync(0xffffffffu, now_row, x);
-        if ((who >> x & 1) && elect_one())
+        for (int x = 0; x < 8; ++x) {
+          pages[x] = __shfl_sync(0xffffffffu, now, x0 + x);
+          rows[x] = __shfl_sync(0xffffffffu, now_row, x0 + x);
+        }
+        if (elect_one()) {
+          if (x0 == 0) {
+            s_lost[k.st] = gone;
+            s_step[k.st] = step;
+            mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who) * L::kHalves * box * 128));
+          }
 #pragma unroll
-          for (int half = 0; half < L::kHalves; ++half)
-            copy_box(to + half * kSlots * 128 + x * box * 128, &k_map, half * 64, first, head, from, bar);
+          for (int x = 0; x < 8; ++x) {
+            const uint32_t there = to + (x0 + x) * L::kHalves * box * 128;  // (a box's halves side by side)
+            if (!(who >> (x0 + x) & 1)) continue;
+            if (L::kHalves == 2 && both) {
+              copy_box(there, &k_map, 0, rows[x], 0, head, pages[x], bar);
+            } else {
+#pragma unroll
+              for (int half = 0; half < L::kHalves; ++half) copy_box(there + half * box * 128, &k_map, half * 64, rows[x], head, pages[x], bar);
+            }
+          }
+        }
+        __syncwarp();
       }
       __syncwarp();
       k.on(k_stages);
@@ -308,8 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kWarps - 3) {
     // ---- copies of rows ----
-    // (A block's -lse are on their way while the one before waits for its stage: fetched in turn they took longer than a block
-    // takes, 115 us for the chains instead of ...)
+    // (A block's -lse are on their way while the one before waits for its stage.)
     int at_lse[kCols / 32];  // of a column: where its lse is past the block's first
 #pragma unroll
     for (int j = 0; j < kCols / 32; ++j) {
@@ -349,28 +373,44 @@ __global__ void __launch_bounds__(kThreads, 1)
     float lse[kCols / 32], next[kCols / 32];
     bool more = enter();
     if (more) fetch(lse);
+    uint32_t landed_parity = 0;
     while (more) {
-      const int head = at.head * group, token0 = at.u.off + blk * tokens;
+      const int head = at.head * group, token0 = at.u.off + blk * tokens, cols = min(tokens, at.u.n - blk * tokens) * group;
       more = on();
       if (more) fetch(next);
       if (t >= q_stages) {
         ok = __all_sync(0xffffffffu, wait(&bars.q_empty[q.st], q.parity ^ 1));
         if (!ok) break;
       }
+      // Rows past the block's last, up to a whole run of 32 columns, are zeros, and their columns' -lse is -inf: weights of 0.
       uint64_t* bar = &bars.q_full[q.st];
+      const bool ragged = cols % 32 != 0;
+      const uint32_t to = q_ring + q.st * L::kStage;
       if (elect_one()) {
-        mbar_arrive_expect_tx(bar, (uint32_t)(tokens * group * L::kHalves * 128));
+        uint64_t* land = ragged ? &bars.landed : bar;
+        mbar_arrive_expect_tx(land, (uint32_t)(tokens * group * L::kHalves * 128));
 #pragma unroll
-        for (int half = 0; half < L::kHalves; ++half)
-          copy_box(q_ring + q.st * L::kStage + half * kCols * 128, &q_map, half * 64, head, token0, 0, bar);
+        for (int half = 0; half < L::kHalves; ++half) copy_box(to + half * kCols * 128, &q_map, half * 64, head, token0, 0, land);
       }
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < kCols / 32; ++j) {
         const unsigned counts = __ballot_sync(0xffffffffu, lse[j] != -INFINITY);
-        s_lse[q.st][lane + 32 * j] = -lse[j] * kLog2e;
+        s_lse[q.st][lane + 32 * j] = lane + 32 * j < cols ? -lse[j] * kLog2e : -INFINITY;
         if (lane == 0) s_counts[q.st][j] = counts;
         lse[j] = next[j];
+      }
+      if (ragged) {
+        ok = __all_sync(0xffffffffu, wait(&bars.landed, landed_parity));
+        landed_parity ^= 1;
+        if (!ok) break;
+        for (int i = cols * 8 + lane; i < ((cols + 31) & ~31) * 8; i += 32)
+#pragma unroll
+          for (int half = 0; half < L::kHalves; ++half)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + half * kCols * 128 + i * 16), "r"(0) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
@@ -412,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               taken_parity[part] ^= 1;
               if (!ok) break;
               fence_after();
-              const uint32_t idesc = product<T>((min(cols - c, wide) + 15) & ~15, false);
+              const uint32_t idesc = product<T>((min(cols - c, wide) + 31) & ~31, false);
               const uint32_t b = q0 + q.st * (L::kStage >> 4) + (c * 128 >> 4), k = tmem + (2 * buffer + team) * L::kKeys;
               const uint32_t d = tmem + L::kScores + (2 * team + part) * kPart;
 #pragma unroll
@@ -423,6 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (blk + 1 >= at.u.blocks) commit(&bars.read[buffer][team]);
               }
               commit(&bars.scores[team][part]);
+              mbar_arrive(&bars.scores[team][part]);  // (what this thread knows, that -lse are there, goes with them)
             }
           }
           if (many || run_ends) q.on(q_stages);
@@ -475,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           fence_after();
           constexpr int kRegs = D / 4;  // D / 2 components
           uint32_t r[kRegs];
-          const uint32_t from = k_ring + k.st * L::kStage + (D == 128 ? part * kSlots * 128 : 0) + row * 128;
+          const uint32_t from = k_ring + k.st * L::kStage + ((row / box * L::kHalves + (D == 128 ? part : 0)) * box + row % box) * 128;
 #pragma unroll
           for (int c = 0; c < kRegs / 4; ++c) {
             const int chunk = (D == 128 ? 0 : part * 4) + c;
@@ -516,12 +557,34 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int blk = now.blk0; blk < now.blocks && ok; ++blk) {
           const int token0 = blk * tokens, cols = min(tokens, now.n - token0) * group;
           const int wide = part_of(cols), c0 = part * wide, c1 = min(cols, c0 + wide);  // this warp's columns: up to 32 or 64
-          if (many || fresh) ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
+          if ((many || fresh) && !(mine && c0 < c1)) ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
           if (mine && c0 < c1) {
             ok = ok && __all_sync(0xffffffffu, wait(&bars.scores[team][part], scores_parity));
             scores_parity ^= 1;
             if (!ok) break;
             fence_after();
+            const auto add = [&](const uint32_t (&r)[32], const float4* lse) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 4) {
+                const float4 l = lse[j / 4];
+                const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), scale2, make_float2(l.x, l.y));
+                const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), scale2, make_float2(l.z, l.w));
+                sum[0] = __fadd2_rn(sum[0], make_float2(ex2(x0.x), ex2(x0.y)));
+                sum[1] = __fadd2_rn(sum[1], make_float2(ex2(x1.x), ex2(x1.y)));
+              }
+            };
+            const uint2 counts = *reinterpret_cast<const uint2*>(&s_counts[q.st][c0 / 32]);
+            if (kWide && whole && c1 - c0 == kPart && (counts.x & counts.y) == 0xffffffffu) {  // all columns count for all slots
+              uint32_t r0[32], r1[32];
+              tmem_load32(r0, my_scores);
+              tmem_load32(r1, my_scores + 32);
+              tmem_wait_load();
+              fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+              add(r0, reinterpret_cast<const float4*>(&s_lse[q.st][c0]));
+              add(r1, reinterpret_cast<const float4*>(&s_lse[q.st][c0 + 32]));
+            } else
 #pragma unroll 1
             for (int c = c0; c < c1; c += 32) {
               const uint32_t from = my_scores + c - c0;
@@ -557,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 continue;
               }
-              if (full && n == 32) {
+              if (full) {  // (columns past the last have weights of 0)
                 uint32_t r[32];
                 tmem_load32(r, from);
                 tmem_wait_load();
@@ -566,14 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   __syncwarp();
                   if (lane == 0) mbar_arrive(&bars.taken[team][part]);
                 }
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                  const float4 l = lse[j / 4];
-                  const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), scale2, make_float2(l.x, l.y));
-                  const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), scale2, make_float2(l.z, l.w));
-                  sum[0] = __fadd2_rn(sum[0], make_float2(ex2(x0.x), ex2(x0.y)));
-                  sum[1] = __fadd2_rn(sum[1], make_float2(ex2(x1.x), ex2(x1.y)));
-                }
+                add(r, lse);
                 continue;
               }
               // (eight columns at a time, in a loop: unrolled with the others' this took so many registers that the whole kernel
@@ -647,15 +703,19 @@ int slots_of_a_box(int page_size) {
   return box;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kWide>
 cudaError_t run(const MassParams& p, bool bf16, int sms, cudaStream_t stream) {
   using L = Plan<D>;
-  const auto kern = mass_many_kernel<T, D>;
+  const auto kern = mass_many_kernel<T, D, kWide>;
   const PagedCache& c = p.a.cache;
   const int box = slots_of_a_box(c.page_size), group = p.a.Hq / c.n_heads, tokens = kCols / group;
   CUtensorMap k_map, q_map;
-  if (!describe(&k_map, c.k, bf16, {p.a.D, c.page_size, c.n_heads, c.n_pages}, {c.row_stride, c.head_stride, c.page_stride}, {box, 1, 1}) ||
-      !describe(&q_map, p.a.q, bf16, {p.a.D, p.a.Hq, p.a.n_tokens, 1}, {p.a.q_head, p.a.q_tok, 0}, {group, tokens, 1}))
+  const bool both = p.a.D == 128;  // (of fewer components what follows them would be read)
+  if (!(both ? describe<5>(&k_map, c.k, bf16, {64, c.page_size, 2, c.n_heads, c.n_pages}, {c.row_stride, 64, c.head_stride, c.page_stride},
+                           {box, 2, 1, 1})
+             : describe<4>(&k_map, c.k, bf16, {p.a.D, c.page_size, c.n_heads, c.n_pages}, {c.row_stride, c.head_stride, c.page_stride},
+                           {box, 1, 1})) ||
+      !describe<4>(&q_map, p.a.q, bf16, {p.a.D, p.a.Hq, p.a.n_tokens, 1}, {p.a.q_head, p.a.q_tok, 0}, {group, tokens, 1}))
     return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmem);
   if (e != cudaSuccess) return e;
@@ -672,7 +732,7 @@ cudaError_t run(const MassParams& p, bool bf16, int sms, cudaStream_t stream) {
   // units of several blocks stream the rows past the keys, others the keys past the rows
   const int64_t mean = (p.a.n_tokens + c.n_seqs - 1) / c.n_seqs;
   const int k_stages = mean > tokens ? L::kStages / 3 : L::kStages * 2 / 3;
-  e = cudaLaunchKernelEx(&cfg, kern, p, k_map, q_map, box, page_shift(c.page_size), tokens, k_stages);
+  e = cudaLaunchKernelEx(&cfg, kern, p, k_map, q_map, box, page_shift(c.page_size), tokens, k_stages, both);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -687,9 +747,15 @@ bool attention_mass_many_takes(const MassParams& p) {
 }
 
 cudaError_t launch_attention_mass_many(const MassParams& p, int dtype, int sms, cudaStream_t stream) {
-  if (dtype == STRIDE_DTYPE_BF16)
-    return p.a.D <= 64 ? run<__nv_bfloat16, 64>(p, true, sms, stream) : run<__nv_bfloat16, 128>(p, true, sms, stream);
-  return p.a.D <= 64 ? run<__half, 64>(p, false, sms, stream) : run<__half, 128>(p, false, sms, stream);
+  // (wide: 64 scores of a lane at once, for which parts of fewer columns have no use, and pay in registers)
+  const bool wide = ((p.a.n_tokens + p.a.cache.n_seqs - 1) / p.a.cache.n_seqs) * (p.a.Hq / p.a.cache.n_heads) > kPart;
+  const bool bf16 = dtype == STRIDE_DTYPE_BF16;
+  const auto of = [&](auto type) {
+    using T = decltype(type);
+    if (p.a.D <= 64) return wide ? run<T, 64, true>(p, bf16, sms, stream) : run<T, 64, false>(p, bf16, sms, stream);
+    return wide ? run<T, 128, true>(p, bf16, sms, stream) : run<T, 128, false>(p, bf16, sms, stream);
+  };
+  return bf16 ? of(__nv_bfloat16()) : of(__half());
 }
 
 }  // namespace stride

@@ -86,6 +86,13 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_u32(bar))
+      : "memory");
+}
+
 // cuTensorMapEncodeTiled, from the driver that the runtime has loaded.
 using Encode = decltype(&cuTensorMapEncodeTiled);
 inline Encode encoder() {
@@ -102,17 +109,22 @@ inline Encode encoder() {
   return f;
 }
 
-// A tensor of four dimensions of 16-bit components, the innermost of unit stride (the others' in elements), read in boxes of 64
+// A tensor of N dimensions of 16-bit components, the innermost of unit stride (the others' in elements), read in boxes of 64
 // components (128 bytes, swizzled); what lies past an extent is zeros.
-inline bool describe(CUtensorMap* map, const void* base, bool bf16, const int64_t (&extent)[4], const int64_t (&stride)[3], const int (&box)[3]) {
+template <int N>
+bool describe(CUtensorMap* map, const void* base, bool bf16, const int64_t (&extent)[N], const int64_t (&stride)[N - 1], const int (&box)[N - 1]) {
   const Encode encode = encoder();
   if (!encode) return false;
   const cuuint64_t row = (cuuint64_t)((extent[0] * 2 + 15) / 16 * 16);  // (any stride will do where there is one of a kind)
-  cuuint64_t dims[4], strides[3];
-  for (int i = 0; i < 4; ++i) dims[i] = (cuuint64_t)extent[i];
-  for (int i = 0; i < 3; ++i) strides[i] = extent[i + 1] > 1 ? (cuuint64_t)stride[i] * 2 : row;
-  const cuuint32_t boxes[4] = {64, (cuuint32_t)box[0], (cuuint32_t)box[1], (cuuint32_t)box[2]}, steps[4] = {1, 1, 1, 1};
-  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, boxes,
+  cuuint64_t dims[N], strides[N - 1];
+  cuuint32_t boxes[N], steps[N];
+  for (int i = 0; i < N; ++i) {
+    dims[i] = (cuuint64_t)extent[i];
+    boxes[i] = i == 0 ? 64 : (cuuint32_t)box[i - 1];
+    steps[i] = 1;
+  }
+  for (int i = 0; i < N - 1; ++i) strides[i] = extent[i + 1] > 1 ? (cuuint64_t)stride[i] * 2 : row;
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, N, const_cast<void*>(base), dims, strides, boxes,
                 steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

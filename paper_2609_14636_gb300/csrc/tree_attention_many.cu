@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // The cache as components x rows of a page x heads x pages, read in boxes of `box` rows.
 bool describe_cache(CUtensorMap* map, const void* base, const AttentionParams& p, int dtype, int box) {
   const PagedCache& c = p.cache;
-  return describe(map, base, dtype == STRIDE_DTYPE_BF16, {p.D, c.page_size, c.n_heads, c.n_pages}, {c.row_stride, c.head_stride, c.page_stride},
+  return describe<4>(map, base, dtype == STRIDE_DTYPE_BF16, {p.D, c.page_size, c.n_heads, c.n_pages}, {c.row_stride, c.head_stride, c.page_stride},
                   {box, 1, 1});
 }
 
