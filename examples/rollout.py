@@ -6,6 +6,11 @@ and scoring is the library's:
     projections -> stride_kv_append (norm, rotation, paged cache) -> stride_tree_attention
     -> logits -> stride_sample -> stride_score_step_compact -> (stop, restart)
 
+A rollout that outgrows its cache goes on with the slots that its attention used most:
+
+    stride_tree_attention -> stride_attention_mass -> (cache full) stride_kv_evict
+    logits -> stride_logit_controls (penalties, a grammar's mask) -> stride_sample
+
 The student then learns from what it wrote (the OPD loss over the kept tokens), with
 stride_qk_norm_rope and its backward pass in its layers.
 
@@ -57,6 +62,26 @@ class Model:
                       for _ in range(shape.layers)]
         self.table = torch.randperm(slots * pages, generator=g, device=device).int().view(slots, pages)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.mass = None
+
+    def watch(self):
+        """From here on each call adds up what attention weight the cached slots get, and evict() may be called."""
+        s = self.s
+        self.mass = [torch.zeros(self.slots, s.kv_heads, s.longest, device=self.device) for _ in self.layers]
+        self.lse = None
+        self.spare = [tuple(torch.empty_like(c) for c in cache) for cache in self.cache]  # (the pages of the next eviction)
+
+    def evict(self, ctx_len, budget, sink=2, recent=8):
+        """Keeps `budget` slots of each sequence and kv head (negative: all) and returns how many are cached then.  The pages that they
+        came from stay as they are until the next eviction."""
+        s, B = self.s, self.slots
+        new_len, kept = torch.empty_like(ctx_len), torch.empty(B, s.kv_heads, s.longest, dtype=torch.int32, device=self.device)
+        for i, (cache, spare) in enumerate(zip(self.cache, self.spare)):
+            mass = torch.zeros_like(self.mass[i])
+            stride.stride_kv_evict(*cache, self.table, ctx_len, self.mass[i], budget, *spare, self.table, new_len, kept, mass_to=mass,
+                                   sink=sink, recent=recent, dev_status=self.status)
+            self.mass[i], self.cache[i], self.spare[i] = mass, spare, cache
+        return new_len
 
     def __call__(self, tokens, position, ctx_len, tok_off, tree_mask=None):
         """Logits [N, vocab] of the new tokens; their keys and values are in the slots from each ctx_len on."""
@@ -66,13 +91,17 @@ class Model:
         out = torch.empty_like(q_out)
         work = torch.empty(stride.stride_tree_attention_workspace_size(N, s.heads, s.kv_heads, s.head_dim), dtype=torch.uint8, device=self.device)
         norm = lambda x: x * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6).bfloat16()  # noqa: E731
-        for layer, (k_cache, v_cache) in zip(self.layers, self.cache):
+        lse = None if self.mass is None else torch.empty(N, s.heads, device=self.device)
+        for i, (layer, (k_cache, v_cache)) in enumerate(zip(self.layers, self.cache)):
             q, k, v = (norm(x) @ layer["qkv"].T).view(N, -1, s.head_dim).split([s.heads, s.kv_heads, s.kv_heads], dim=1)
             self.kv.append((k, v))
             stride.stride_kv_append(k, v, k_cache, v_cache, self.table, ctx_len, tok_off, pos=position, cos=self.cos, sin=self.sin,
                                     k_weight=layer["kn"], q=q, q_out=q_out, q_weight=layer["qn"], dev_status=self.status)
             stride.stride_tree_attention(q_out, k_cache, v_cache, self.table, ctx_len, tok_off, tree_mask, s.head_dim ** -0.5, out,
-                                         workspace=work, dev_status=self.status)
+                                         lse=lse, workspace=work, dev_status=self.status)
+            if self.mass is not None:
+                stride.stride_attention_mass(q_out, lse, k_cache, self.table, ctx_len, tok_off, tree_mask, s.head_dim ** -0.5,
+                                             self.mass[i], dev_status=self.status)
             x = x + out.view(N, -1) @ layer["out"].T
             x = x + torch.nn.functional.silu(norm(x) @ layer["up"].T) @ layer["down"].T
         return norm(x) @ self.head.T
@@ -167,6 +196,37 @@ def draft_step(model, ctx_len, last, seed):
     return token, accepted, logits
 
 
+def write_on(model, prompts, steps, budget, seed, repetition=1.1, presence=0.2, allowed=None):
+    """Writes `steps` tokens after each prompt, with no more than `budget` slots of the cache for a sequence once it has been
+    filled.  Tokens that a sequence has are penalised; allowed: a mask of the vocabulary's tokens (bits of int32 words) or
+    None.  Returns the tokens, the number of evictions and the cached slots."""
+    dev, (B, prompt), V = prompts.device, prompts.shape, model.s.vocab
+    g = torch.Generator(device=dev).manual_seed(seed)
+    model.watch()
+    history = torch.cat([prompts, torch.full((B, steps), -1, dtype=torch.int32, device=dev)], dim=1)
+    ctx_len, counts = torch.zeros(B, dtype=torch.int32, device=dev), torch.full((B,), prompt - 1, device=dev)
+    model(prompts[:, :-1].reshape(-1), chain(ctx_len, counts), ctx_len, offsets(counts))
+    ctx_len += counts.int()
+    one, made = offsets(torch.ones_like(counts)), 0
+    position = torch.full((B,), prompt - 1, dtype=torch.int32, device=dev)  # (goes on counting where slots are evicted)
+    token, raw = torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, V, dtype=torch.bfloat16, device=dev)
+    length, prompt_len = torch.full_like(token, prompt), torch.full_like(token, prompt)
+    for step in range(steps):
+        if int(ctx_len.max()) >= 2 * budget:
+            ctx_len, made = model.evict(ctx_len, budget), made + 1
+        raw.copy_(model(history[:, prompt - 1 + step].contiguous(), position, ctx_len, one))
+        ctx_len, position = ctx_len + 1, position + 1
+        logits = torch.empty_like(raw)  # (the raw ones are what a scoring step takes)
+        stride.stride_logit_controls(raw, logits, history=history, history_len=length, prompt_len=prompt_len, repetition=repetition,
+                                     presence=presence, allowed=allowed, dev_status=model.status)
+        stride.stride_sample(logits, torch.empty(B, V, device=dev).exponential_(generator=g), token, temperature=0.9, top_p=0.95,
+                             dev_status=model.status)
+        history[:, prompt + step] = token
+        length += 1
+    assert int(model.status) == 0
+    return history[:, prompt:], made, ctx_len
+
+
 class QkNormRope(torch.autograd.Function):
     """stride_qk_norm_rope where gradients flow; q, k [N, heads, D] of a layer, norm weights [D]."""
 
@@ -255,6 +315,8 @@ def main(B=16, turn_len=8, turns=6, prompt=40):
     print(f"restarted after {reused.tolist()} reused tokens, {sum(map(len, second.tokens))} new ones")
     token, accepted, _ = draft_step(student, ctx_len, torch.tensor([t[-1] for t in second.tokens], dtype=torch.int32, device=dev), seed=7)
     print(f"drafted step: {int((accepted > 0).sum())} of {B} guesses accepted")
+    written, evictions, cached = write_on(Model(shape, B, 1), prompts, 2 * prompt, prompt, seed=8)
+    print(f"{written.numel()} tokens more under a budget of {prompt} slots: {evictions} evictions, {int(cached.max())} slots cached")
     gap = [learn(student, teacher, prompts, first.tokens, rate=0.02) for _ in range(2)]
     print(f"mean of log p_S - log p_T over the rollouts: {gap[0]:.4f}, after a step {gap[1]:.4f}")
     return student, teacher, prompts, first, second
