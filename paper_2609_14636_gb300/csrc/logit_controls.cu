@@ -64,6 +64,31 @@ constexpr int kMostWords = 8192;  // of a slice's bits
 constexpr int kWindow = 4096;     // places that have counts at a time
 constexpr uint32_t kPrompt = 0x80000000u, kBias = 0x40000000u;  // flags of a count
 
+// What applies to a row.
+struct Applies {
+  float rep, freq, pres;
+  int n, prompt, bias0, biases, bad;
+};
+__device__ __forceinline__ Applies applies_to(const stride_logit_rules& r, int row) {
+  Applies a = {1.f, 0.f, 0.f, 0, 0, 0, 0, 0};
+  if (r.history) {
+    a.n = __ldg(r.history_len + row);
+    a.prompt = r.prompt_len ? __ldg(r.prompt_len + row) : 0;
+    a.rep = r.repetition ? __ldg(r.repetition + row) : r.repetition_all;
+    a.freq = r.frequency ? __ldg(r.frequency + row) : r.frequency_all;
+    a.pres = r.presence ? __ldg(r.presence + row) : r.presence_all;
+    if (a.n < 0 || a.n > r.history_most) a.bad |= STRIDE_DEV_BAD_LAYOUT;
+    if (!(a.rep > 0.f && isfinite(a.rep)) || !isfinite(a.freq) || !isfinite(a.pres)) a.bad |= STRIDE_DEV_BAD_CONTROL;
+  }
+  if (r.bias_off) {
+    a.bias0 = __ldg(r.bias_off + row);
+    const int end = __ldg(r.bias_off + row + 1);
+    if (a.bias0 < 0 || end < a.bias0 || end > r.n_bias) a.bad |= STRIDE_DEV_BAD_LAYOUT;
+    a.biases = end - a.bias0;
+  }
+  return a;
+}
+
 // A run of a lane: kAhead vectors, 32 lanes' side by side, and the words of the mask that they need.
 struct Run {
   int first;  // the lane's first vector; past the last: none
@@ -80,6 +105,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   constexpr int kVec = 16 / (int)sizeof(T);
   constexpr uint32_t kFull = (1u << kVec) - 1;
   extern __shared__ __align__(16) uint32_t smem[];
+  __shared__ Applies s_applies;
   __shared__ int s_run, s_total, s_part[kThreads / 32];
   const int words = slice / 32;
   uint32_t* const bits = smem;
@@ -95,33 +121,9 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   const bool in_place = p.x == p.out;
   const uint32_t* const mask = mask_row(r, row);
   if (tid == 0) s_run = 0;
+  __syncthreads();
 
-  // ---- what applies to the row ----
-  float rep = 1.f, freq = 0.f, pres = 0.f;
-  int n = 0, prompt = 0, bias0 = 0, biases = 0, bad = 0;
-  if (r.history) {
-    n = __ldg(r.history_len + row);
-    prompt = r.prompt_len ? __ldg(r.prompt_len + row) : 0;
-    rep = r.repetition ? __ldg(r.repetition + row) : r.repetition_all;
-    freq = r.frequency ? __ldg(r.frequency + row) : r.frequency_all;
-    pres = r.presence ? __ldg(r.presence + row) : r.presence_all;
-    if (n < 0 || n > r.history_most) bad |= STRIDE_DEV_BAD_LAYOUT;
-    if (!(rep > 0.f && isfinite(rep)) || !isfinite(freq) || !isfinite(pres)) bad |= STRIDE_DEV_BAD_CONTROL;
-  }
-  if (r.bias_off) {
-    bias0 = __ldg(r.bias_off + row);
-    const int end = __ldg(r.bias_off + row + 1);
-    if (bias0 < 0 || end < bias0 || end > r.n_bias) bad |= STRIDE_DEV_BAD_LAYOUT;
-    biases = end - bias0;
-  }
-  if (bad) {  // (all of the row's CTAs alike)
-    for (int c = c0 + tid; c < c1; c += kThreads) out[c] = rounded<T>(NAN);
-    if (tid == 0) set_status(p.dev_status, bad);
-    return;
-  }
   const int32_t* const history = r.history + row * r.history_stride;
-  const int32_t* const bias_token = r.bias_token + bias0;
-  const bool any = n > 0 || biases > 0;
   // f(i, place in the slice) for this thread's tokens of a list, of `by` threads
   const auto each = [&](const int32_t* list, int len, int me, int by, auto&& f) {
     constexpr int kOnce = 8;
@@ -136,23 +138,23 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   const auto inside = [&](int t) { return t >= c0 && t < c1; };
   const auto place = [&](int t) { return before[t >> 5] + __popc(bits[t >> 5] & ((1u << (t & 31)) - 1)); };
   // Counts, tokens and biases of places w0 .. w0 + kWindow - 1, by all of `by` threads; `sync` between its steps.
-  const auto fill = [&](uint32_t w0, int me, int by, auto&& sync) {
+  const auto fill = [&](const Applies& h, uint32_t w0, int me, int by, auto&& sync) {
     for (int i = me; i < kWindow / 4; i += by) {
       reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
-      if (biases) reinterpret_cast<uint4*>(entry)[i] = make_uint4(0, 0, 0, 0);
+      if (h.biases) reinterpret_cast<uint4*>(entry)[i] = make_uint4(0, 0, 0, 0);
     }
     sync();
-    each(history, n, me, by, [&](int i, int t) {
+    each(history, h.n, me, by, [&](int i, int t) {
       if (!inside(t)) return;
       const uint32_t k = place(t - c0) - w0;
       if (k >= kWindow) return;
       token[k] = t;
-      if (i < prompt)
+      if (i < h.prompt)
         atomicOr(&count[k], kPrompt);
       else
         atomicAdd(&count[k], 1u);
     });
-    each(bias_token, biases, me, by, [&](int i, int t) {
+    each(r.bias_token + h.bias0, h.biases, me, by, [&](int i, int t) {
       if (!inside(t)) return;
       const uint32_t k = place(t - c0) - w0;
       if (k >= kWindow) return;
@@ -161,46 +163,68 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       atomicMax(&entry[k], (uint32_t)i + 1);  // (of several entries the last)
     });
   };
-  __syncthreads();
 
   // ---- which tokens occur, and how often ----
-  if (any && tid < counters) {
+  const bool fixes = r.history || r.bias_off;
+  if (fixes && tid < counters) {
     const auto sync = [&] { asm volatile("bar.sync 1, %0;" ::"r"(counters) : "memory"); };
-    for (int i = tid; i < words / 4; i += counters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
-    sync();
-    const auto set = [&](int, int t) {
-      if (inside(t))
-        atomicOr(&bits[(t - c0) >> 5], 1u << ((t - c0) & 31));
-      else if (t >= p.V && c0 == 0)
-        set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
-    };
-    each(history, n, tid, counters, set);
-    each(bias_token, biases, tid, counters, set);
-    sync();
-    int base = 0;  // bits before the words at hand
-    for (int i0 = 0; i0 < words; i0 += counters) {
-      const int i = i0 + tid, own = i < words ? __popc(bits[i]) : 0;
-      int upto = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-      }
-      if (lane == 31) s_part[tid >> 5] = upto;
+    const Applies h = applies_to(r, row);
+    if (tid == 0) s_applies = h;
+    const bool any = !h.bad && (h.n > 0 || h.biases > 0);
+    if (tid == 0) s_total = 0;
+    if (any) {
+      for (int i = tid; i < words / 4; i += counters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
       sync();
-      int all = 0;
+      const auto set = [&](int, int t) {
+        if (inside(t))
+          atomicOr(&bits[(t - c0) >> 5], 1u << ((t - c0) & 31));
+        else if (t >= p.V && c0 == 0)
+          set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
+      };
+      each(history, h.n, tid, counters, set);
+      each(r.bias_token + h.bias0, h.biases, tid, counters, set);
+      sync();
+      // bits before each word: a warp's run of words by itself, four words of a lane at a time, then the warps' sums
+      const int warp = tid >> 5, warps = counters >> 5, run = (words + 128 * warps - 1) / (128 * warps) * 128;
+      const int i1 = min(words, (warp + 1) * run);
+      int base = 0;
+      for (int i0 = warp * run; i0 < i1; i0 += 128) {
+        const int i = i0 + lane * 4;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (i < i1) w = *reinterpret_cast<const uint4*>(bits + i);
+        const int c[4] = {__popc(w.x), __popc(w.y), __popc(w.z), __popc(w.w)};
+        const int own = c[0] + c[1] + c[2] + c[3];
+        int upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += v;
+        }
+        const int first = base + upto - own;
+        if (i < i1) *reinterpret_cast<uint4*>(before + i) = make_uint4(first, first + c[0], first + c[0] + c[1], first + c[0] + c[1] + c[2]);
+        base += __shfl_sync(0xffffffffu, upto, 31);
+      }
+      if (lane == 0) s_part[warp] = base;
+      sync();
+      int others = 0, all = 0;
 #pragma unroll
       for (int w = 0; w < kThreads / 32; ++w) {
-        const int v = w < counters >> 5 ? s_part[w] : 0;
-        if (w < tid >> 5) upto += v;
+        const int v = w < warps ? s_part[w] : 0;
+        if (w < warp) others += v;
         all += v;
       }
-      if (i < words) before[i] = base + upto - own;
-      base += all;
+      for (int i = warp * run + lane * 4; i < i1; i += 128) {
+        uint4 w = *reinterpret_cast<const uint4*>(before + i);
+        w.x += others;
+        w.y += others;
+        w.z += others;
+        w.w += others;
+        *reinterpret_cast<uint4*>(before + i) = w;
+      }
+      if (tid == 0) s_total = all;
       sync();
+      fill(h, 0, tid, counters, sync);
     }
-    if (tid == 0) s_total = base;
-    fill(0, tid, counters, sync);
   }
 
   // ---- the slice with the mask ----
@@ -264,12 +288,18 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
     const int tail = head + vecs * kVec + tid;
     if (tail < c1) one(tail);
   }
-  if (!any) return;
+  if (!fixes) return;
   __syncthreads();
 
   // ---- the tokens that something applies to ----
+  const Applies h = s_applies;
+  if (h.bad) {  // (all of the row's CTAs alike)
+    for (int c = c0 + tid; c < c1; c += kThreads) out[c] = rounded<T>(NAN);
+    if (tid == 0) set_status(p.dev_status, h.bad);
+    return;
+  }
   const auto sync = [] { __syncthreads(); };
-  for (int w0 = 0;; w0 += kWindow) {
+  for (int w0 = 0; w0 < s_total; w0 += kWindow) {
     const int here = min(kWindow, s_total - w0);
     constexpr int kOnce = 4;  // logits of a thread on their way
     for (int i0 = tid; i0 < here; i0 += kOnce * kThreads) {
@@ -282,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
         const int t = token[i];
         y[u] = value(x[t]);
         word[u] = mask ? __ldg(mask + (t >> 5)) : 0xffffffffu;
-        bias[u] = count[i] & kBias ? __ldg(r.bias + bias0 + entry[i] - 1) : 0.f;
+        bias[u] = count[i] & kBias ? __ldg(r.bias + h.bias0 + entry[i] - 1) : 0.f;
       }
 #pragma unroll
       for (int u = 0; u < kOnce; ++u) {
@@ -291,15 +321,15 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
         const int t = token[i];
         if (!(word[u] >> (t & 31) & 1)) continue;
         const uint32_t seen = count[i], made = seen & ~(kPrompt | kBias);
-        if (seen & ~kBias) y[u] = y[u] > 0.f ? __fdiv_rn(y[u], rep) : y[u] * rep;
-        if (made) y[u] = y[u] - freq * (float)made - pres;
+        if (seen & ~kBias) y[u] = y[u] > 0.f ? __fdiv_rn(y[u], h.rep) : y[u] * h.rep;
+        if (made) y[u] = y[u] - h.freq * (float)made - h.pres;
         if (seen & kBias) y[u] += bias[u];
         out[t] = rounded<T>(y[u]);
       }
     }
     if (w0 + kWindow >= s_total) break;
     __syncthreads();
-    fill(w0 + kWindow, tid, kThreads, sync);
+    fill(h, w0 + kWindow, tid, kThreads, sync);
     __syncthreads();
   }
 }
