@@ -123,11 +123,37 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   if (tid == 0) s_run = 0;
   __syncthreads();
 
+  // ---- a first run of the slice on its way ----
+  const bool streams = !in_place || mask;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(x + c0);
+  const bool apart = ((at ^ reinterpret_cast<uintptr_t>(out + c0)) & 15) != 0;  // (no vector of one is one of the other)
+  const int head = min(c1, c0 + (int)(((16 - (at & 15)) & 15) / sizeof(T))), vecs = streams && !apart ? (c1 - head) / kVec : 0;
+  const auto take = [&](Run& u) {  // the next run
+    int k = 0;
+    if (lane == 0) k = atomicAdd(&s_run, 1);
+    u.first = __shfl_sync(0xffffffffu, k, 0) * 32 * kAhead + lane;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = u.first + 32 * j;
+      if (i < vecs) u.v[j] = *(reinterpret_cast<const uint4*>(x + head) + i);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = u.first + 32 * j, c = head + i * kVec, w = c >> 5;
+      u.lo[j] = u.hi[j] = 0xffffffffu;
+      if (!mask || i >= vecs) continue;
+      u.lo[j] = __ldg(mask + w);
+      if ((c & 31) + kVec > 32 && (w + 1) * 32 < p.V) u.hi[j] = __ldg(mask + w + 1);
+    }
+  };
+  Run a;
+  take(a);
+
   const int32_t* const history = r.history + row * r.history_stride;
   // f(i, place in the slice) for this thread's tokens of a list, of `by` threads
-  const auto each = [&](const int32_t* list, int len, int me, int by, auto&& f) {
-    constexpr int kOnce = 8;
-    for (int64_t i0 = me; i0 < len; i0 += kOnce * by) {
+  constexpr int kOnce = 8;
+  const auto each = [&](const int32_t* list, int64_t from, int len, int by, auto&& f) {  // (from: this thread's first)
+    for (int64_t i0 = from; i0 < len; i0 += kOnce * by) {
       int t[kOnce];
 #pragma unroll
       for (int u = 0; u < kOnce; ++u) t[u] = i0 + (int64_t)u * by < len ? __ldg(list + i0 + (int64_t)u * by) : -1;
@@ -137,14 +163,15 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   };
   const auto inside = [&](int t) { return t >= c0 && t < c1; };
   const auto place = [&](int t) { return before[t >> 5] + __popc(bits[t >> 5] & ((1u << (t & 31)) - 1)); };
-  // Counts, tokens and biases of places w0 .. w0 + kWindow - 1, by all of `by` threads; `sync` between its steps.
-  const auto fill = [&](const Applies& h, uint32_t w0, int me, int by, auto&& sync) {
+  // Counts, tokens and biases of places w0 .. w0 + kWindow - 1, by all of `by` threads; `sync` between its steps.  held: this
+  // thread's first tokens of the history, if it has them, at first, first + by, ...
+  const auto fill = [&](const Applies& h, uint32_t w0, int me, int by, const int* held, auto&& sync) {
     for (int i = me; i < kWindow / 4; i += by) {
       reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
       if (h.biases) reinterpret_cast<uint4*>(entry)[i] = make_uint4(0, 0, 0, 0);
     }
     sync();
-    each(history, h.n, me, by, [&](int i, int t) {
+    const auto count_one = [&](int i, int t) {
       if (!inside(t)) return;
       const uint32_t k = place(t - c0) - w0;
       if (k >= kWindow) return;
@@ -153,8 +180,12 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
         atomicOr(&count[k], kPrompt);
       else
         atomicAdd(&count[k], 1u);
-    });
-    each(r.bias_token + h.bias0, h.biases, me, by, [&](int i, int t) {
+    };
+    if (held)
+#pragma unroll
+      for (int u = 0; u < kOnce; ++u) count_one(me + u * by, held[u]);
+    each(history, me + (held ? (int64_t)kOnce * by : 0), h.n, by, count_one);
+    each(r.bias_token + h.bias0, me, h.biases, by, [&](int i, int t) {
       if (!inside(t)) return;
       const uint32_t k = place(t - c0) - w0;
       if (k >= kWindow) return;
@@ -168,7 +199,16 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   const bool fixes = r.history || r.bias_off;
   if (fixes && tid < counters) {
     const auto sync = [&] { asm volatile("bar.sync 1, %0;" ::"r"(counters) : "memory"); };
+    int held[kOnce];  // (on their way with what says how many count)
+#pragma unroll
+    for (int u = 0; u < kOnce; ++u) {
+      const int64_t i = tid + (int64_t)u * counters;
+      held[u] = r.history && i < r.history_most ? __ldg(history + i) : -1;
+    }
     const Applies h = applies_to(r, row);
+#pragma unroll
+    for (int u = 0; u < kOnce; ++u)
+      if (tid + u * counters >= h.n) held[u] = -1;
     if (tid == 0) s_applies = h;
     const bool any = !h.bad && (h.n > 0 || h.biases > 0);
     if (tid == 0) s_total = 0;
@@ -181,8 +221,10 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
         else if (t >= p.V && c0 == 0)
           set_status(p.dev_status, STRIDE_DEV_TOKEN_RANGE);
       };
-      each(history, h.n, tid, counters, set);
-      each(r.bias_token + h.bias0, h.biases, tid, counters, set);
+#pragma unroll
+      for (int u = 0; u < kOnce; ++u) set(0, held[u]);
+      each(history, tid + (int64_t)kOnce * counters, h.n, counters, set);
+      each(r.bias_token + h.bias0, tid, h.biases, counters, set);
       sync();
       // bits before each word: a warp's run of words by itself, four words of a lane at a time, then the warps' sums
       const int warp = tid >> 5, warps = counters >> 5, run = (words + 128 * warps - 1) / (128 * warps) * 128;
@@ -223,14 +265,12 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       }
       if (tid == 0) s_total = all;
       sync();
-      fill(h, 0, tid, counters, sync);
+      fill(h, 0, tid, counters, held, sync);
     }
   }
 
   // ---- the slice with the mask ----
-  const uintptr_t at = reinterpret_cast<uintptr_t>(x + c0);
-  if (in_place && !mask) {
-  } else if (((at ^ reinterpret_cast<uintptr_t>(out + c0)) & 15) != 0) {  // no vector of one is one of the other
+  if (apart) {
     T v[8];
     for (int c = c0 + tid; c < c1; c += 8 * kThreads) {
 #pragma unroll
@@ -240,26 +280,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       for (int u = 0; u < 8; ++u)
         if (c + u * kThreads < c1) out[c + u * kThreads] = is_allowed(mask, c + u * kThreads) ? v[u] : rounded<T>(-INFINITY);
     }
-  } else {
-    const int head = min(c1, c0 + (int)(((16 - (at & 15)) & 15) / sizeof(T))), vecs = (c1 - head) / kVec;
-    const auto take = [&](Run& u) {  // the next run
-      int k = 0;
-      if (lane == 0) k = atomicAdd(&s_run, 1);
-      u.first = __shfl_sync(0xffffffffu, k, 0) * 32 * kAhead + lane;
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int i = u.first + 32 * j;
-        if (i < vecs) u.v[j] = *(reinterpret_cast<const uint4*>(x + head) + i);
-      }
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int i = u.first + 32 * j, c = head + i * kVec, w = c >> 5;
-        u.lo[j] = u.hi[j] = 0xffffffffu;
-        if (!mask || i >= vecs) continue;
-        u.lo[j] = __ldg(mask + w);
-        if ((c & 31) + kVec > 32 && (w + 1) * 32 < p.V) u.hi[j] = __ldg(mask + w + 1);
-      }
-    };
+  } else if (streams) {
     const auto put = [&](const Run& u) {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -269,8 +290,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
         if (!(in_place && ok == kFull)) *(reinterpret_cast<uint4*>(out + head) + i) = masked<T>(u.v[j], ok);
       }
     };
-    Run a, b;
-    take(a);
+    Run b;
     while (__any_sync(0xffffffffu, a.first < vecs)) {
       take(b);
       put(a);
@@ -329,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
     }
     if (w0 + kWindow >= s_total) break;
     __syncthreads();
-    fill(h, w0 + kWindow, tid, kThreads, sync);
+    fill(h, w0 + kWindow, tid, kThreads, nullptr, sync);
     __syncthreads();
   }
 }
