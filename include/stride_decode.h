@@ -246,7 +246,7 @@ typedef struct stride_evict_params {
  * mass (ties: the lower slot; a NaN is below every number).  Slot number i of those,
  * counted from 0 in rising order of slots, goes to slot i of sequence b in `to`, and
  *   kept[b, h, i] = its slot in `from`,  mass_to[b, h, i] = its mass,  new_len[b] = m.
- * kept: int32 [n_seqs, heads, most] and required; mass_to: stride_slot_mass of at least
+ * new_len is another array than from->ctx_len.  kept: int32 [n_seqs, heads, most] and required; mass_to: stride_slot_mass of at least
  * `most` slots, nullable, not over mass.  What lies past m in kept, mass_to and the pages stays as
  * it is, and `from` is read only: pages that several sequences share (the prefix
  * that restarts reuse) stay whole.  So no page of `to` may be one that the call reads;

@@ -302,7 +302,7 @@ int stride_kv_evict(const stride_paged_cache* from, const stride_slot_mass* mass
                     int32_t* dev_status, void* stream) {
   const size_t es = elem_bytes(dtype);
   if (es == 0) return STRIDE_ERR_UNSUPPORTED_DTYPE;
-  if (D < 1 || D > STRIDE_MAX_HEAD_DIM || !from || !to || !how || !new_len || !kept) return STRIDE_ERR_INVALID_ARG;
+  if (D < 1 || D > STRIDE_MAX_HEAD_DIM || !from || !to || !how || !new_len || !kept || new_len == from->ctx_len) return STRIDE_ERR_INVALID_ARG;
   stride_paged_cache f = *from, t = *to;
   f.tok_off = f.ctx_len;  // (not used)
   t.tok_off = t.ctx_len = f.ctx_len;

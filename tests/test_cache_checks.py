@@ -47,7 +47,7 @@ def test_attention_mass(env, bad, code):  # noqa: F811
 
 
 @pytest.mark.parametrize("bad", [
-    dict(dtype=3), dict(D=0), dict(D=1025), dict(sink=-1), dict(recent=-1), dict(most=0), dict(new_len=None), dict(kept=None),
+    dict(dtype=3), dict(D=0), dict(D=1025), dict(sink=-1), dict(recent=-1), dict(most=0), dict(new_len=None), dict(new_len=DUMMY), dict(kept=None),
     dict(k=None), dict(v=None), dict(n_pages=0), dict(block_table=None), dict(ctx_len=None), dict(n_seqs=0), dict(to_heads=3),
     dict(to_seqs=2), dict(to_k=DUMMY + 1), dict(mass_data=None), dict(to_slots=15), dict(to_mass=DUMMY)], ids=str)
 def test_evict(env, bad):  # noqa: F811
@@ -60,7 +60,7 @@ def test_evict(env, bad):  # noqa: F811
     how = decode._EvictParams(*[d[n] for n, _ in decode._EvictParams._fields_])
     m, m2 = mass(decode, data=bad.get("mass_data", DUMMY)), mass(decode, data=bad.get("to_mass", DUMMY * 2), slots=bad.get("to_slots", 16))
     assert L.stride_kv_evict(ctypes.byref(f), ctypes.byref(m), ctypes.byref(t), bad.get("dtype", 0), bad.get("D", 64),
-                             ctypes.byref(how), bad.get("new_len", DUMMY), bad.get("kept", DUMMY), ctypes.byref(m2), None,
+                             ctypes.byref(how), bad.get("new_len", 3 * DUMMY), bad.get("kept", DUMMY), ctypes.byref(m2), None,
                              None) == (2 if "dtype" in bad else 1)
 
 
