@@ -21,7 +21,6 @@ namespace cg = cooperative_groups;
 namespace stride {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
 // Copies of the first digit's counts, by lane: nearly all masses have one of a few exponents, and lanes that count alike wait for
 // one another.
@@ -54,9 +53,10 @@ __device__ __forceinline__ Plan plan_of(const EvictParams& p, int b) {
   return r;
 }
 
-// Blocks: unit * cluster + rank.  kHeld: masses of a thread that stay in registers.
-template <int kHeld>
-__global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) select_kernel(const __grid_constant__ EvictParams p) {
+// Blocks: unit * cluster + rank.  kHeld: masses of a thread that stay in registers; kBlocks: CTAs on an SM.
+template <int kThreads, int kHeld, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks) select_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kWarps = kThreads / 32;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   __shared__ __align__(16) uint32_t s_first[256 * kCopies];  // the first digit's counts, a digit's copies side by side
@@ -296,13 +296,16 @@ cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, 
   const int units = p.from.n_seqs * p.from.n_heads;
   const int64_t slots = std::min<int64_t>(p.mass.slots, p.from.table_stride * (int64_t)p.from.page_size);
   int C = 1;
-  while (C < kMaxCluster && (int64_t)units * C * 2 <= sms && slots > (int64_t)C * kThreads * 2) C *= 2;
-  const int64_t held = (slots + C * kThreads - 1) / (C * kThreads);  // masses of a thread at most
-  cudaError_t e = cudaFuncSetAttribute(held <= 8 ? select_kernel<8> : select_kernel<16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  while (C < kMaxCluster && (int64_t)units * C * 2 <= sms && slots > (int64_t)C * 1024) C *= 2;
+  // (256 sequences of up to 4,096 slots, us: 256 threads of 16 masses each 344, 512 of 8 352; a cluster's, of up to 131,072 slots:
+  // 512 threads 45, 256 77)
+  const bool few = C == 1 && slots <= 4096;
+  const auto kern = few ? select_kernel<256, 16, 5> : select_kernel<512, 16, 2>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(units * C);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(few ? 256 : 512);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -312,8 +315,7 @@ cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, 
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  // (sequences of up to 4,096 slots a CTA: half the registers, half as many CTAs again)
-  e = cudaLaunchKernelEx(&cfg, held <= 8 ? select_kernel<8> : select_kernel<16>, p);
+  e = cudaLaunchKernelEx(&cfg, kern, p);
   if (e != cudaSuccess) return e;
   const int64_t most = std::min<int64_t>(std::min<int64_t>(p.how.most, slots), p.to.table_stride * (int64_t)p.to.page_size);
   const int64_t parts = std::min<int64_t>((most + kRows - 1) / kRows, ((int64_t)sms * 64 + units - 1) / units);
