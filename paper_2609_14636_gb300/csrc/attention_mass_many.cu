@@ -486,6 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t my = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's lanes of tensor memory
     const uint32_t my_scores = my + L::kScores + (2 * team + part) * kPart;
     const float2 scale2 = make_float2(a.scale * kLog2e, a.scale * kLog2e);
+    const int part_token = part * kPart / group;  // of a whole part's first column, past the block's
     Place k, q;
     // What is at hand of a step.
     struct Now {
@@ -573,8 +574,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 sum[1] = __fadd2_rn(sum[1], make_float2(ex2(x1.x), ex2(x1.y)));
               }
             };
-            const uint2 counts = *reinterpret_cast<const uint2*>(&s_counts[q.st][c0 / 32]);
-            if (kWide && whole && c1 - c0 == kPart && (counts.x & counts.y) == 0xffffffffu) {  // all columns count for all slots
+            // all columns count for all of the warp's slots (in a chain: those of tokens past the last of them)
+            bool all = kWide && c1 - c0 == kPart && (s_counts[q.st][c0 / 32] & s_counts[q.st][c0 / 32 + 1]) == 0xffffffffu;
+            if (all && !whole) all = __all_sync(0xffffffffu, back < 0 || (chain && back <= token0 + part_token));
+            if (all) {
               uint32_t r0[32], r1[32];
               tmem_load32(r0, my_scores);
               tmem_load32(r1, my_scores + 32);
