@@ -35,19 +35,22 @@ constexpr int kWarps = 2 * kTeamWarps + 4, kThreads = kWarps * 32;
 constexpr int kMaxStages = 12;
 constexpr int kTileCost = 4;       // what a tile costs at least, in blocks
 
-template <int D>
+// kWide: a team's products take three places for their scores in turn, so that two are on their way while one is worked on, and its
+// keys have one; else each half of the columns has a place and the keys two, as they count.
+template <int D, bool kWide>
 struct Plan {
   static constexpr int kHalves = D / 64;  // 128-byte column groups of a row
   static constexpr int kStage = kHalves * kSlots * 128;  // bytes: a tile of keys, a block of rows
   static constexpr int kStages = D == 128 ? 6 : 12;
   static constexpr size_t kSmem = (size_t)kStages * kStage + 1024;  // (the base rounded up to 1,024)
-  // columns of tensor memory: keys of two steps' two tiles, scores of two tiles
-  static constexpr int kKeys = D / 2, kScores = 4 * kKeys, kColumns = 512;
-  static_assert(kScores + 2 * kCols <= kColumns, "tensor memory");
+  static constexpr int kKeyPlaces = kWide ? 1 : 2, kScorePlaces = kWide ? 3 : 2;
+  // columns of tensor memory: keys of two tiles, scores of two tiles
+  static constexpr int kKeys = D / 2, kScores = 2 * kKeyPlaces * kKeys, kColumns = 512;
+  static_assert(kScores + 2 * kScorePlaces * kPart <= kColumns, "tensor memory");
 };
 
 struct Barriers {
-  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][2], taken[2][2], sums[2], joined[2], landed, drained[2];
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][3], taken[2][3], sums[2], joined[2], landed, drained[2];
 };
 
 // A place in a ring, and the parity of its barriers' phase.
@@ -146,7 +149,7 @@ template <typename T, int D, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1)
     mass_many_kernel(const __grid_constant__ MassParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap q_map,
                      const int box, const int page_shift, const int tokens, const int k_stages, const bool both) {
-  using L = Plan<D>;
+  using L = Plan<D, kWide>;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   extern __shared__ unsigned char dyn[];
@@ -177,8 +180,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.keys[0][i], kTeamWarps);
       mbar_init(&bars.keys[1][i], kTeamWarps);
-      for (int j = 0; j < 2; ++j) {
-        mbar_init(&bars.read[i][j], 1);
+      for (int j = 0; j < 2; ++j) mbar_init(&bars.read[i][j], 1);
+      for (int j = 0; j < 3; ++j) {
         mbar_init(&bars.scores[i][j], 2);
         mbar_init(&bars.taken[i][j], kTeamWarps / 2);
       }
@@ -428,15 +431,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int team = warp - (kWarps - 2);
       const uint32_t q0 = matrix(q_ring, 16);
       Place q;
-      uint32_t keys_parity[2] = {0, 0}, taken_parity[2] = {1, 1};
+      uint32_t keys_parity = 0;  // bits: places of keys
+      Place score;               // of the next product (kWide)
+      uint32_t halves = 0;       // bits: parity of each half's place (else)
       int buffer = 0;
       bool fresh = true;
       while (at.pos < end && ok) {
         const int by = at.step(end);
         const bool many = at.u.blocks > 1, run_ends = at.run_ends(by, end), mine = team < by;
         if (mine) {
-          ok = wait(&bars.keys[buffer][team], keys_parity[buffer]);
-          keys_parity[buffer] ^= 1;
+          ok = wait(&bars.keys[buffer][team], keys_parity >> buffer & 1);
+          keys_parity ^= 1u << buffer;
         }
         for (int blk = at.first_block(chain, tokens); blk < at.u.blocks && ok; ++blk) {
           if (many || fresh) ok = wait(&bars.q_full[q.st], q.parity);
@@ -448,13 +453,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int part = 0; part < 2; ++part) {
               const int c = part * wide;
               if (c >= cols || !ok) break;
-              ok = wait(&bars.taken[team][part], taken_parity[part]);
-              taken_parity[part] ^= 1;
+              const int place = kWide ? score.st : part;
+              ok = wait(&bars.taken[team][place], (kWide ? score.parity : halves >> part & 1) ^ 1);
               if (!ok) break;
               fence_after();
               const uint32_t idesc = product<T>((min(cols - c, wide) + 31) & ~31, false);
               const uint32_t b = q0 + q.st * (L::kStage >> 4) + (c * 128 >> 4), k = tmem + (2 * buffer + team) * L::kKeys;
-              const uint32_t d = tmem + L::kScores + (2 * team + part) * kPart;
+              const uint32_t d = tmem + L::kScores + (team * L::kScorePlaces + place) * kPart;
 #pragma unroll
               for (int x = 0; x < D / 16; ++x) mma_ts(d, k + x * 8, b + (x / 4) * (kCols * 128 >> 4) + (x % 4) * 2, idesc, x > 0);
               // (the stage and the keys first: whoever has seen the last scores knows that nothing more arrives)
@@ -462,14 +467,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (many || run_ends) commit(&bars.q_empty[q.st]);
                 if (blk + 1 >= at.u.blocks) commit(&bars.read[buffer][team]);
               }
-              commit(&bars.scores[team][part]);
-              mbar_arrive(&bars.scores[team][part]);  // (what this thread knows, that -lse are there, goes with them)
+              commit(&bars.scores[team][place]);
+              mbar_arrive(&bars.scores[team][place]);  // (what this thread knows, that -lse are there, goes with them)
+              score.on(L::kScorePlaces);
+              halves ^= 1u << part;
             }
           }
           if (many || run_ends) q.on(q_stages);
         }
         fresh = run_ends;
-        buffer ^= 1;
+        buffer ^= L::kKeyPlaces - 1;
         at.on(p, tokens, by);
       }
       if (!ok) {
@@ -484,7 +491,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---- weights ----
     const int team = (warp >> 2) & 1, part = warp >> 3, row = (warp & 3) * 32 + lane;  // tile of the step, half of the columns, slot of the tile
     const uint32_t my = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's lanes of tensor memory
-    const uint32_t my_scores = my + L::kScores + (2 * team + part) * kPart;
     const float2 scale2 = make_float2(a.scale * kLog2e, a.scale * kLog2e);
     const int part_token = part * kPart / group;  // of a whole part's first column, past the block's
     Place k, q;
@@ -540,14 +546,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       return x;
     };
-    uint32_t scores_parity = 0, sums_parity = part;  // (the second half's: the first half's have been read)
+    uint32_t sums_parity = part;  // (the second half's: the first half's have been read)
+    Place score;                  // of the team's next product (kWide)
+    uint32_t own_parity = 0;      // of this half's place (else)
     int buffer = 0;
     bool fresh = true;
     if (at.pos < end) {
       Now now = convert(0), next = now;
       while (ok) {
         const bool ends = now.flags & 8;
-        if (!ends) next = convert(buffer ^ 1);
+        if (!kWide && !ends) next = convert(buffer ^ 1);
         if (!ok) break;
         const bool many = now.blocks > 1, run_ends = now.flags & 4, mine = team < (now.flags & 3);
         const int back = now.back, slot_back = back - row;  // (of the tile's first slot)
@@ -558,11 +566,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int blk = now.blk0; blk < now.blocks && ok; ++blk) {
           const int token0 = blk * tokens, cols = min(tokens, now.n - token0) * group;
           const int wide = part_of(cols), c0 = part * wide, c1 = min(cols, c0 + wide);  // this warp's columns: up to 32 or 64
-          if ((many || fresh) && !(mine && c0 < c1)) ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
+          // (A place's barrier is never a lap ahead of a half.  Where a half has no columns, in a unit's last block, the keys of the
+          // team's next step wait for all products of this one.)
+          Place at_score = score;  // of this half's product
+          if (part == 1) at_score.on(L::kScorePlaces);
+          const int place = kWide ? at_score.st : part;
           if (mine && c0 < c1) {
-            ok = ok && __all_sync(0xffffffffu, wait(&bars.scores[team][part], scores_parity));
-            scores_parity ^= 1;
-            if (!ok) break;
+            ok = ok && __all_sync(0xffffffffu, wait(&bars.scores[team][place], kWide ? at_score.parity : own_parity));
+            own_parity ^= 1;
+          } else if (many || fresh) {
+            ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
+          }
+          if (mine) {
+            score.on(L::kScorePlaces);
+            if (cols > wide) score.on(L::kScorePlaces);
+          }
+          if (!ok) break;
+          if (mine && c0 < c1) {
+            uint64_t* const taken = &bars.taken[team][place];
+            const uint32_t my_scores = my + L::kScores + (team * L::kScorePlaces + place) * kPart;
             fence_after();
             const auto add = [&](const uint32_t (&r)[32], const float4* lse) {
 #pragma unroll
@@ -584,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               tmem_wait_load();
               fence_before();
               __syncwarp();
-              if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+              if (lane == 0) mbar_arrive(taken);
               add(r0, reinterpret_cast<const float4*>(&s_lse[q.st][c0]));
               add(r1, reinterpret_cast<const float4*>(&s_lse[q.st][c0 + 32]));
             } else
@@ -619,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (last) {
                   fence_before();
                   __syncwarp();
-                  if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+                  if (lane == 0) mbar_arrive(taken);
                 }
                 continue;
               }
@@ -630,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (last) {
                   fence_before();
                   __syncwarp();
-                  if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+                  if (lane == 0) mbar_arrive(taken);
                 }
                 add(r, lse);
                 continue;
@@ -646,7 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (last && j + 8 >= n) {
                   fence_before();
                   __syncwarp();
-                  if (lane == 0) mbar_arrive(&bars.taken[team][part]);
+                  if (lane == 0) mbar_arrive(taken);
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -662,6 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             q.on(q_stages);
           }
         }
+        if (kWide && !ends) next = convert(0);
         if (!ok) break;
         fresh = run_ends;
         if (mine) {  // the columns' halves meet
@@ -684,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ends) break;
         now = next;
-        buffer ^= 1;
+        buffer ^= L::kKeyPlaces - 1;
       }
     }
     if (!ok && lane == 0) {
@@ -708,7 +731,7 @@ int slots_of_a_box(int page_size) {
 
 template <typename T, int D, bool kWide>
 cudaError_t run(const MassParams& p, bool bf16, int sms, cudaStream_t stream) {
-  using L = Plan<D>;
+  using L = Plan<D, kWide>;
   const auto kern = mass_many_kernel<T, D, kWide>;
   const PagedCache& c = p.a.cache;
   const int box = slots_of_a_box(c.page_size), group = p.a.Hq / c.n_heads, tokens = kCols / group;
