@@ -329,8 +329,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       k.on(k_stages);
     }
-    if (!ok) {  // (never seen.  No copy may outlive the CTA: those on their way end, or take their time)
-      if (lane == 0) s_abort = 1;
+    if (!ok && lane == 0) s_abort = 1;
+    {  // (no copy may outlive the CTA, whatever the others did: those on their way end, or take their time)
       volatile int32_t go_on = 0;
       for (int i = t < k_stages ? 0 : t - k_stages; i < t; ++i) mbar_wait_warp(&bars.k_full[i % k_stages], (i / k_stages) & 1, kWaitTimeoutNs, &go_on);
     }
@@ -385,7 +385,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = __all_sync(0xffffffffu, wait(&bars.q_empty[q.st], q.parity ^ 1));
         if (!ok) break;
       }
-      // Rows past the block's last, up to a whole run of 32 columns, are zeros, and their columns' -lse is -inf: weights of 0.
+      // Rows past the block's last, up to a whole run of 32 columns, are the block's first again (zeros would make NaN of a key's
+      // infinities), and their columns' -lse is -inf: weights of 0.
       uint64_t* bar = &bars.q_full[q.st];
       const bool ragged = cols % 32 != 0;
       const uint32_t to = q_ring + q.st * L::kStage;
@@ -406,11 +407,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ragged) {
         ok = __all_sync(0xffffffffu, wait(&bars.landed, landed_parity));
         landed_parity ^= 1;
-        if (!ok) break;
-        for (int i = cols * 8 + lane; i < ((cols + 31) & ~31) * 8; i += 32)
+        if (!ok) {
+          ++t;
+          break;
+        }
+        for (int i = cols * 8 + lane; i < ((cols + 31) & ~31) * 8; i += 32) {
+          const int chunk = (i & 7) ^ (i >> 3 & 7);  // (of the first row, where nothing is swizzled)
 #pragma unroll
-          for (int half = 0; half < L::kHalves; ++half)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + half * kCols * 128 + i * 16), "r"(0) : "memory");
+          for (int half = 0; half < L::kHalves; ++half) {
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "r"(to + half * kCols * 128 + chunk * 16)
+                         : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + half * kCols * 128 + i * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                         : "memory");
+          }
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(bar);
@@ -420,8 +433,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       q.on(q_stages);
       ++t;
     }
-    if (!ok) {
-      if (lane == 0) s_abort = 1;
+    if (!ok && lane == 0) s_abort = 1;
+    {
       volatile int32_t go_on = 0;
       for (int i = t < q_stages ? 0 : t - q_stages; i < t; ++i) mbar_wait_warp(&bars.q_full[i % q_stages], (i / q_stages) & 1, kWaitTimeoutNs, &go_on);
     }
@@ -479,12 +492,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         buffer ^= L::kKeyPlaces - 1;
         at.on(p, tokens, by);
       }
-      if (!ok) {
-        s_abort = 1;
-        volatile int32_t go_on = 0;
-        commit(&bars.drained[team]);
-        mbar_wait(&bars.drained[team], 0, kWaitTimeoutNs, &go_on);
-      }
+      if (!ok) s_abort = 1;
+      volatile int32_t go_on = 0;  // (nor a product tensor memory)
+      commit(&bars.drained[team]);
+      mbar_wait(&bars.drained[team], 0, kWaitTimeoutNs, &go_on);
     }
     __syncwarp();
   } else {

@@ -188,6 +188,32 @@ def test_rows_that_see_nothing(env):
         assert (x["mass"][0, :, 19] == 0).all() and torch.isfinite(x["mass"]).all()
 
 
+def test_infinite_keys_that_rows_see(env):
+    """Weights of 0 and nothing else, where a block's rows do not fill the products' columns."""
+    torch, stride, dev = env
+    for case in (([(37, 1)], 3, 1, 64, 16, "rows", False, 1.0, "bf16"), ([(140, 9), (300, 11)], 5, 1, 128, 16, "rows", False, 1.0, "bf16"),
+                 ([(300, 37)], 6, 2, 64, 16, "rows", False, 1.0, "f16"), ([(130, 13), (20, 7)], 4, 2, 128, 16, "rows", True, 1.0, "bf16")):
+        x = mass_inputs(torch, case)
+        x["q"].copy_(x["q"].abs() + 0.1)
+        lost = (3, 19, case[0][0][0] - 1)
+        for j in lost:
+            x["k"][int(x["table"][0, j // 16]), j % 16, :, 5] = float("-inf")
+        before = x["mass"].double().cpu().numpy()
+        call_mass(stride, torch, x, case)
+        after = x["mass"].double().cpu().numpy()
+        for j in lost:
+            assert np.array_equal(after[0, :, j], before[0, :, j]), (case, j)
+        x["k"].nan_to_num_(neginf=0.0)
+        got = after.copy()
+        got[0][:, list(lost)] = 0
+        again = x["mass"]
+        again.copy_(torch.from_numpy(before))
+        call_mass(stride, torch, x, case)
+        rest = again.double().cpu().numpy()
+        rest[0][:, list(lost)] = 0
+        assert np.array_equal(rest, got), case  # (other slots: the same bits)
+
+
 def test_mass_layouts(env):
     """Masses of other strides; a slot without a page, lengths that do not fit, trees of too many tokens."""
     torch, stride, dev = env
