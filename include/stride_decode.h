@@ -189,7 +189,7 @@ STRIDE_API int stride_tree_attention(const stride_head_rows* q, const stride_hea
                                      void* stream);
 
 /* Attention weight of cached slots (host struct): float [n_seqs, heads, slots]
- * of unit stride along the slots, other strides in elements.  Slot s is the
+ * of unit stride along the slots, other strides in elements; where it is written no two rows overlap.  Slot s is the
  * sequence's s-th, not a place in a page: sequences that share pages of a prefix
  * have weights of their own. */
 typedef struct stride_slot_mass {
@@ -209,8 +209,8 @@ typedef struct stride_slot_mass {
  * Slots past those, and sequences without new tokens, stay as they are.  decay >= 0; with 0
  * mass is not read (it may hold anything).  A row whose lse is -inf sees nothing
  * and adds nothing; keys that a row does not see may hold anything and change nothing
- * in its weights.  Sums are held in 32 bits in an order that does not depend on
- * the other sequences of the call: the same call gives the same bits.
+ * in its weights.  Sums are held in 32 bits, in an order that follows from the
+ * sequence and from the mean of new tokens over the call's sequences alone: the same call gives the same bits.
  *
  * A slot without a page: NaN and STRIDE_DEV_BAD_LAYOUT.  Sequences of a length that
  * the block table or mass->slots does not hold, or, under a tree mask, of more than
@@ -246,7 +246,7 @@ typedef struct stride_evict_params {
  * mass (ties: the lower slot; a NaN is below every number).  Slot number i of those,
  * counted from 0 in rising order of slots, goes to slot i of sequence b in `to`, and
  *   kept[b, h, i] = its slot in `from`,  mass_to[b, h, i] = its mass,  new_len[b] = m.
- * new_len is another array than from->ctx_len.  kept: int32 [n_seqs, heads, most] and required; mass_to: stride_slot_mass of at least
+ * new_len is another array than from->ctx_len and budget.  kept: int32 [n_seqs, heads, most] and required; mass_to: stride_slot_mass of at least
  * `most` slots, nullable, not over mass.  What lies past m in kept, mass_to and the pages stays as
  * it is, and `from` is read only: pages that several sequences share (the prefix
  * that restarts reuse) stay whole.  So no page of `to` may be one that the call reads;

@@ -5,6 +5,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "decode_internal.h"
 
 namespace {
@@ -55,6 +57,19 @@ int check_cache(const stride_paged_cache* c, size_t e) {
 
 int check_mass(const stride_slot_mass* m) {
   return !m || !m->data || !multiple(m->data, sizeof(float)) || m->slots < 1 ? STRIDE_ERR_INVALID_ARG : STRIDE_OK;
+}
+
+// Sequences' and heads' slots, where they are written, are apart.
+bool apart(const stride_slot_mass& m, const stride_paged_cache& c) {
+  const auto size = [](int64_t x) { return x < 0 ? -x : x; };
+  int64_t a = size(m.seq_stride), b = size(m.head_stride), n = c.n_heads;  // a: the larger of two
+  if (c.n_seqs <= 1) return n <= 1 || b >= m.slots;
+  if (n <= 1) return a >= m.slots;
+  if (a < b) {
+    std::swap(a, b);
+    n = c.n_seqs;
+  }
+  return b >= m.slots && a >= m.slots && (a - m.slots) / b >= n - 1;
 }
 
 SlotMass view(const stride_slot_mass& m) { return {m.data, m.seq_stride, m.head_stride, m.slots}; }
@@ -271,6 +286,7 @@ int stride_attention_mass(const stride_head_rows* q, const float* lse, int32_t d
   int rc = check_cache(&keys, elem_bytes(dtype));
   if (rc != STRIDE_OK) return rc;
   if ((rc = check_mass(mass)) != STRIDE_OK) return rc;
+  if (!apart(*mass, keys)) return STRIDE_ERR_INVALID_ARG;
   if (!Q.valid(n_tokens, elem_bytes(dtype)) || Q.r.n_heads < 1 || Q.r.n_heads % keys.n_heads != 0) return STRIDE_ERR_INVALID_ARG;
   if (!Q.whole(n_tokens, 8, 2) || !cache_whole(keys, 8, 2)) return STRIDE_ERR_INVALID_ARG;
   if (n_tokens * (Q.r.n_heads / keys.n_heads) > (1 << 30)) return STRIDE_ERR_INVALID_ARG;
@@ -302,7 +318,7 @@ int stride_kv_evict(const stride_paged_cache* from, const stride_slot_mass* mass
                     int32_t* dev_status, void* stream) {
   const size_t es = elem_bytes(dtype);
   if (es == 0) return STRIDE_ERR_UNSUPPORTED_DTYPE;
-  if (D < 1 || D > STRIDE_MAX_HEAD_DIM || !from || !to || !how || !new_len || !kept || new_len == from->ctx_len) return STRIDE_ERR_INVALID_ARG;
+  if (D < 1 || D > STRIDE_MAX_HEAD_DIM || !from || !to || !how || !new_len || !kept || new_len == from->ctx_len || new_len == how->budget) return STRIDE_ERR_INVALID_ARG;
   stride_paged_cache f = *from, t = *to;
   f.tok_off = f.ctx_len;  // (not used)
   t.tok_off = t.ctx_len = f.ctx_len;
@@ -311,7 +327,7 @@ int stride_kv_evict(const stride_paged_cache* from, const stride_slot_mass* mass
   if ((rc = check_cache(&t, es)) != STRIDE_OK) return rc;
   if ((rc = check_mass(mass)) != STRIDE_OK || (mass_to && (rc = check_mass(mass_to)) != STRIDE_OK)) return rc;
   if (f.n_heads != t.n_heads || f.n_seqs != t.n_seqs || how->sink < 0 || how->recent < 0 || how->most < 1) return STRIDE_ERR_INVALID_ARG;
-  if (mass_to && (mass_to->slots < how->most || mass_to->data == mass->data)) return STRIDE_ERR_INVALID_ARG;
+  if (mass_to && (mass_to->slots < how->most || mass_to->data == mass->data || !apart(*mass_to, f))) return STRIDE_ERR_INVALID_ARG;
   if ((int64_t)f.n_seqs * f.n_heads > INT32_MAX / 16) return STRIDE_ERR_INVALID_ARG;
   if ((rc = check_device()) != STRIDE_OK) return rc;
   cudaError_t e = cudaSuccess;

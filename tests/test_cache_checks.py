@@ -35,19 +35,21 @@ def test_names_match_the_header(env):  # noqa: F811
     (dict(rows=DUMMY + 2), 1), (dict(token=4 * 64 + 4), 1), (dict(head=68), 1), (dict(k=None), 1), (dict(k=DUMMY + 8), 1),
     (dict(row_stride=129), 1), (dict(page_stride=4), 1), (dict(head_stride=4), 1), (dict(tok_off=None), 1), (dict(ctx_len=None), 1),
     (dict(lse=None), 1), (dict(lse=DUMMY + 2), 1), (dict(mass=None), 1), (dict(mass_data=None), 1), (dict(mass_data=DUMMY + 2), 1),
-    (dict(slots=0), 1), (dict(N=-1), 1), (dict(N=2 ** 29 + 1), 1), (dict(N=0), 0), (dict(N=0, lse=None), 0), (dict(N=0, v=None), 0)])
+    (dict(slots=0), 1), (dict(seq=127, n_seqs=2), 1), (dict(mass_head=63), 1), (dict(mass_head=0), 1), (dict(mass_head=-64, n_seqs=2, N=0), 0),
+    (dict(seq=64, mass_head=128, n_seqs=2, N=0), 0), (dict(seq=64, mass_head=127, n_seqs=2), 1), (dict(N=-1), 1), (dict(N=2 ** 29 + 1), 1), (dict(N=0), 0), (dict(N=0, lse=None), 0), (dict(N=0, v=None), 0)])
 def test_attention_mass(env, bad, code):  # noqa: F811
     stride, decode, L = env
     q = rows(decode, heads=bad.get("heads", 4), data=bad.get("rows", DUMMY), token=bad.get("token"), head=bad.get("head"))
     c = cache(decode, **of(decode._PagedCache._fields_, bad))
-    m = mass(decode, data=bad.get("mass_data", DUMMY), slots=bad.get("slots", 64))
+    m = mass(decode, data=bad.get("mass_data", DUMMY), slots=bad.get("slots", 64), seq_stride=bad.get("seq", 128),
+             head_stride=bad.get("mass_head", 64))
     assert L.stride_attention_mass(ctypes.byref(q), bad.get("lse", DUMMY), bad.get("dtype", 0), bad.get("N", 5), bad.get("D", 64),
                                    bad.get("scale", 0.1), None, ctypes.byref(c), bad.get("decay", 1.0),
                                    ctypes.byref(m) if "mass" not in bad else None, None, None) == code
 
 
 @pytest.mark.parametrize("bad", [
-    dict(dtype=3), dict(D=0), dict(D=1025), dict(sink=-1), dict(recent=-1), dict(most=0), dict(new_len=None), dict(new_len=DUMMY), dict(kept=None),
+    dict(dtype=3), dict(D=0), dict(D=1025), dict(sink=-1), dict(recent=-1), dict(most=0), dict(new_len=None), dict(new_len=DUMMY), dict(budget=3 * DUMMY), dict(to_slots=65), dict(kept=None),
     dict(k=None), dict(v=None), dict(n_pages=0), dict(block_table=None), dict(ctx_len=None), dict(n_seqs=0), dict(to_heads=3),
     dict(to_seqs=2), dict(to_k=DUMMY + 1), dict(mass_data=None), dict(to_slots=15), dict(to_mass=DUMMY)], ids=str)
 def test_evict(env, bad):  # noqa: F811
