@@ -3,19 +3,28 @@
 //
 // The product of 128 slots by up to 128 rows on the tensor cores, turned so that a slot is
 // a lane of tensor memory: a slot's sum over the rows is then a thread's own, and
-// nothing is joined but two halves of the columns.  One CTA on an SM takes a share of
+// nothing is joined but two halves of the columns at most.  One CTA on an SM takes a share of
 // the tiles of 128 slots, two at a time; its warps:
-//   16   looks up a tile's pages and starts the tensor copies of its keys (boxes of
-//        slots by 128 bytes, swizzled), some tiles ahead;
+//   16   looks up tiles' pages, a run of tiles ahead, and starts the tensor copies of the keys
+//        (boxes of slots by 128 bytes, swizzled);
 //   17   starts the copies of the rows, a block of whole tokens at a time, and leaves
 //        what a column needs beside them: -lse, and which columns count;
-//   18, 19  one thread each issues a tile's products, of half of a block's columns;
+//   18, 19  one thread each issues a tile's products, of up to 64 of a block's columns each;
 //   0-15 keys from shared memory into tensor memory, where they are the first operand
 //        of all the unit's blocks (from shared memory they would be read again for each,
-//        which is more of its bandwidth than there is); then scores from tensor
-//        memory, weights, sums: four warps for each tile and half of the columns, whose
-//        waits for their next product are filled by the three others of a scheduler.
+//        which is more of its bandwidth than there is), and scores from tensor
+//        memory, weights, sums.
+// Where units have many rows (kWide) the exponentials count: each of the sixteen does both, four
+// for each tile and half of the columns, whose waits for their next product are filled
+// by the three others of a scheduler.  Where they have up to 64, a tile costs its
+// way through the CTA: eight bring keys, two steps ahead, eight add up (all sixteen doing
+// both, one after the other: 32 trees of 13 tokens 87 us, 79).
 // The rows of a unit that fit in one block are copied once for all its tiles.
+//
+// Measured, us (floor: of bytes at 6,683 GB/s, of products at 1,981 TFLOP/s): 32 trees of 13 tokens, 32 / 8 heads of 128, over up to
+// 8,000 slots 79 (55; 4.6 TB/s: the weights' chain of waits, 3,600 clocks for two tiles); 4 chains of 511 over up to 6,000 90
+// (35, the exponentials 30 at 32 a clock and SM; 0.78 PFLOP/s: without the exponentials 70, product, scores and sums one after the
+// other).  The simple kernel of mma.sync took 313 and 1,126.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -33,10 +42,11 @@ constexpr int kPart = 64;          // of them, those of a product at most
 constexpr int kTeamWarps = 8;      // of a tile's
 constexpr int kWarps = 2 * kTeamWarps + 4, kThreads = kWarps * 32;
 constexpr int kMaxStages = 12;
+constexpr int kInfos = 4;          // steps that weights may be behind the keys
 constexpr int kTileCost = 4;       // what a tile costs at least, in blocks
 
 // kWide: a team's products take three places for their scores in turn, so that two are on their way while one is worked on, and its
-// keys have one; else each half of the columns has a place and the keys two, as they count.
+// keys have one; else two places each, as the keys count.
 template <int D, bool kWide>
 struct Plan {
   static constexpr int kHalves = D / 64;  // 128-byte column groups of a row
@@ -50,7 +60,7 @@ struct Plan {
 };
 
 struct Barriers {
-  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][3], taken[2][3], sums[2], joined[2], landed, drained[2];
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], q_full[kMaxStages], q_empty[kMaxStages], keys[2][2], read[2][2], scores[2][3], taken[2][3], sums[2], joined[2], info_full[kInfos], info_empty[kInfos], landed, drained[2];
 };
 
 // A place in a ring, and the parity of its barriers' phase.
@@ -114,11 +124,17 @@ struct Cursor2 {
 __device__ __forceinline__ int part_of(int cols) { return cols > kPart ? kPart : kPart / 2; }
 
 // A step, as the warps that add up its weights need it.
-struct Step {
+struct __align__(16) Step {
   int64_t mass;   // where its first slot's is
   int32_t back;   // of the first slot: its place among the new tokens
   int32_t n, off, blk0, blocks;
   int32_t flags;  // tiles, 4: the share's last step of the unit, 8: the share's last
+};
+
+// The same, of both tiles, where other warps than those of the weights have its keys.
+struct __align__(16) Info {
+  Step step;
+  uint32_t lost[2];
 };
 
 // Sum over the CTA's threads before this one, and of all.
@@ -159,6 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ Step s_step[kMaxStages];         // of the step that starts with a tile
   __shared__ float s_sum[2][kSlots];
   __shared__ uint32_t s_lost[kMaxStages];                // boxes of a tile that have no page
+  __shared__ Info s_info[kInfos];                        // of a step (not kWide)
   __shared__ int64_t s_scan[kWarps], s_pos;
   __shared__ int32_t s_seq, s_abort;
   __shared__ uint32_t s_tmem;
@@ -173,13 +190,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < kMaxStages; ++i) {
       mbar_init(&bars.k_full[i], 1);
-      mbar_init(&bars.k_empty[i], 2 * kTeamWarps);
+      mbar_init(&bars.k_empty[i], kWide ? 2 * kTeamWarps : kTeamWarps);
       mbar_init(&bars.q_full[i], 2);
-      mbar_init(&bars.q_empty[i], 2 * kTeamWarps + 2);
+      mbar_init(&bars.q_empty[i], (kWide ? 2 * kTeamWarps : kTeamWarps) + 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars.keys[0][i], kTeamWarps);
-      mbar_init(&bars.keys[1][i], kTeamWarps);
+      mbar_init(&bars.keys[0][i], kWide ? kTeamWarps : kTeamWarps / 2);
+      mbar_init(&bars.keys[1][i], kWide ? kTeamWarps : kTeamWarps / 2);
       for (int j = 0; j < 2; ++j) mbar_init(&bars.read[i][j], 1);
       for (int j = 0; j < 3; ++j) {
         mbar_init(&bars.scores[i][j], 2);
@@ -189,6 +206,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars.sums[i], kTeamWarps / 2);
       mbar_init(&bars.joined[i], kTeamWarps / 2);
       mbar_init(&bars.drained[i], 1);
+    }
+    for (int i = 0; i < kInfos; ++i) {
+      mbar_init(&bars.info_full[i], 1);
+      mbar_init(&bars.info_empty[i], kTeamWarps);
     }
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -254,42 +275,49 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int run_tiles = 32 / boxes, my_tile = lane / boxes, bx = lane & (boxes - 1);
     // A run of tiles of a unit and the pages of their boxes, one a lane, looked up a run ahead.
     struct Run {
-      int32_t len, page, row;  // (the page's first row of the box)
-      bool some;               // there is something to read
+      Step step;               // of its first tile, without blk0 and flags
+      int32_t len, left, head;  // tiles; the share's of the unit from here on
+      int32_t page, row;       // (the page's first row of the box)
+      bool some, last;         // there is something to read; the share ends with the unit's
     };
-    Cursor2 ahead = at;
+    int left = 0;  // tiles of the share in the unit here
+    bool last = true;
+    const auto enter = [&] {
+      if (at.pos >= end) return;
+      left = at.u.tiles - at.tile;
+      const int64_t cost = end - at.pos;
+      last = cost <= (int64_t)left * at.u.cost;
+      if (last) left = (int)((cost + at.u.cost - 1) / at.u.cost);
+    };
     const auto look_up = [&](Run& x) {
-      x = {0, 0, 0, false};
-      if (ahead.pos >= end) return;
-      x.len = min(run_tiles, ahead.u.tiles - ahead.tile);
-      const int64_t left = end - ahead.pos;
-      if (left < (int64_t)x.len * ahead.u.cost) x.len = ((int)left + ahead.u.cost - 1) / ahead.u.cost;
-      const int slot = (ahead.tile + my_tile) * kSlots + bx * box;
-      x.some = my_tile < x.len && slot < ahead.u.ctx + ahead.u.n;
+      x.len = min(run_tiles, left);
+      x.some = false;
+      if (left == 0) return;
+      x.left = left;
+      x.last = last;
+      x.head = at.head;
+      x.step = {at.b * p.mass.seq_stride + at.head * p.mass.head_stride + at.tile * kSlots, at.tile * kSlots - at.u.ctx, at.u.n, at.u.off, 0, at.u.blocks, 0};
+      x.page = 0;
+      const int slot = (at.tile + my_tile) * kSlots + bx * box;
+      x.some = my_tile < x.len && slot < at.u.ctx + at.u.n;
       if (x.some) {
         const int e = page_shift >= 0 ? slot >> page_shift : slot / pc.page_size;
         x.row = slot - e * pc.page_size;
-        x.page = __ldg(pc.block_table + (int64_t)ahead.b * pc.table_stride + e);
+        x.page = __ldg(pc.block_table + (int64_t)at.b * pc.table_stride + e);
       }
-      ahead.on(p, tokens, x.len);
+      at.on(p, tokens, x.len);
+      left -= x.len;
+      if (left == 0 && !last) enter();
     };
     Place k;
     int t = 0;
-    const auto copy = [&](const Run& run) {
+    const auto copy = [&](Run& run) {
       const bool real = run.some && run.page >= 0 && run.page < pc.n_pages;
       const unsigned gone = __ballot_sync(0xffffffffu, run.some && !real), who = __ballot_sync(0xffffffffu, real);
-      const int head = at.head, len = run.len;
-      Step step = {at.b * p.mass.seq_stride + head * p.mass.head_stride + at.tile * kSlots, at.tile * kSlots - at.u.ctx, at.u.n, at.u.off, 0, at.u.blocks, 0};
-      for (int i = 0; i < len; ++i) {
-        const int by = at.step(end);
-        step.blk0 = at.first_block(chain, tokens);
-        step.flags = by | (at.run_ends(by, end) ? 4 : 0) | (at.pos + (int64_t)by * at.u.cost >= end ? 8 : 0);
-        if (i + 1 < len) {
-          ++at.tile;
-          at.pos += at.u.cost;
-        } else {
-          at.on(p, tokens, 1);
-        }
+      for (int i = 0; i < run.len; ++i) {
+        const int rest = run.left - i, by = rest > 1 ? 2 : 1;
+        run.step.blk0 = chain && run.step.back > 0 ? run.step.back / tokens : 0;
+        run.step.flags = by | (rest <= by ? 4 : 0) | (rest <= by && run.last ? 8 : 0);
         if (t >= k_stages) {
           ok = __all_sync(0xffffffffu, wait(&bars.k_empty[k.st], k.parity ^ 1));
           if (!ok) return;
@@ -301,25 +329,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           const unsigned mine = (1u << boxes) - 1;
           mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who >> (i * boxes) & mine) * L::kHalves * box * 128));
           s_lost[k.st] = gone >> (i * boxes) & mine;
-          s_step[k.st] = step;
+          s_step[k.st] = run.step;
         }
         __syncwarp();
         if (my_tile == i && real) {
           const uint32_t there = k_ring + k.st * L::kStage + bx * L::kHalves * box * 128;  // (a box's halves side by side)
           if (L::kHalves == 2 && both) {
-            copy_box(there, &k_map, 0, run.row, 0, head, run.page, bar);
+            copy_box(there, &k_map, 0, run.row, 0, run.head, run.page, bar);
           } else {
 #pragma unroll
-            for (int half = 0; half < L::kHalves; ++half) copy_box(there + half * box * 128, &k_map, half * 64, run.row, head, run.page, bar);
+            for (int half = 0; half < L::kHalves; ++half) copy_box(there + half * box * 128, &k_map, half * 64, run.row, run.head, run.page, bar);
           }
         }
         __syncwarp();
-        step.mass += kSlots;
-        step.back += kSlots;
+        run.step.mass += kSlots;
+        run.step.back += kSlots;
         k.on(k_stages);
         ++t;
       }
     };
+    enter();
     Run x0, x1;  // (by name: registers that move wait for their loads)
     look_up(x0);
     while (true) {
@@ -446,8 +475,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t q0 = matrix(q_ring, 16);
       Place q;
       uint32_t keys_parity = 0;  // bits: places of keys
-      Place score;               // of the next product (kWide)
-      uint32_t halves = 0;       // bits: parity of each half's place (else)
+      Place score;               // of the next product
       int buffer = 0;
       bool fresh = true;
       while (at.pos < end && ok) {
@@ -459,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int blk = at.first_block(chain, tokens); blk < at.u.blocks && ok; ++blk) {
           if (many || fresh) ok = wait(&bars.q_full[q.st], q.parity);
-          const int cols = min(tokens, at.u.n - blk * tokens) * group, wide = part_of(cols);
+          const int cols = min(tokens, at.u.n - blk * tokens) * group, wide = kWide ? part_of(cols) : kPart;
           if (!mine) {
             if (ok && (many || run_ends)) mbar_arrive(&bars.q_empty[q.st]);
           } else {
@@ -467,8 +495,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int part = 0; part < 2; ++part) {
               const int c = part * wide;
               if (c >= cols || !ok) break;
-              const int place = kWide ? score.st : part;
-              ok = wait(&bars.taken[team][place], (kWide ? score.parity : halves >> part & 1) ^ 1);
+              const int place = score.st;
+              ok = wait(&bars.taken[team][place], score.parity ^ 1);
               if (!ok) break;
               fence_after();
               const uint32_t idesc = product<T>((min(cols - c, wide) + 31) & ~31, false);
@@ -484,7 +512,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               commit(&bars.scores[team][place]);
               mbar_arrive(&bars.scores[team][place]);  // (what this thread knows, that -lse are there, goes with them)
               score.on(L::kScorePlaces);
-              halves ^= 1u << part;
             }
           }
           if (many || run_ends) q.on(q_stages);
@@ -501,10 +528,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ---- weights ----
-    const int team = (warp >> 2) & 1, part = warp >> 3, row = (warp & 3) * 32 + lane;  // tile of the step, half of the columns, slot of the tile
+    // tile of the step, half of the columns (kWide; else whether the keys' or the weights'), slot of the tile
+    const int team = (warp >> 2) & 1, part = warp >> 3, row = (warp & 3) * 32 + lane;
+    const int box_shift = __ffs(box) - 1;
     const uint32_t my = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's lanes of tensor memory
     const float2 scale2 = make_float2(a.scale * kLog2e, a.scale * kLog2e);
-    const int part_token = part * kPart / group;  // of a whole part's first column, past the block's
     Place k, q;
     // What is at hand of a step.
     struct Now {
@@ -512,40 +540,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       int32_t back, n, off, blk0, blocks, flags;
       bool lost;                  // the slot has no page
     };
-    // The next step, its keys of this team's tile into tensor memory (half of the components), where products have read the ones
-    // before them.
+    const auto now_of = [&](const Step& s) {
+      const Now x = {p.mass.data + s.mass + team * kSlots + row, s.back + team * kSlots + row, s.n, s.off, s.blk0, s.blocks, s.flags, false};
+      return x;
+    };
+    // Half of the components of this thread's slot, from the stage at hand into tensor memory.
+    const auto move = [&](int half, int buffer) {
+      constexpr int kRegs = D / 4;  // D / 2 components
+      uint32_t r[kRegs];
+      const uint32_t from = k_ring + k.st * L::kStage + (((row >> box_shift) * L::kHalves + (D == 128 ? half : 0)) * box + (row & (box - 1))) * 128;
+#pragma unroll
+      for (int c = 0; c < kRegs / 4; ++c) {
+        const int chunk = (D == 128 ? 0 : half * 4) + c;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[4 * c]), "=r"(r[4 * c + 1]), "=r"(r[4 * c + 2]), "=r"(r[4 * c + 3])
+                     : "r"(from + ((chunk ^ (row & 7)) << 4))
+                     : "memory");
+      }
+      tmem_store(my + (2 * buffer + team) * L::kKeys + half * kRegs, r);
+    };
+    // The next step, its keys of this team's tile into tensor memory, where products have read the ones before them.
     // Every warp waits for every tile and lets go of it, in order: a stage's barriers are never a lap ahead of a team that has
     // no tile in a step.
     uint32_t read_parity = 3;  // bits: a buffer (nothing to wait for at first)
-    const auto convert = [&](int buffer) {
+    const auto convert = [&](int buffer, Info* info) {
       Now x = {};
       int by = 1;
       for (int i = 0; i < by; ++i, k.on(k_stages)) {
         ok = ok && __all_sync(0xffffffffu, wait(&bars.k_full[k.st], k.parity));
         if (!ok) return x;
         if (i == 0) {
-          const Step& s = s_step[k.st];
-          x = {p.mass.data + s.mass + team * kSlots + row, s.back + team * kSlots + row, s.n, s.off, s.blk0, s.blocks, s.flags, false};
-          by = s.flags & 3;
+          x = now_of(s_step[k.st]);
+          by = x.flags & 3;
+          if (info) info->step = s_step[k.st];
         }
+        if (info) info->lost[i] = s_lost[k.st];
         if (i == team) {
           ok = __all_sync(0xffffffffu, wait(&bars.read[buffer][team], read_parity >> buffer & 1));
           read_parity ^= 1u << buffer;
           if (!ok) return x;
           fence_after();
-          constexpr int kRegs = D / 4;  // D / 2 components
-          uint32_t r[kRegs];
-          const uint32_t from = k_ring + k.st * L::kStage + ((row / box * L::kHalves + (D == 128 ? part : 0)) * box + row % box) * 128;
-#pragma unroll
-          for (int c = 0; c < kRegs / 4; ++c) {
-            const int chunk = (D == 128 ? 0 : part * 4) + c;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(r[4 * c]), "=r"(r[4 * c + 1]), "=r"(r[4 * c + 2]), "=r"(r[4 * c + 3])
-                         : "r"(from + ((chunk ^ (row & 7)) << 4))
-                         : "memory");
+          if (kWide) {
+            move(part, buffer);
+          } else {
+            move(0, buffer);
+            move(1, buffer);
           }
-          x.lost = (s_lost[k.st] >> (row / box)) & 1;
-          tmem_store(my + (2 * buffer + team) * L::kKeys + part * kRegs, r);
+          x.lost = (s_lost[k.st] >> (row >> box_shift)) & 1;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.k_empty[k.st]);
@@ -558,168 +599,232 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       return x;
     };
-    uint32_t sums_parity = part;  // (the second half's: the first half's have been read)
-    Place score;                  // of the team's next product (kWide)
-    uint32_t own_parity = 0;      // of this half's place (else)
-    int buffer = 0;
-    bool fresh = true;
-    if (at.pos < end) {
-      Now now = convert(0), next = now;
-      while (ok) {
-        const bool ends = now.flags & 8;
-        if (!kWide && !ends) next = convert(buffer ^ 1);
-        if (!ok) break;
-        const bool many = now.blocks > 1, run_ends = now.flags & 4, mine = team < (now.flags & 3);
-        const int back = now.back, slot_back = back - row;  // (of the tile's first slot)
-        const bool whole = slot_back + kSlots <= 0;
-        float old = 0.f;
-        if (mine && part == 0 && p.decay != 0.f && back < 0) old = *now.mass;
-        float2 sum[2] = {};
-        for (int blk = now.blk0; blk < now.blocks && ok; ++blk) {
-          const int token0 = blk * tokens, cols = min(tokens, now.n - token0) * group;
-          const int wide = part_of(cols), c0 = part * wide, c1 = min(cols, c0 + wide);  // this warp's columns: up to 32 or 64
-          // (A place's barrier is never a lap ahead of a half.  Where a half has no columns, in a unit's last block, the keys of the
-          // team's next step wait for all products of this one.)
-          Place at_score = score;  // of this half's product
-          if (part == 1) at_score.on(L::kScorePlaces);
-          const int place = kWide ? at_score.st : part;
-          if (mine && c0 < c1) {
-            ok = ok && __all_sync(0xffffffffu, wait(&bars.scores[team][place], kWide ? at_score.parity : own_parity));
-            own_parity ^= 1;
-          } else if (many || fresh) {
-            ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
-          }
-          if (mine) {
-            score.on(L::kScorePlaces);
-            if (cols > wide) score.on(L::kScorePlaces);
-          }
-          if (!ok) break;
-          if (mine && c0 < c1) {
-            uint64_t* const taken = &bars.taken[team][place];
-            const uint32_t my_scores = my + L::kScores + (team * L::kScorePlaces + place) * kPart;
-            fence_after();
-            const auto add = [&](const uint32_t (&r)[32], const float4* lse) {
+    float2 sum[2];  // of this thread's slot
+    // Adds the weights of columns [c0, c1) of a block, up to 64 of one product, whose scores are in `place`.
+    const auto weigh = [&](const Now& now, int blk, int cols, int c0, int c1, int place) {
+      const int back = now.back, token0 = blk * tokens;
+      const bool whole = back - row + kSlots <= 0;
+      uint64_t* const taken = &bars.taken[team][place];
+      const uint32_t my_scores = my + L::kScores + (team * L::kScorePlaces + place) * kPart;
+      fence_after();
+      const auto add = [&](const uint32_t (&r)[32], const float4* lse) {
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 l = lse[j / 4];
-                const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), scale2, make_float2(l.x, l.y));
-                const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), scale2, make_float2(l.z, l.w));
-                sum[0] = __fadd2_rn(sum[0], make_float2(ex2(x0.x), ex2(x0.y)));
-                sum[1] = __fadd2_rn(sum[1], make_float2(ex2(x1.x), ex2(x1.y)));
-              }
-            };
-            // all columns count for all of the warp's slots (in a chain: those of tokens past the last of them)
-            bool all = kWide && c1 - c0 == kPart && (s_counts[q.st][c0 / 32] & s_counts[q.st][c0 / 32 + 1]) == 0xffffffffu;
-            if (all && !whole) all = __all_sync(0xffffffffu, back < 0 || (chain && back <= token0 + part_token));
-            if (all) {
-              uint32_t r0[32], r1[32];
-              tmem_load32(r0, my_scores);
-              tmem_load32(r1, my_scores + 32);
-              tmem_wait_load();
-              fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(taken);
-              add(r0, reinterpret_cast<const float4*>(&s_lse[q.st][c0]));
-              add(r1, reinterpret_cast<const float4*>(&s_lse[q.st][c0 + 32]));
-            } else
+        for (int j = 0; j < 32; j += 4) {
+          const float4 l = lse[j / 4];
+          const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), scale2, make_float2(l.x, l.y));
+          const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), scale2, make_float2(l.z, l.w));
+          sum[0] = __fadd2_rn(sum[0], make_float2(ex2(x0.x), ex2(x0.y)));
+          sum[1] = __fadd2_rn(sum[1], make_float2(ex2(x1.x), ex2(x1.y)));
+        }
+      };
+      // all columns count for all of the warp's slots (in a chain: those of tokens past the last of them)
+      bool all = kWide && c1 - c0 > 32 && s_counts[q.st][c0 / 32] == 0xffffffffu && s_counts[q.st][c0 / 32 + 1] == 0xffffffffu >> (c0 + kPart - c1);
+      if (all && !whole) all = __all_sync(0xffffffffu, back < 0 || (chain && back <= token0 + c0 / group));
+      if (all) {
+        uint32_t r0[32], r1[32];
+        tmem_load32(r0, my_scores);
+        tmem_load32(r1, my_scores + 32);
+        tmem_wait_load();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(taken);
+        add(r0, reinterpret_cast<const float4*>(&s_lse[q.st][c0]));
+        add(r1, reinterpret_cast<const float4*>(&s_lse[q.st][c0 + 32]));
+      } else
 #pragma unroll 1
-            for (int c = c0; c < c1; c += 32) {
-              const uint32_t from = my_scores + c - c0;
-              const float4* lse = reinterpret_cast<const float4*>(&s_lse[q.st][c]);
-              const int n = min(c1 - c, 32);  // columns
-              const bool last = c + 32 >= c1;
-              const uint32_t every = 0xffffffffu >> (32 - n);
-              uint32_t see = s_counts[q.st][c / 32];
-              bool full = see == every, none = see == 0;
-              if (!whole) {
-                if (back >= 0) {
-                  if (chain) {  // from the first column of a token that is as far on as the slot
-                    const int first = back > token0 ? min(back - token0, tokens) * group - c : 0;
-                    see = first >= 32 ? 0 : first > 0 ? see >> first << first : see;
-                  } else {
-                    const int last_token = (min(c + 32, cols) - 1) / group;
-                    uint32_t by_bits = 0;
-                    for (int i = c / group; i <= last_token; ++i) {  // (tokens with a column among these)
-                      const int first = max(i * group - c, 0), upto = min((i + 1) * group - c, 32);
-                      if (__ldg(a.tree_mask + now.off + token0 + i) >> (back & 63) & 1) by_bits |= (0xffffffffu >> (32 - (upto - first))) << first;
-                    }
-                    see &= by_bits;
-                  }
-                }
-                full = __all_sync(0xffffffffu, see == every);
-                none = __all_sync(0xffffffffu, see == 0);
+      for (int c = c0; c < c1; c += 32) {
+        const uint32_t from = my_scores + c - c0;
+        const float4* lse = reinterpret_cast<const float4*>(&s_lse[q.st][c]);
+        const int n = min(c1 - c, 32);  // columns
+        const bool last = c + 32 >= c1;
+        const uint32_t every = 0xffffffffu >> (32 - n);
+        uint32_t see = s_counts[q.st][c / 32];
+        bool full = see == every, none = see == 0;
+        if (!whole) {
+          if (back >= 0) {
+            if (chain) {  // from the first column of a token that is as far on as the slot
+              const int first = back > token0 ? min(back - token0, tokens) * group - c : 0;
+              see = first >= 32 ? 0 : first > 0 ? see >> first << first : see;
+            } else {
+              const int last_token = (min(c + 32, cols) - 1) / group;
+              uint32_t by_bits = 0;
+              for (int i = c / group; i <= last_token; ++i) {  // (tokens with a column among these)
+                const int first = max(i * group - c, 0), upto = min((i + 1) * group - c, 32);
+                if (__ldg(a.tree_mask + now.off + token0 + i) >> (back & 63) & 1) by_bits |= (0xffffffffu >> (32 - (upto - first))) << first;
               }
-              if (none) {
-                if (last) {
-                  fence_before();
-                  __syncwarp();
-                  if (lane == 0) mbar_arrive(taken);
-                }
-                continue;
-              }
-              if (full) {  // (columns past the last have weights of 0)
-                uint32_t r[32];
-                tmem_load32(r, from);
-                tmem_wait_load();
-                if (last) {
-                  fence_before();
-                  __syncwarp();
-                  if (lane == 0) mbar_arrive(taken);
-                }
-                add(r, lse);
-                continue;
-              }
-              // (eight columns at a time, in a loop: unrolled with the others' this took so many registers that the whole kernel
-              // was slower: 32 trees of 13 tokens 147 us)
-#pragma unroll 1
-              for (int j = 0; j < n; j += 8) {
-                uint32_t r[8];
-                __syncwarp();
-                tmem_load8(r, from + j);
-                tmem_wait_load();
-                if (last && j + 8 >= n) {
-                  fence_before();
-                  __syncwarp();
-                  if (lane == 0) mbar_arrive(taken);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  const float e = ex2(fmaf(__uint_as_float(r[i]), scale2.x, reinterpret_cast<const float*>(lse)[j + i]));
-                  sum[i & 1].x += see >> (j + i) & 1 ? e : 0.f;
-                }
-              }
+              see &= by_bits;
             }
           }
-          if (many || run_ends) {
+          full = __all_sync(0xffffffffu, see == every);
+          none = __all_sync(0xffffffffu, see == 0);
+        }
+        if (none) {
+          if (last) {
+            fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.q_empty[q.st]);
-            q.on(q_stages);
+            if (lane == 0) mbar_arrive(taken);
+          }
+          continue;
+        }
+        if (full) {  // (columns past the last have weights of 0)
+          uint32_t r[32];
+          tmem_load32(r, from);
+          tmem_wait_load();
+          if (last) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(taken);
+          }
+          add(r, lse);
+          continue;
+        }
+        // (eight columns at a time, in a loop: unrolled with the others' this took so many registers that the whole kernel
+        // was slower: 32 trees of 13 tokens 147 us)
+#pragma unroll 1
+        for (int j = 0; j < n; j += 8) {
+          uint32_t r[8];
+          __syncwarp();
+          tmem_load8(r, from + j);
+          tmem_wait_load();
+          if (last && j + 8 >= n) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(taken);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float e = ex2(fmaf(__uint_as_float(r[i]), scale2.x, reinterpret_cast<const float*>(lse)[j + i]));
+            sum[i & 1].x += see >> (j + i) & 1 ? e : 0.f;
           }
         }
-        if (kWide && !ends) next = convert(0);
-        if (!ok) break;
-        fresh = run_ends;
-        if (mine) {  // the columns' halves meet
-          float w = (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
-          ok = __all_sync(0xffffffffu, wait(part == 0 ? &bars.sums[team] : &bars.joined[team], sums_parity));
-          sums_parity ^= 1;
+      }
+    };
+    // (A load behind a branch was waited for there.)
+    const auto old_mass = [&](const Now& now, bool mine) {
+      float x = 0.f;
+      asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n @p ld.global.f32 %0, [%1];\n}"
+                   : "+f"(x)
+                   : "l"(now.mass), "r"((uint32_t)(mine && p.decay != 0.f && now.back < 0))
+                   : "memory");
+      return x;
+    };
+    const auto put = [&](const Now& now, float w, float old) {
+      if (now.back < 0 && p.decay != 0.f) w = fmaf(p.decay, old, w);
+      if (now.back < now.n) *now.mass = now.lost ? NAN : w;
+      if (now.lost && now.back < now.n) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
+    };
+    Place score;  // of the team's next product
+    bool fresh = true;
+    if (kWide) {
+      uint32_t sums_parity = part;  // (the second half's: the first half's have been read)
+      if (at.pos < end) {
+        Now now = convert(0, nullptr), next = now;
+        while (ok) {
+          const bool ends = now.flags & 8, many = now.blocks > 1, run_ends = now.flags & 4, mine = team < (now.flags & 3);
+          const float old = old_mass(now, mine && part == 0);
+          sum[0] = sum[1] = make_float2(0.f, 0.f);
+          for (int blk = now.blk0; blk < now.blocks && ok; ++blk) {
+            const int cols = min(tokens, now.n - blk * tokens) * group;
+            const int wide = part_of(cols), c0 = part * wide, c1 = min(cols, c0 + wide);  // this warp's columns: up to 32 or 64
+            // (Where a half has no columns, in a unit's last block, the keys of the team's next step wait for all products of this
+            // one: a place's barrier is never a lap ahead of a half.)
+            Place own = score;  // of this half's product
+            if (part == 1) own.on(L::kScorePlaces);
+            if (mine && c0 < c1)
+              ok = __all_sync(0xffffffffu, wait(&bars.scores[team][own.st], own.parity));
+            else if (many || fresh)
+              ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
+            if (!ok) break;
+            if (mine) {
+              score.on(L::kScorePlaces);
+              if (cols > wide) score.on(L::kScorePlaces);
+              if (c0 < c1) weigh(now, blk, cols, c0, c1, own.st);
+            }
+            if (many || run_ends) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars.q_empty[q.st]);
+              q.on(q_stages);
+            }
+          }
+          if (!ends) next = convert(0, nullptr);
           if (!ok) break;
-          if (part == 1) {
-            s_sum[team][row] = w;
+          fresh = run_ends;
+          if (mine) {  // the columns' halves meet
+            float w = (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+            ok = __all_sync(0xffffffffu, wait(part == 0 ? &bars.sums[team] : &bars.joined[team], sums_parity));
+            sums_parity ^= 1;
+            if (!ok) break;
+            if (part == 1) {
+              s_sum[team][row] = w;
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars.sums[team]);
+            } else {
+              w += s_sum[team][row];
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars.joined[team]);
+              put(now, w, old);
+            }
+          }
+          if (ends) break;
+          now = next;
+        }
+      }
+    } else if (at.pos < end) {
+      Place info;
+      if (part == 1) {  // keys, up to two steps ahead of their products
+        bool ends = false;
+        for (int buffer = 0; !ends; buffer ^= 1) {
+          Info x;
+          const Now now = convert(buffer, &x);
+          if (!ok) break;
+          ends = now.flags & 8;
+          if (warp == kTeamWarps) {  // (one warp leaves what the weights need: the stages are let go of)
+            ok = __all_sync(0xffffffffu, wait(&bars.info_empty[info.st], info.parity ^ 1));
+            if (!ok) break;
+            if (lane == 0) {
+              s_info[info.st] = x;
+              mbar_arrive(&bars.info_full[info.st]);
+            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.sums[team]);
-          } else {
-            w += s_sum[team][row];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.joined[team]);
-            if (back < 0 && p.decay != 0.f) w = fmaf(p.decay, old, w);
-            if (back < now.n) *now.mass = now.lost ? NAN : w;
-            if (now.lost && back < now.n) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
+            info.on(kInfos);
           }
         }
-        if (ends) break;
-        now = next;
-        buffer ^= L::kKeyPlaces - 1;
+      } else {
+        bool ends = false;
+        while (!ends) {
+          ok = __all_sync(0xffffffffu, wait(&bars.info_full[info.st], info.parity));
+          if (!ok) break;
+          Now now = now_of(s_info[info.st].step);
+          now.lost = (s_info[info.st].lost[team] >> (row >> box_shift)) & 1;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars.info_empty[info.st]);
+          info.on(kInfos);
+          ends = now.flags & 8;
+          const bool many = now.blocks > 1, run_ends = now.flags & 4, mine = team < (now.flags & 3);
+          const float old = old_mass(now, mine);
+          sum[0] = sum[1] = make_float2(0.f, 0.f);
+          for (int blk = now.blk0; blk < now.blocks && ok; ++blk) {
+            const int cols = min(tokens, now.n - blk * tokens) * group;
+            if (mine) {
+              for (int c0 = 0; c0 < cols && ok; c0 += kPart) {
+                ok = __all_sync(0xffffffffu, wait(&bars.scores[team][score.st], score.parity));
+                if (ok) weigh(now, blk, cols, c0, min(cols, c0 + kPart), score.st);
+                score.on(L::kScorePlaces);
+              }
+            } else if (many || fresh) {
+              ok = __all_sync(0xffffffffu, wait(&bars.q_full[q.st], q.parity));
+            }
+            if (!ok) break;
+            if (many || run_ends) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars.q_empty[q.st]);
+              q.on(q_stages);
+            }
+          }
+          if (!ok) break;
+          fresh = run_ends;
+          if (mine) put(now, (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y), old);
+        }
       }
     }
     if (!ok && lane == 0) {
