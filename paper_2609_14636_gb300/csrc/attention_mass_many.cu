@@ -16,13 +16,13 @@
 //        memory, weights, sums.
 // Where units have many rows (kWide) the exponentials count: each of the sixteen does both, four
 // for each tile and half of the columns, whose waits for their next product are filled
-// by the three others of a scheduler.  Where they have up to 64, a tile costs its
+// by the three others of a scheduler.  Where they have few blocks, a tile costs its
 // way through the CTA: eight bring keys, two steps ahead, eight add up (all sixteen doing
 // both, one after the other: 32 trees of 13 tokens 87 us, 79).
 // The rows of a unit that fit in one block are copied once for all its tiles.
 //
 // Measured, us (floor: of bytes at 6,683 GB/s, of products at 1,981 TFLOP/s): 32 trees of 13 tokens, 32 / 8 heads of 128, over up to
-// 8,000 slots 79 (55; 4.6 TB/s: the weights' chain of waits, 3,600 clocks for two tiles); 4 chains of 511 over up to 6,000 90
+// 8,000 slots 78 (55; 4.7 TB/s: the weights' chain of waits, 3,600 clocks for two tiles); 4 chains of 511 over up to 6,000 90
 // (35, the exponentials 30 at 32 a clock and SM; 0.78 PFLOP/s: without the exponentials 70, product, scores and sums one after the
 // other).  The simple kernel of mma.sync took 313 and 1,126.
 #include <cuda_bf16.h>
@@ -43,7 +43,6 @@ constexpr int kTeamWarps = 8;      // of a tile's
 constexpr int kWarps = 2 * kTeamWarps + 4, kThreads = kWarps * 32;
 constexpr int kMaxStages = 12;
 constexpr int kInfos = 4;          // steps that weights may be behind the keys
-constexpr int kTileCost = 4;       // what a tile costs at least, in blocks
 
 // kWide: a team's products take three places for their scores in turn, so that two are on their way while one is worked on, and its
 // keys have one; else two places each, as the keys count.
@@ -75,23 +74,28 @@ struct Place {
   }
 };
 
-// A sequence's tiles of a head, and what one costs.
+// A sequence's tiles of a head, and what one costs: its blocks, and three at least where all warps take part in a step's start and end
+// (two chains of 511 tokens among six of 40 over 4,000 slots, us: at least 1 95, 2 95, 3 79, 4 91; a chain of 1,000 among seven of 13
+// over 6,000: 181, 113, 124, 125).  Elsewhere that is done beside the blocks (31 of 8 tokens and a chain of 300 over 4,000: 1 87, 2
+// 140, 4 224).
 struct Unit {
   int32_t ctx, n, off, tiles, blocks, cost;
   bool bad;
 };
+template <bool kWide>
 __device__ __forceinline__ Unit unit_of(const MassParams& p, int b, int tokens) {
   const Seq s = sequence(p.a, b);
   Unit u = {s.ctx, s.n, s.off, 0, 0, 0, s.bad || (s.n > 0 && (int64_t)s.ctx + s.n > p.mass.slots)};
   if (!u.bad && u.n > 0) {
     u.tiles = (u.ctx + u.n + kSlots - 1) / kSlots;
     u.blocks = (u.n + tokens - 1) / tokens;
-    u.cost = max(kTileCost, u.blocks);
+    u.cost = max(kWide ? 3 : 1, u.blocks);
   }
   return u;
 }
 
 // A place among the tiles of the call: sequences, of one the heads, of one the tiles.
+template <bool kWide>
 struct Cursor2 {
   int32_t b, head, tile;
   int64_t pos;  // the cost of what lies before it
@@ -106,7 +110,7 @@ struct Cursor2 {
     head = 0;
     do {
       if (++b >= p.a.cache.n_seqs) return;  // (past the last tile: pos is the call's cost)
-      u = unit_of(p, b, tokens);
+      u = unit_of<kWide>(p, b, tokens);
     } while (u.tiles == 0);
   }
   // Tiles of the step here: two where the unit and the share, which ends at `end`, have them.
@@ -219,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   int64_t total = 0, first = 0, of_all;
   const auto cost_of = [&](int b) -> int64_t {
     if (b >= pc.n_seqs) return 0;
-    const Unit u = unit_of(p, b, tokens);
+    const Unit u = unit_of<kWide>(p, b, tokens);
     if (u.bad && blockIdx.x == 0) set_status(a.dev_status, STRIDE_DEV_BAD_LAYOUT);
     return (int64_t)u.tiles * u.cost * pc.n_heads;
   };
@@ -251,9 +255,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   fence_after();
   constexpr uint32_t tmem = 0;  // (all columns are this CTA's)
-  Cursor2 at;
+  Cursor2<kWide> at;
   at.b = s_seq;
-  at.u = unit_of(p, at.b, tokens);
+  at.u = unit_of<kWide>(p, at.b, tokens);
   {  // the first tile that starts at `begin` or after it
     const int64_t tile = (begin - s_pos + at.u.cost - 1) / at.u.cost;
     at.head = (int)(tile / at.u.tiles);
@@ -872,7 +876,8 @@ cudaError_t run(const MassParams& p, bool bf16, int sms, cudaStream_t stream) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  // units of several blocks stream the rows past the keys, others the keys past the rows
+  // units of several blocks stream the rows past the keys, others the keys past the rows (chains of 511 tokens, us: 2 stages of keys 97,
+  // 3 99, 4 105; trees of 13 72, 68, 68, of 5 70)
   const int64_t mean = (p.a.n_tokens + c.n_seqs - 1) / c.n_seqs;
   const int k_stages = mean > tokens ? L::kStages / 3 : L::kStages * 2 / 3;
   e = cudaLaunchKernelEx(&cfg, kern, p, k_map, q_map, box, page_shift(c.page_size), tokens, k_stages, both);
@@ -890,8 +895,9 @@ bool attention_mass_many_takes(const MassParams& p) {
 }
 
 cudaError_t launch_attention_mass_many(const MassParams& p, int dtype, int sms, cudaStream_t stream) {
-  // (wide: 64 scores of a lane at once, for which parts of fewer columns have no use, and pay in registers)
-  const bool wide = ((p.a.n_tokens + p.a.cache.n_seqs - 1) / p.a.cache.n_seqs) * (p.a.Hq / p.a.cache.n_heads) > kPart;
+  // By the mean of rows a sequence: all warps add up from two blocks on (a sequence's rows, us else, so: 64 68 106, 128 78 111, 256
+  // 124 139, 384 97 94, 512 122 109, 2,044 130 97; 4 to 32 sequences of 4,000 slots).
+  const bool wide = ((p.a.n_tokens + p.a.cache.n_seqs - 1) / p.a.cache.n_seqs) * (p.a.Hq / p.a.cache.n_heads) > 2 * kCols;
   const bool bf16 = dtype == STRIDE_DTYPE_BF16;
   const auto of = [&](auto type) {
     using T = decltype(type);

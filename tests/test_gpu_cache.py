@@ -77,6 +77,7 @@ MASS = [
     ([(1000, 1)] * 40 + [(20, 90)], 4, 2, 64, 16, "rows", False, 1.0, "bf16"),
     # several tiles for each CTA, odd numbers of them among them, of one block of rows or more
     ([(3900, 40), (1200, 33), (5000, 45), (130, 60)], 32, 8, 128, 32, "rows", False, 0.9, "bf16"),
+    ([(3900, 140), (1200, 33), (5000, 145), (130, 60)], 32, 8, 128, 32, "rows", False, 0.9, "f16"),
     ([(3900, 13), (1200, 9), (5000, 11), (130, 2)], 16, 8, 120, 24, "heads", True, 1.0, "f16"),
 ]
 
