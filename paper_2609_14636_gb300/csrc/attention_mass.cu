@@ -20,6 +20,10 @@
 // slots, as registers bound what is on its way.)  The rows are the second operand and stay
 // in registers where a unit has no more than the kernel takes at once; a result's two
 // columns are added in the lane, the quad's by shuffles.
+//
+// Measured, us (floor: of bytes at 6,683 GB/s): 256 sequences, a token each over up to 4,096 slots, 32 / 8 heads of 128, 224 (212; 6.3
+// TB/s: memory); one token over 131,072 48.8 (41; the ramp and the last tiles of 7 us); over 37 4.9 (a launch and a chain of four
+// loads).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

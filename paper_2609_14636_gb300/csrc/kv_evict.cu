@@ -9,6 +9,11 @@
 // as far as they fit.  The second copies the rows, which is what counts: pages are
 // looked up and offsets computed once for a CTA's rows, then threads move 16 bytes at
 // a time, several loads each on their way.
+//
+// Measured, us (floor: of bytes at 6,683 GB/s): 256 sequences of up to 4,096 slots to 1,024, 8 heads of 128, 343 (310: the copy 300,
+// before it the selection); one of 131,072 to 16,384 45 (21: the copy 20, the selection's exchanges in clusters of 16 before it 22);
+// three of up to 323 9.6 (two launches and the digits' passes).  Rows that remain for sure copied by CTAs of the first kernel: 420
+// and 48.
 #include <cooperative_groups.h>
 
 #include <algorithm>
