@@ -302,8 +302,8 @@ cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, 
   const int64_t slots = std::min<int64_t>(p.mass.slots, p.from.table_stride * (int64_t)p.from.page_size);
   int C = 1;
   while (C < kMaxCluster && (int64_t)units * C * 2 <= sms && slots > (int64_t)C * 1024) C *= 2;
-  // (256 sequences of up to 4,096 slots, us: 256 threads of 16 masses each 344, 512 of 8 352; a cluster's, of up to 131,072 slots:
-  // 512 threads 45, 256 77)
+  // (256 sequences of up to 4,096 slots, us: 256 threads of 16 masses each 343, 512 of 8 368; a cluster's, of up to 131,072 slots:
+  // 512 threads 45, 256 78)
   const bool few = C == 1 && slots <= 4096;
   const auto kern = few ? select_kernel<256, 16, 5> : select_kernel<512, 16, 2>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);

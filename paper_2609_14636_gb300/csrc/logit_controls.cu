@@ -63,7 +63,8 @@ __device__ __forceinline__ uint4 masked(uint4 v, uint32_t bits) {
 }
 
 constexpr int kThreads = 512;
-constexpr int kAhead = 3;         // vectors of a lane in a run (256 rows of 151,936, us: 2 40.6, 3 40.2, 4 43.1)
+constexpr int kCounters = 256;    // of them, those that count first (256 rows of 151,936, us: 36.8, all 42.1; one row in a graph 5.6, 5.9)
+constexpr int kAhead = 3;         // vectors of a lane in a run (256 rows of 151,936, us: 2 38.3, 3 36.8, 4 38.5)
 constexpr int kMostWords = 8192;  // of a slice's bits
 constexpr int kWindow = 4096;     // places that have counts at a time
 constexpr uint32_t kPrompt = 0x80000000u, kBias = 0x40000000u;  // flags of a count
@@ -100,10 +101,9 @@ struct Run {
   uint32_t lo[kAhead], hi[kAhead];
 };
 
-// Blocks: row * slices + slice; counters: threads (256 or all) that count first.  Shared memory: the bits and their prefix sums, counts, tokens and last biases of a window.
+// Blocks: row * slices + slice.  Shared memory: the bits and their prefix sums, counts, tokens and last biases of a window.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_constant__ ControlParams p, const int slice, const int slices,
-                                                                const int counters) {
+__global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_constant__ ControlParams p, const int slice, const int slices) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int kVec = 16 / (int)sizeof(T);
@@ -201,23 +201,23 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
 
   // ---- which tokens occur, and how often ----
   const bool fixes = r.history || r.bias_off;
-  if (fixes && tid < counters) {
-    const auto sync = [&] { asm volatile("bar.sync 1, %0;" ::"r"(counters) : "memory"); };
+  if (fixes && tid < kCounters) {
+    const auto sync = [&] { asm volatile("bar.sync 1, %0;" ::"r"(kCounters) : "memory"); };
     int held[kOnce];  // (on their way with what says how many count)
 #pragma unroll
     for (int u = 0; u < kOnce; ++u) {
-      const int64_t i = tid + (int64_t)u * counters;
+      const int64_t i = tid + (int64_t)u * kCounters;
       held[u] = r.history && i < r.history_most ? __ldg(history + i) : -1;
     }
     const Applies h = applies_to(r, row);
 #pragma unroll
     for (int u = 0; u < kOnce; ++u)
-      if (tid + u * counters >= h.n) held[u] = -1;
+      if (tid + u * kCounters >= h.n) held[u] = -1;
     if (tid == 0) s_applies = h;
     const bool any = !h.bad && (h.n > 0 || h.biases > 0);
     if (tid == 0) s_total = 0;
     if (any) {
-      for (int i = tid; i < words / 4; i += counters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
+      for (int i = tid; i < words / 4; i += kCounters) reinterpret_cast<uint4*>(bits)[i] = make_uint4(0, 0, 0, 0);
       sync();
       const auto set = [&](int, int t) {
         if (inside(t))
@@ -227,11 +227,11 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       };
 #pragma unroll
       for (int u = 0; u < kOnce; ++u) set(0, held[u]);
-      each(history, tid + (int64_t)kOnce * counters, h.n, counters, set);
-      each(r.bias_token + h.bias0, tid, h.biases, counters, set);
+      each(history, tid + (int64_t)kOnce * kCounters, h.n, kCounters, set);
+      each(r.bias_token + h.bias0, tid, h.biases, kCounters, set);
       sync();
       // bits before each word: a warp's run of words by itself, four words of a lane at a time, then the warps' sums
-      const int warp = tid >> 5, warps = counters >> 5, run = (words + 128 * warps - 1) / (128 * warps) * 128;
+      const int warp = tid >> 5, warps = kCounters >> 5, run = (words + 128 * warps - 1) / (128 * warps) * 128;
       const int i1 = min(words, (warp + 1) * run);
       int base = 0;
       for (int i0 = warp * run; i0 < i1; i0 += 128) {
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
       }
       if (tid == 0) s_total = all;
       sync();
-      fill(h, 0, tid, counters, held, sync);
+      fill(h, 0, tid, kCounters, held, sync);
     }
   }
 
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
 
 template <typename T>
 cudaError_t run(const ControlParams& p, int sms, cudaStream_t stream) {
-  // twice as many slices as run at once (256 rows of 151,936, us: as many 45, twice 43, four times 46), of 8,192 tokens at least
+  // twice as many slices as run at once (256 rows of 151,936, us: as many 39.6, twice 36.8, four times 46.6), of 8,192 tokens at least
   // and as many as there are bits for at most
   const int64_t most = (int64_t)p.V + 8191, wanted = std::max<int64_t>(1, 4 * sms / p.rows);
   const int64_t about = std::max<int64_t>(std::min<int64_t>(wanted, most / 8192), (p.V + kMostWords * 32 - 1) / (kMostWords * 32));
@@ -380,9 +380,7 @@ cudaError_t run(const ControlParams& p, int sms, cudaStream_t stream) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  // where a CTA has an SM to itself nothing is gained by streaming early (one row: 256 of them 8.1 us, all 7.2; 256 rows: 43, 48)
-  const int counters = (int64_t)slices * p.rows <= sms ? kThreads : kThreads / 2;
-  e = cudaLaunchKernelEx(&cfg, kern, p, slice, slices, counters);
+  e = cudaLaunchKernelEx(&cfg, kern, p, slice, slices);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
