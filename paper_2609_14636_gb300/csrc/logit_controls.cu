@@ -14,9 +14,9 @@
 // own after the copy they came from memory again, 61 us beside the copy's 24 for 256
 // rows of 151,936).  In place and without a mask only they are read.
 //
-// Measured, us (floor: of bytes at 6,683 GB/s): 256 rows of 151,936 bf16 with a mask, histories of up to 4,096 and 100 biases 36.7
+// Measured, us (floor: of bytes at 6,683 GB/s): 256 rows of 151,936 bf16 with a mask, histories of up to 4,096 and 100 biases 36.5
 // (24.5; 4.5 TB/s: the listed logits, after the slice, with few CTAs left to hide their latency); 512 rows of 32,000 fp32 without a
-// mask 25.5 (20); one row 5.9 in a graph (a chain of eight steps between barriers).
+// mask 25.3 (20); one row 5.6 in a graph (a chain of eight steps between barriers).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
