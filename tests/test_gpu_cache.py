@@ -75,6 +75,10 @@ MASS = [
     ([(129, 100), (0, 0), (7, 300)], 6, 2, 120, 8, "wide", False, 0.99, "bf16"),
     ([(70, 90)], 2, 1, 128, 20, "rows", False, 1.0, "f16"),
     ([(1000, 1)] * 40 + [(20, 90)], 4, 2, 64, 16, "rows", False, 1.0, "bf16"),
+    # a chain of many blocks among units of one; pages of a tile and more, of which a warp looks up many at once
+    ([(700, 3)] * 12 + [(300, 200)], 16, 2, 128, 16, "rows", False, 1.0, "bf16"),
+    ([(5000, 9), (0, 0), (64, 64), (9000, 30)], 8, 2, 64, 128, "heads", False, 0.9, "f16"),
+    ([(5000, 90), (1, 1), (9000, 120)], 8, 2, 128, 256, "rows", False, 1.0, "bf16"),
     # several tiles for each CTA, odd numbers of them among them, of one block of rows or more
     ([(3900, 40), (1200, 33), (5000, 45), (130, 60)], 32, 8, 128, 32, "rows", False, 0.9, "bf16"),
     ([(3900, 140), (1200, 33), (5000, 145), (130, 60)], 32, 8, 128, 32, "rows", False, 0.9, "f16"),
