@@ -331,9 +331,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         // 13 tokens 87 us, 96)
         if (elect_one()) {
           const unsigned mine = (1u << boxes) - 1;
-          mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who >> (i * boxes) & mine) * L::kHalves * box * 128));
+          // (before the arrival, which publishes them: a tile without pages has no bytes to come, and its phase ends there)
           s_lost[k.st] = gone >> (i * boxes) & mine;
           s_step[k.st] = run.step;
+          mbar_arrive_expect_tx(bar, (uint32_t)(__popc(who >> (i * boxes) & mine) * L::kHalves * box * 128));
         }
         __syncwarp();
         if (my_tile == i && real) {
