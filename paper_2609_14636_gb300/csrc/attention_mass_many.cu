@@ -29,6 +29,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <cfloat>
 
 #include "attention_line.cuh"
 #include "tensor_core.cuh"
@@ -420,8 +421,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = __all_sync(0xffffffffu, wait(&bars.q_empty[q.st], q.parity ^ 1));
         if (!ok) break;
       }
-      // Rows past the block's last, up to a whole run of 32 columns, are the block's first again (zeros would make NaN of a key's
-      // infinities), and their columns' -lse is -inf: weights of 0.
+      // Rows past the block's last, up to a whole run of 32 columns, are its last again, and their columns' -lse is the lowest number:
+      // weights of 0.  They are added only where all rows of the run count and see the slot, the last among them, so that a score
+      // of theirs that is infinite or NaN makes the sum no other than that row's own does.  (Zeros, or a row that need not see the
+      // slot, would make NaN of a key's infinities.)
       uint64_t* bar = &bars.q_full[q.st];
       const bool ragged = cols % 32 != 0;
       const uint32_t to = q_ring + q.st * L::kStage;
@@ -435,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int j = 0; j < kCols / 32; ++j) {
         const unsigned counts = __ballot_sync(0xffffffffu, lse[j] != -INFINITY);
-        s_lse[q.st][lane + 32 * j] = lane + 32 * j < cols ? -lse[j] * kLog2e : -INFINITY;
+        s_lse[q.st][lane + 32 * j] = lane + 32 * j < cols ? -lse[j] * kLog2e : -FLT_MAX;
         if (lane == 0) s_counts[q.st][j] = counts;
         lse[j] = next[j];
       }
@@ -446,8 +449,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++t;
           break;
         }
+        const int last = cols - 1;
         for (int i = cols * 8 + lane; i < ((cols + 31) & ~31) * 8; i += 32) {
-          const int chunk = (i & 7) ^ (i >> 3 & 7);  // (of the first row, where nothing is swizzled)
+          const int chunk = last * 8 + ((i ^ i >> 3 ^ last) & 7);  // (a row's chunks are exchanged by its number)
 #pragma unroll
           for (int half = 0; half < L::kHalves; ++half) {
             uint32_t w[4];

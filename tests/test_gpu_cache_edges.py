@@ -57,3 +57,71 @@ def test_tiles_without_pages(env, page, D, new, lost):
         assert int(status) == BAD_LAYOUT
         got = m.double().cpu().numpy()
         assert np.isnan(got[nan]).all() and np.array_equal(got[~nan], whole[~nan])
+
+
+# sequences whose last block of rows (128 / group tokens) has a ragged run of 32 columns after a whole one: new tokens, Hq, Hk, D, tree
+RAGGED = [
+    # up to 256 rows a sequence: 40, 34, 63, 126 = 96 + 30 columns, 40 and 100 under trees
+    (20, 4, 2, 64, False), (17, 2, 1, 128, False), (21, 3, 1, 64, False), (42, 3, 1, 128, False), (20, 4, 2, 128, True), (25, 4, 1, 64, True),
+    # more: a last block of 40, 68, 116 columns; of 36 and 112 under trees (groups of 8, 9, 14)
+    (74, 8, 2, 64, False), (81, 4, 1, 128, False), (93, 4, 1, 64, False), (53, 8, 1, 128, True), (46, 9, 1, 64, True), (35, 14, 1, 128, True),
+]
+
+
+def ragged(torch, shape, decay=1.0, dtype="bf16"):
+    """Two sequences, of whose slots a warp's 32 have committed and new ones, all seen by a block's later rows; q of either sign."""
+    new, Hq, Hk, D, tree = shape
+    case = ([(120, new), (1000, new)], Hq, Hk, D, 16, "rows", tree, decay, dtype)
+    x = mass_inputs(torch, case)
+    if tree:  # a block's first token sees itself alone, the others all
+        tokens, bits = 128 // (Hq // Hk), np.full(2 * new, (1 << new) - 1, np.uint64)
+        for i in range(2 * new):
+            if i % new % tokens == 0:
+                bits[i] = 1 << (i % new)
+        x["mask"] = torch.tensor(bits.view(np.int64), device="cuda")
+    return case, x
+
+
+@pytest.mark.parametrize("shape", RAGGED, ids=str)
+def test_rows_of_any_values_that_do_not_vote(env, shape):
+    """An lse of -inf: the row may hold NaN and infinities, wherever in a block it is."""
+    torch, stride, dev = env
+    new, Hq, Hk, D, _ = shape
+    tokens = 128 // (Hq // Hk)
+    for some in ([0], list(range(0, new, tokens)), [new - 1], [min(new // tokens * tokens, new - 1)], list(range(0, new, 3))):
+        case, x = ragged(torch, shape)
+        for i, t in enumerate(some):
+            for b in range(2):
+                x["lse"][b * new + t] = float("-inf")
+                x["q"][b * new + t] = (float("nan"), float("inf"), float("-inf"))[i % 3]
+        before = x["mass"].double().cpu().numpy()
+        call_mass(stride, torch, x, case)
+        check_mass(x, case, before, x["mass"].double().cpu().numpy())
+
+
+@pytest.mark.parametrize("shape", RAGGED, ids=str)
+def test_infinite_new_keys(env, shape):
+    """A new key whose scores are -inf for the rows that see it and +inf or NaN for those that do not: weights of 0, and all other
+    slots as if it were finite, with the same bits.  And one whose scores are +inf for the rows that see it: that slot is infinite."""
+    torch, stride, dev = env
+    new, Hq, Hk, D, tree = shape
+    tokens = 128 // (Hq // Hk)
+    at = [3] if tree else [t for t in (*range(1, 8), tokens + 1, 2 * tokens + 2) if t < new]
+    for value, j in [(v, j) for v in ("-inf", "+inf") for j in at]:
+        case, x = ragged(torch, shape)
+        x["q"][..., 5] = x["q"][..., 5].abs() + 0.1
+        sees = (np.arange(new) >= j) if not tree else np.arange(new) % tokens != 0
+        for b in range(2):
+            for i in np.flatnonzero(~sees):
+                x["q"][b * new + int(i), :, 5] *= (-1, 0)[int(i) % 2]  # (+inf, NaN)
+        finite = x["mass"].clone()
+        call_mass(stride, torch, x, case, mass=finite)
+        for b, (c, _) in enumerate(case[0]):
+            x["k"][int(x["table"][b, (c + j) // 16]), (c + j) % 16, :, 5] = float(value)
+        call_mass(stride, torch, x, case)
+        for b, (c, _) in enumerate(case[0]):
+            assert (x["mass"][b, :, c + j] == (0.0 if value == "-inf" else float("inf"))).all(), (value, j, x["mass"][b, :, c + j])
+            x["mass"][b, :, c + j] = finite[b, :, c + j]
+        assert torch.equal(x["mass"], finite), (value, j)
+        assert finite.isfinite().all()
+
