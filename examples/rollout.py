@@ -72,9 +72,11 @@ class Model:
         self.spare = [tuple(torch.empty_like(c) for c in cache) for cache in self.cache]  # (the pages of the next eviction)
 
     def evict(self, ctx_len, budget, sink=2, recent=8):
-        """Keeps `budget` slots of each sequence and kv head (negative: all) and returns how many are cached then.  The pages that they
-        came from stay as they are until the next eviction."""
+        """Keeps `budget` slots (a number, or int32 for each sequence) of each sequence and kv head (negative: all) and returns how many
+        are cached then.  The pages that they came from stay as they are until the next eviction."""
         s, B = self.s, self.slots
+        budget = torch.as_tensor(budget, dtype=torch.int32, device=self.device).expand(B)
+        budget = torch.where(budget < 0, ctx_len, budget)  # (the call would leave such a sequence in the old pages)
         new_len, kept = torch.empty_like(ctx_len), torch.empty(B, s.kv_heads, s.longest, dtype=torch.int32, device=self.device)
         for i, (cache, spare) in enumerate(zip(self.cache, self.spare)):
             mass = torch.zeros_like(self.mass[i])

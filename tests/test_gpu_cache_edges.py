@@ -3,10 +3,14 @@ the same call on whole inputs or their plain forms in 64 bits (tests/cache_refer
 tolerances)."""
 from __future__ import annotations
 
+import importlib.util
+import sys
+from pathlib import Path
+
 import numpy as np
 import pytest
 
-from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, mass_inputs
+from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, i32, mass_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +129,43 @@ def test_infinite_new_keys(env, shape):
         assert torch.equal(x["mass"], finite), (value, j)
         assert finite.isfinite().all()
 
+
+# ---------------------------------------------------------------------------------------------------------------------
+# eviction
+# ---------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("budget", [-1, [-1, 8, -7]], ids=str)
+def test_the_example_keeps_all_slots_of_a_negative_budget(env, budget):
+    """Such a sequence's slots and their masses go along to the new pages: with all kept, the next logits are the same bits."""
+    torch, stride, dev = env
+    path = Path(__file__).resolve().parents[1] / "examples" / "rollout.py"
+    spec = importlib.util.spec_from_file_location("rollout_example_edges", path)
+    example = importlib.util.module_from_spec(spec)
+    sys.modules[spec.name] = example
+    spec.loader.exec_module(example)
+    counts = torch.tensor([37, 20, 5], device=dev)
+    tokens = torch.randint(0, 4096, (int(counts.sum()),), generator=torch.Generator(device="cuda").manual_seed(6), device=dev).int()
+    zero, more = torch.zeros(3, dtype=torch.int32, device=dev), torch.tensor([7, 8, 9], dtype=torch.int32, device=dev)
+    models = [example.Model(example.Shape(), 3, 1) for _ in range(2)]
+    for m in models:
+        m.watch()
+        m(tokens, example.chain(zero, counts), zero, example.offsets(counts))
+    ctx = counts.int()
+    m, other = models
+    new_len = m.evict(ctx, budget if isinstance(budget, int) else i32(torch, budget))
+    left = torch.where(torch.tensor(budget, device=dev) < 0, ctx, torch.tensor(budget, device=dev))
+    assert torch.equal(new_len, left.int()) and int(m.status) == 0
+    page = m.s.page
+    for layer in range(m.s.layers):
+        for b in range(3):
+            if int(left[b]) < int(ctx[b]):
+                continue
+            i = torch.arange(int(ctx[b]), device=dev)
+            at = m.table[b].long()[i // page], i % page
+            for a, c in zip(m.cache[layer], other.cache[layer]):
+                assert torch.equal(a[at], c[at])
+            assert torch.equal(m.mass[layer][b, :, :len(i)], other.mass[layer][b, :, :len(i)])
+    step = example.offsets(torch.ones_like(counts))
+    a, c = m(more, ctx, new_len, step), other(more, ctx, ctx, step)
+    assert a.isfinite().all()
+    if isinstance(budget, int):
+        assert torch.equal(a, c)
