@@ -247,13 +247,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks) select_kernel(const __grid_
 
 constexpr int kRows = 64;          // rows of a CTA at a time
 constexpr int kCopyThreads = 256;
+constexpr int64_t kNowhere = INT64_MIN;  // (an offset may be negative: a pool's strides may)
 
 // Blocks: unit * splits + part, which takes every splits-th run of kRows rows.
 template <typename V>
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ EvictParams p, const int elem, const int splits) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  __shared__ int64_t s_from[kRows], s_to[kRows];  // bytes; -1: not copied
+  __shared__ int64_t s_from[kRows], s_to[kRows];  // bytes; kNowhere: not copied
   const int unit = blockIdx.x / splits, part = blockIdx.x - unit * splits, b = unit / p.from.n_heads, head = unit - b * p.from.n_heads;
   if (p.how.budget ? __ldg(p.how.budget + b) < 0 : p.how.budget_all < 0) return;
   const int m = p.new_len[b];
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
       const bool ok = page >= 0 && page < p.from.n_pages && there >= 0 && there < p.to.n_pages;
       if (!ok) set_status(p.dev_status, STRIDE_DEV_BAD_LAYOUT);
       s_from[tid] = (page * p.from.page_stride + (slot - e * p.from.page_size) * p.from.row_stride + head * p.from.head_stride) * elem;
-      s_to[tid] = ok ? (there * p.to.page_stride + (i - f * p.to.page_size) * p.to.row_stride + head * p.to.head_stride) * elem : -1;
+      s_to[tid] = ok ? (there * p.to.page_stride + (i - f * p.to.page_size) * p.to.row_stride + head * p.to.head_stride) * elem : kNowhere;
     }
     __syncthreads();
     constexpr int kAhead = 4;
@@ -278,15 +279,15 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const int v = v0 + u * kCopyThreads, r = v / per, c = (v - r * per) * (int)sizeof(V);
-        to[u] = v < have * per ? s_to[r] : -1;
-        if (to[u] < 0) continue;
+        to[u] = v < have * per ? s_to[r] : kNowhere;
+        if (to[u] == kNowhere) continue;
         k[u] = *reinterpret_cast<const V*>(static_cast<const char*>(p.from.k) + s_from[r] + c);
         w[u] = *reinterpret_cast<const V*>(static_cast<const char*>(p.from.v) + s_from[r] + c);
         to[u] += c;
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        if (to[u] < 0) continue;
+        if (to[u] == kNowhere) continue;
         *reinterpret_cast<V*>(static_cast<char*>(p.to.k) + to[u]) = k[u];
         *reinterpret_cast<V*>(static_cast<char*>(p.to.v) + to[u]) = w[u];
       }

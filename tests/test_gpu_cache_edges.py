@@ -3,6 +3,7 @@ the same call on whole inputs or their plain forms in 64 bits (tests/cache_refer
 tolerances)."""
 from __future__ import annotations
 
+import ctypes
 import importlib.util
 import sys
 from pathlib import Path
@@ -10,7 +11,7 @@ from pathlib import Path
 import numpy as np
 import pytest
 
-from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, i32, mass_inputs
+from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, evict_inputs, i32, mass_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -169,3 +170,48 @@ def test_the_example_keeps_all_slots_of_a_negative_budget(env, budget):
     assert a.isfinite().all()
     if isinstance(budget, int):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("backwards", ["heads", "rows", "pages", "all"])
+@pytest.mark.parametrize("side", ["from", "to", "both"])
+@pytest.mark.parametrize("D", [64, 51], ids=["vectors", "elements"])
+def test_evict_pools_of_negative_strides(env, backwards, side, D):
+    """A pool whose base is its last head, row or page, through the C entry: the same rows as in a pool that is flipped in memory."""
+    torch, stride, dev = env
+    from paper_2609_14636_gb300 import decode
+
+    case = ([70, 64, 90], 20, 3, D, 16, 8, "rows", 2, 5, "bf16")
+    dims = {"pages": [0], "rows": [1], "heads": [2], "all": [0, 1, 2]}[backwards]
+
+    def call(flip):
+        """Outputs, in the order of the pools that are not flipped."""
+        x = evict_inputs(torch, case, "spread")
+        i = dict(table=i32(torch, x["table"]), to=i32(torch, x["to_table"]), n=i32(torch, case[0]))
+        held = []
+
+        def cache(names, table, turned):
+            pools = [x[n].contiguous() for n in names]
+            strides, base = list(pools[0].stride()[:3]), 0
+            if turned:
+                pools = [p.flip(dims) for p in pools]
+                for d in dims:
+                    base += (pools[0].shape[d] - 1) * strides[d] * pools[0].element_size()
+                    strides[d] = -strides[d]
+            held.append((pools, turned))
+            return decode._PagedCache(pools[0].data_ptr() + base, pools[1].data_ptr() + base, *strides, *pools[0].shape[:3], 3, table.data_ptr(),
+                                      table.shape[1], i["n"].data_ptr(), None)
+
+        source, to = cache("kv", i["table"], flip and side != "to"), cache(["k_to", "v_to"], i["to"], flip and side != "from")
+        m, m2 = decode._slot_mass(x["mass"], "mass", 3, 3), decode._slot_mass(x["mass_to"], "mass_to", 3, 3)
+        how = decode._EvictParams(None, case[1], case[7], case[8], x["most"])
+        status = torch.zeros(1, dtype=torch.int32, device=dev)
+        torch.cuda.synchronize()
+        assert stride.lib().stride_kv_evict(ctypes.byref(source), ctypes.byref(m), ctypes.byref(to), 0, D, ctypes.byref(how),
+                                            x["new_len"].data_ptr(), x["kept"].data_ptr(), ctypes.byref(m2), status.data_ptr(), None) == 0
+        torch.cuda.synchronize()
+        assert int(status) == 0
+        pools, turned = held[1]
+        return [p.flip(dims) if turned else p for p in pools] + [x["new_len"], x["kept"], x["mass_to"]]
+
+    for got, want in zip(call(True), call(False)):
+        assert torch.equal(got, want)
