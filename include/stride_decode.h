@@ -211,6 +211,7 @@ typedef struct stride_slot_mass {
  * and adds nothing; keys that a row does not see may hold anything and change nothing
  * in its weights.  Sums are held in 32 bits, in an order that follows from the
  * sequence and from the mean of new tokens over the call's sequences alone: the same call gives the same bits.
+ * Of itself a weight is off by what its score is, and 2^-24 (|score| + |lse|) + 2^-23 |score - lse| + 2^-22 at most.
  *
  * A slot without a page: NaN and STRIDE_DEV_BAD_LAYOUT.  Sequences of a length that
  * the block table or mass->slots does not hold, or, under a tree mask, of more than

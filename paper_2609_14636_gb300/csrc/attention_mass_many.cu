@@ -616,6 +616,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint64_t* const taken = &bars.taken[team][place];
       const uint32_t my_scores = my + L::kScores + (team * L::kScorePlaces + place) * kPart;
       fence_after();
+      // (log2 e is in scale's and lse's factors: their roundings make 2^-24 (|score| + |lse|) of a weight, as lse's own in 32 bits does
+      // and a score's.  The difference first, its product after it: 32 trees of 13 tokens 82 us instead of 78, 4 chains of 511 94
+      // instead of 91; a factor of each column for what lse's leaves 82 and 98.)
       const auto add = [&](const uint32_t (&r)[32], const float4* lse) {
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {

@@ -11,7 +11,8 @@ from pathlib import Path
 import numpy as np
 import pytest
 
-from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, evict_inputs, i32, mass_inputs
+import decode_reference as dec
+from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, evict_inputs, i32, mass_inputs, sees_of, slots
 
 pytestmark = pytest.mark.gpu
 
@@ -129,6 +130,39 @@ def test_infinite_new_keys(env, shape):
             x["mass"][b, :, c + j] = finite[b, :, c + j]
         assert torch.equal(x["mass"], finite), (value, j)
         assert finite.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,Hq,Hk,D", [(1, 8, 2, 64), (13, 8, 2, 128), (20, 6, 1, 64), (90, 8, 2, 64), (81, 4, 1, 128)], ids=str)
+def test_large_scores(env, new, Hq, Hk, D, dtype):
+    """Scores of about 2,048 that are whole eighths, lse that are whole sixteenths, both exact in 32 bits: what is left of a weight's
+    error is what the header states.  Its factors scale log2 e and lse log2 e are rounded once each, 2^-24 (|s| + |lse|); the constant's
+    rounding is common to both, 2^-24 |s - lse|, and so is that of their difference; the exponential's is 2^-22.  A sum of R weights
+    and the masses' last one: (R + 2) 2^-24."""
+    torch, stride, dev = env
+    case = ([(300, new), (37, new)], Hq, Hk, D, 16, "rows", False, 1.0, dtype)
+    x = mass_inputs(torch, case)
+    for name in ("q", "k"):
+        x[name].copy_(torch.where(x[name] > 0.5, 1.0, torch.where(x[name] < -0.5, -1.0, 0.0)))
+        x[name][..., 0] = 128
+    x["scale"] = 0.125
+    x["lse"].copy_(2048 + 3 + torch.arange(Hq, device=dev) * 0.4375)  # (alike for all of a head's rows: roundings do not cancel)
+    x["mass"].zero_()
+    call_mass(stride, torch, x, case)
+    got, G = x["mass"].double().cpu().numpy(), Hq // Hk
+    q, lse = dec.f64(x["q"]), dec.f64(x["lse"])
+    for b, (c, n) in enumerate(case[0]):
+        K, sees = slots(x["k"], x["table"], b, c + n), sees_of(x, case, b)
+        for h in range(Hk):
+            rows, heads = slice(x["off"][b], x["off"][b] + n), slice(h * G, (h + 1) * G)
+            d = q[rows, heads] @ K[:, h].T * 0.125 - lse[rows, heads, None]  # [n, G, slots]
+            assert np.array_equal(d * 16, np.round(d * 16)) and np.abs(d).max() < 2.0 ** 8
+            e = np.exp(d) * sees[:, None]
+            want, R = e.sum((0, 1)), n * G
+            off = 2.0 ** -24 * (np.abs(d + lse[rows, heads, None]) + np.abs(lse[rows, heads, None])) + 2.0 ** -23 * np.abs(d) + 2.0 ** -22
+            tol = (e * np.expm1(off)).sum((0, 1)) + (R + 2) * 2.0 ** -24 * want
+            error = np.abs(got[b, h, :c + n] - want)
+            assert (error <= tol).all(), (b, h, (error / want).max(), (tol / want).min())
 
 
 # ---------------------------------------------------------------------------------------------------------------------
