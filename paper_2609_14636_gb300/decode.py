@@ -179,6 +179,14 @@ def _each(value, name: str, dtype, rows: int, convert):
     return None, convert(value)
 
 
+def _int32(value, name: str) -> int:
+    """A number that the C structs hold in 32 bits (ctypes would cut it)."""
+    v = int(value)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name} is {v}, beyond 32 bits")
+    return v
+
+
 # ---------------------------------------------------------------------------
 # the calls
 # ---------------------------------------------------------------------------
@@ -325,7 +333,8 @@ def stride_kv_evict(k_cache, v_cache, block_table, ctx_len, mass, budget, k_to, 
         raise ValueError("both caches must have the same heads and sequences")
     if not isinstance(kept, torch.Tensor) or kept.dim() != 3 or kept.shape[1] != source.n_heads:
         raise ValueError("kept must be int32 [sequences, kv heads, most]")
-    how = _EvictParams(*_each(budget, "budget", torch.int32, source.n_seqs, int), int(sink), int(recent), kept.shape[2])
+    how = _EvictParams(*_each(budget, "budget", torch.int32, source.n_seqs, lambda v: _int32(v, "budget")), _int32(sink, "sink"),
+                       _int32(recent, "recent"), _int32(kept.shape[2], "kept's row"))
     rc = _s.lib().stride_kv_evict(
         ctypes.byref(source), ctypes.byref(_slot_mass(mass, "mass", source.n_seqs, source.n_heads)), ctypes.byref(to), dt,
         k_cache.shape[3], ctypes.byref(how), _s._dev(new_len, "new_len", torch.int32, source.n_seqs),
@@ -363,7 +372,8 @@ def stride_logit_controls(logits, out, history=None, history_len=None, prompt_le
             raise TypeError("history must be an int32 CUDA tensor")
         if history.dim() != 2 or history.shape[0] < rows or (history.shape[1] > 1 and history.stride(1) != 1):
             raise ValueError("history must be [rows, longest] with unit column stride")
-        r.history, r.history_stride, r.history_most = history.data_ptr(), history.stride(0), history.shape[1]
+        r.history, r.history_stride = history.data_ptr(), history.stride(0)
+        r.history_most = _int32(history.shape[1], "history's row")
         r.history_len = _s._dev(history_len, "history_len", torch.int32, rows)
         r.prompt_len = _s._dev(prompt_len, "prompt_len", torch.int32, rows, optional=True)
     elif history_len is not None or prompt_len is not None:
@@ -377,7 +387,7 @@ def stride_logit_controls(logits, out, history=None, history_len=None, prompt_le
         r.bias_off = _s._dev(bias_off, "bias_off", torch.int32, rows + 1)
         r.bias = _s._dev(bias, "bias", torch.float32)
         r.bias_token = _s._dev(bias_token, "bias_token", torch.int32, bias.numel())
-        r.n_bias = bias.numel()
+        r.n_bias = _int32(bias.numel(), "biases")
     if allowed is not None:
         if not isinstance(allowed, torch.Tensor) or not allowed.is_cuda or allowed.dtype != torch.int32:
             raise TypeError("allowed must be an int32 CUDA tensor")

@@ -12,7 +12,7 @@ import numpy as np
 import pytest
 
 import decode_reference as dec
-from test_gpu_cache import BAD_LAYOUT, call_mass, check_mass, evict_inputs, i32, mass_inputs, sees_of, slots
+from test_gpu_cache import BAD_LAYOUT, call_evict, call_mass, check_mass, evict_inputs, i32, mass_inputs, outputs, sees_of, slots
 
 pytestmark = pytest.mark.gpu
 
@@ -249,3 +249,19 @@ def test_evict_pools_of_negative_strides(env, backwards, side, D):
 
     for got, want in zip(call(True), call(False)):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32, 2 ** 40, -2 ** 31 - 1, 10 ** 30], ids=str)
+@pytest.mark.parametrize("name", ["budget", "sink", "recent"])
+def test_evict_numbers_past_32_bits(env, name, big):
+    """Refused, not cut: 2^40 slots would be none, 2^31 a sequence that is left out."""
+    torch, stride, dev = env
+    case = ([70, 64], 20, 2, 64, 16, 16, "rows", 2, 5, "bf16")
+    x = evict_inputs(torch, case, "spread")
+    before = outputs(x)
+    case = case[:1] + (big if name == "budget" else 20,) + case[2:7] + (big if name == "sink" else 2, big if name == "recent" else 5) + case[9:]
+    with pytest.raises(ValueError, match=f"{name} is {big}, beyond 32 bits"):
+        call_evict(stride, torch, x, case)
+    torch.cuda.synchronize()
+    for k, t in before.items():
+        assert torch.equal(x[k], t)
