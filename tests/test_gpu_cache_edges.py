@@ -132,6 +132,30 @@ def test_infinite_new_keys(env, shape):
         assert finite.isfinite().all()
 
 
+@pytest.mark.parametrize("case", [
+    # trees (and a chain) of more than 256 rows a sequence: several blocks, whose columns' halves are of two warps; last blocks of few
+    # columns; groups that do not divide 128, and one of a token a block
+    ([(700, 64), (130, 60), (0, 50)], 32, 4, 128, 16, "rows", True, 0.9, "bf16"),
+    ([(700, 64), (0, 0), (130, 33), (5, 64)], 32, 4, 64, 8, "heads", True, 1.0, "f16"),
+    ([(300, 64), (40, 61), (0, 11)], 24, 1, 64, 16, "rows", True, 1.0, "bf16"),
+    ([(1000, 64), (90, 55), (127, 37)], 14, 2, 128, 24, "wide", True, 0.5, "f16"),
+    ([(90, 64), (64, 63), (3, 1)], 40, 4, 24, 32, "rows", True, 0.0, "bf16"),
+    ([(200, 13), (129, 3)], 128, 1, 64, 16, "rows", True, 1.0, "bf16"),
+    ([(200, 13), (129, 3), (0, 2)], 200, 2, 128, 16, "rows", False, 1.0, "f16"),
+    ([(2000, 64)] * 24, 16, 2, 128, 64, "rows", True, 0.9, "bf16"),
+], ids=str)
+def test_trees_of_many_rows(env, case):
+    torch, stride, dev = env
+    x = mass_inputs(torch, case)
+    before = x["mass"].double().cpu().numpy()
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    again = x["mass"].clone()
+    call_mass(stride, torch, x, case, status)
+    call_mass(stride, torch, x, case, mass=again)
+    assert int(status) == 0 and torch.equal(again, x["mass"])
+    check_mass(x, case, before, x["mass"].double().cpu().numpy(), skip=() if len(case[0]) < 9 else range(3, 23))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("new,Hq,Hk,D", [(1, 8, 2, 64), (13, 8, 2, 128), (20, 6, 1, 64), (90, 8, 2, 64), (81, 4, 1, 128)], ids=str)
 def test_large_scores(env, new, Hq, Hk, D, dtype):
