@@ -219,6 +219,9 @@ typedef struct stride_slot_mass {
  * STRIDE_DEV_TIMEOUT (as of stride_tree_attention): masses of the whole call hold
  * nothing of use.
  *
+ * One kernel takes the call, by the mean of new tokens: sequences of one token each and
+ * long chains are faster in calls of their own.
+ *
  * To let a prompt's last tokens alone vote, pass their rows of q and lse with ctx_len
  * moved on over the others and a decay of 0.
  *

@@ -304,7 +304,8 @@ cudaError_t launch_kv_evict(const EvictParams& p, int elem, int chunk, int sms, 
   int C = 1;
   while (C < kMaxCluster && (int64_t)units * C * 2 <= sms && slots > (int64_t)C * 1024) C *= 2;
   // (256 sequences of up to 4,096 slots, us: 256 threads of 16 masses each 343, 512 of 8 368; a cluster's, of up to 131,072 slots:
-  // 512 threads 45, 256 78)
+  // 512 threads 45, 256 78.  By what there is room for, as the host does not know the lengths: 256 of 4,096 with room for 32,768 take
+  // 402, with room for as many 375, L2 flushed.  Masses past 16 a thread are read again in each pass: eight of 131,072 355, one 50)
   const bool few = C == 1 && slots <= 4096;
   const auto kern = few ? select_kernel<256, 16, 5> : select_kernel<512, 16, 2>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);

@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 2) controls_kernel(const __grid_cons
   }
 
   // ---- the slice with the mask ----
-  if (apart) {
+  if (apart) {  // (an element at a time: 256 rows of 151,936 under a mask 147 us, 44 where both are alike, L2 flushed)
     T v[8];
     for (int c = c0 + tid; c < c1; c += 8 * kThreads) {
 #pragma unroll
